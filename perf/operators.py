@@ -217,7 +217,7 @@ def prepare_matmul(c, g):
     x = _randn(g, m, kk, dtype=torch.bfloat16)
     if not c["train"]:
         q, sc = _quantise(x, c["scale"])
-        return dict(s, x=q, xs=_stored(sc, c["scale"]))
+        return dict(s, x=q.contiguous(), xs=_stored(sc, c["scale"]))      # rows of `hidden` values back to back, as `run` says
     st = torch.uint8 if c["scale"] == "e8" else torch.float32
     wide = _blocks(m) * BLOCK + e * BLOCK                        # room for every group's rows, in whole blocks of 128
     s.update(x=x, dy=_randn(g, m, n, dtype=torch.bfloat16), wt=w.transpose(1, 2).contiguous(), wts=ws.transpose(1, 2).contiguous(),
