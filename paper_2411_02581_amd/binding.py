@@ -34,11 +34,21 @@ TUNA_MODE_AUTO, TUNA_MODE_STAGED, TUNA_MODE_FUSED = 0, 1, 2
 TUNA_T_SLOTS, TUNA_T_EXACT, TUNA_T_AUTO = 0, 1, 2
 TUNA_HOP_ENGINE, TUNA_HOP_TILED, TUNA_HOP_DIRECT, TUNA_HOP_ROWS, TUNA_HOP_LONG = 1, 2, 4, 8, 16
 
+# tuna_moe.h
+TUNA_F32, TUNA_BF16, TUNA_F8 = 0, 1, 2
+TUNA_SCALE_F32, TUNA_SCALE_E8 = 0, 1
+TUNA_ACT_NONE, TUNA_ACT_SWIGLU = 0, 1
+TUNA_ROUTE_RENORM = 1
+TUNA_MOE_MAX_EXPERTS, TUNA_MOE_MAX_K, TUNA_MOE_FEW_TOKENS = 1024, 16, 64
+
 EXPORTS = ("tuna_alltoallv", "tuna_alltoallv_hier", "tuna_alltoallv_noalloc", "tuna_alltoallv_ex", "tuna_alltoallv_init_ex",
            "tuna_opts_init", "tuna_ctx_create", "tuna_ctx_destroy", "tuna_ctx_get_stats", "tuna_build_id", "tuna_debug_phase_sizes", "tuna_workspace_bytes", "tuna_set_workspace",
            "tuna_release", "tuna_set_option", "tuna_get_stats", "tuna_plan_info", "tuna_plan_phase",
            "tuna_t_index", "tuna_plan_phase_device", "tuna_plan_phase_sources", "tuna_plain_copy", "tuna_select", "tuna_predict_ms", "tuna_calibrate", "tuna_model_constants", "tuna_alltoallv_init", "tuna_start", "tuna_plan_free",
            "tuna_strerror", "tuna_version")
+MOE_EXPORTS = ("tuna_moe_route", "tuna_moe_route_workspace", "tuna_moe_route_grad", "tuna_fp8_quantize", "tuna_fp8_quantize_columns",
+               "tuna_moe_swiglu_grad", "tuna_fp8_matmul", "tuna_fp8_matmul_grad_w", "tuna_moe_combine", "tuna_moe_combine_grad",
+               "tuna_moe_few", "tuna_moe_few_workspace")
 
 
 class tuna_phase_stats_t(ctypes.Structure):
@@ -140,10 +150,23 @@ def load() -> ctypes.CDLL:
     lib.tuna_plan_phase_sources.argtypes = [i, i, i, i, i, i, vp, i]
     lib.tuna_t_index.argtypes = [i, i]
     lib.tuna_plain_copy.argtypes = [vp, vp, ctypes.c_size_t, vp]
+    l, sz = ctypes.c_int64, ctypes.c_size_t
+    lib.tuna_moe_route.argtypes = [vp, i, l, l, i, i, i, vp, vp, vp, vp, l, vp, vp, vp, vp, vp, sz, vp]
+    lib.tuna_moe_route_workspace.argtypes = [l, i, i, i, ctypes.POINTER(sz)]
+    lib.tuna_moe_route_grad.argtypes = [vp, i, l, l, i, i, i, vp, vp, vp, vp, l, vp]
+    lib.tuna_fp8_quantize.argtypes = [vp, i, l, l, l, i, vp, i, l, vp, l, vp, l, i, vp]
+    lib.tuna_fp8_quantize_columns.argtypes = [vp, i, l, l, l, vp, i, vp, l, vp, l, i, vp]
+    lib.tuna_moe_swiglu_grad.argtypes = [vp, i, l, vp, l, l, l, vp, l, vp]
+    lib.tuna_fp8_matmul.argtypes = [vp, l, vp, l, vp, l, l, vp, l, l, i, vp, i, vp, i, l, l, l, l, vp]
+    lib.tuna_fp8_matmul_grad_w.argtypes = [vp, l, vp, l, vp, l, vp, l, i, vp, i, vp, i, l, l, l, l, l, vp]
+    lib.tuna_moe_combine.argtypes = [vp, i, l, l, vp, vp, l, i, l, vp, i, l, vp]
+    lib.tuna_moe_combine_grad.argtypes = [vp, i, l, vp, i, l, l, vp, vp, l, i, l, vp, l, vp, vp]
+    lib.tuna_moe_few.argtypes = [vp, l, l, l, vp, i, l, i, i, i, vp, vp, vp, vp, l, i, i, vp, i, l, vp, sz, vp]
+    lib.tuna_moe_few_workspace.argtypes = [l, l, l, i, i, ctypes.POINTER(sz)]
     lib.tuna_strerror.argtypes = [i]
     lib.tuna_strerror.restype = ctypes.c_char_p
     lib.tuna_version.argtypes = []
-    for name in EXPORTS:
+    for name in EXPORTS + MOE_EXPORTS:
         if name not in ("tuna_strerror", "tuna_build_id"):
             getattr(lib, name).restype = ctypes.c_int
     _lib = lib
@@ -413,3 +436,96 @@ def tuna_strerror(code: int) -> str:
 
 def tuna_version() -> int:
     return load().tuna_version()
+
+
+# ---------------------------------------------------------------------------------------------------- tuna_moe.h
+
+
+def _rows(a: Any, type_code: Optional[int] = None) -> Optional[int]:
+    """Device address of an array of rows: a tensor whose last axis is dense (the distance of its rows is an argument of
+    the call), or a plain integer address."""
+    if a is None or isinstance(a, int):
+        return a
+    if not a.is_cuda:
+        raise TypeError("device tensor expected")
+    if a.dim() and a.shape[-1] > 1 and a.stride(-1) != 1:
+        raise TypeError("a tensor with a dense last axis expected")
+    if type_code is not None and a.element_size() != (4, 2, 1)[type_code]:
+        raise TypeError("tensor dtype %s does not fit the type named" % a.dtype)
+    return a.data_ptr()
+
+
+def tuna_moe_route(logits, type: int, ld: int, n_tokens: int, n_experts: int, k: int, flags: int, experts, weights, slots, expert_rows,
+                   row_bytes: int, sendcounts, sdispls, recvcounts, rdispls, workspace, workspace_bytes: int, stream=None) -> int:
+    return load().tuna_moe_route(_rows(logits, type), type, ld, n_tokens, n_experts, k, flags, _ptr(experts), _ptr(weights), _ptr(slots),
+                                 _ptr(expert_rows), row_bytes, _ptr(sendcounts), _ptr(sdispls), _ptr(recvcounts), _ptr(rdispls),
+                                 _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def tuna_moe_route_workspace(n_tokens: int, n_experts: int, k: int, with_plan: bool):
+    """Returns (code, bytes).  Host only."""
+    out = ctypes.c_size_t(0)
+    rc = load().tuna_moe_route_workspace(n_tokens, n_experts, k, 1 if with_plan else 0, ctypes.byref(out))
+    return rc, int(out.value)
+
+
+def tuna_moe_route_grad(logits, type: int, ld: int, n_tokens: int, n_experts: int, k: int, flags: int, experts, weights, dweights,
+                        dlogits, ld_dlogits: int, stream=None) -> int:
+    return load().tuna_moe_route_grad(_rows(logits, type), type, ld, n_tokens, n_experts, k, flags, _ptr(experts), _ptr(weights),
+                                      _ptr(dweights), _rows(dlogits, type), ld_dlogits, _stream(stream))
+
+
+def tuna_fp8_quantize(x, type: int, ldx: int, rows: int, cols: int, act: int, slots, copies: int, out_rows: int, q, ldq: int,
+                      scales, ld_scales: int, scale_type: int, stream=None) -> int:
+    return load().tuna_fp8_quantize(_rows(x, type), type, ldx, rows, cols, act, _ptr(slots), copies, out_rows, _rows(q), ldq,
+                                    _rows(scales), ld_scales, scale_type, _stream(stream))
+
+
+def tuna_fp8_quantize_columns(x, type: int, ldx: int, rows: int, cols: int, group_rows, groups: int, q, ldq: int, scales,
+                              ld_scales: int, scale_type: int, stream=None) -> int:
+    return load().tuna_fp8_quantize_columns(_rows(x, type), type, ldx, rows, cols, _ptr(group_rows), groups, _rows(q), ldq,
+                                            _rows(scales), ld_scales, scale_type, _stream(stream))
+
+
+def tuna_moe_swiglu_grad(x, type: int, ldx: int, dh, ld_dh: int, rows: int, cols: int, dx, ld_dx: int, stream=None) -> int:
+    return load().tuna_moe_swiglu_grad(_rows(x, type), type, ldx, _rows(dh, type), ld_dh, rows, cols, _rows(dx, type), ld_dx, _stream(stream))
+
+
+def tuna_fp8_matmul(x, ldx: int, xs, ld_xs: int, w, ldw: int, w_group: int, ws, ld_ws: int, ws_group: int, scale_type: int,
+                    group_rows, groups: int, y, y_type: int, ldy: int, m: int, n: int, k: int, stream=None) -> int:
+    return load().tuna_fp8_matmul(_rows(x, TUNA_F8), ldx, _rows(xs), ld_xs, _rows(w, TUNA_F8), ldw, w_group, _rows(ws), ld_ws, ws_group,
+                                  scale_type, _ptr(group_rows), groups, _rows(y, y_type), y_type, ldy, m, n, k, _stream(stream))
+
+
+def tuna_fp8_matmul_grad_w(dyt, ld_dyt: int, dyt_scales, ld_dyt_scales: int, xt, ld_xt: int, xt_scales, ld_xt_scales: int, scale_type: int,
+                           group_rows, groups: int, dw, dw_type: int, ld_dw: int, dw_group: int, m: int, n: int, k: int, stream=None) -> int:
+    return load().tuna_fp8_matmul_grad_w(_rows(dyt, TUNA_F8), ld_dyt, _rows(dyt_scales), ld_dyt_scales, _rows(xt, TUNA_F8), ld_xt,
+                                         _rows(xt_scales), ld_xt_scales, scale_type, _ptr(group_rows), groups, _rows(dw, dw_type),
+                                         dw_type, ld_dw, dw_group, m, n, k, _stream(stream))
+
+
+def tuna_moe_combine(y, y_type: int, ldy: int, y_rows: int, slots, weights, n_tokens: int, k: int, cols: int, out, out_type: int,
+                     ld_out: int, stream=None) -> int:
+    return load().tuna_moe_combine(_rows(y, y_type), y_type, ldy, y_rows, _ptr(slots), _ptr(weights), n_tokens, k, cols,
+                                   _rows(out, out_type), out_type, ld_out, _stream(stream))
+
+
+def tuna_moe_combine_grad(dout, out_type: int, ld_dout: int, y, y_type: int, ldy: int, y_rows: int, slots, weights, n_tokens: int, k: int,
+                          cols: int, dy, ld_dy: int, dweights, stream=None) -> int:
+    return load().tuna_moe_combine_grad(_rows(dout, out_type), out_type, ld_dout, _rows(y, y_type), y_type, ldy, y_rows, _ptr(slots),
+                                        _ptr(weights), n_tokens, k, cols, _rows(dy, y_type), ld_dy, _ptr(dweights), _stream(stream))
+
+
+def tuna_moe_few(x, ldx: int, n_tokens: int, hidden: int, logits, logits_type: int, ld_logits: int, n_experts: int, k: int, flags: int,
+                 w1, s1, w2, s2, inner: int, weight_type: int, scale_type: int, out, out_type: int, ld_out: int,
+                 workspace, workspace_bytes: int, stream=None) -> int:
+    return load().tuna_moe_few(_rows(x, TUNA_BF16), ldx, n_tokens, hidden, _rows(logits, logits_type), logits_type, ld_logits, n_experts, k,
+                               flags, _ptr(w1), _ptr(s1), _ptr(w2), _ptr(s2), inner, weight_type, scale_type, _rows(out, out_type),
+                               out_type, ld_out, _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def tuna_moe_few_workspace(n_tokens: int, hidden: int, inner: int, n_experts: int, k: int):
+    """Returns (code, bytes).  Host only."""
+    out = ctypes.c_size_t(0)
+    rc = load().tuna_moe_few_workspace(n_tokens, hidden, inner, n_experts, k, ctypes.byref(out))
+    return rc, int(out.value)

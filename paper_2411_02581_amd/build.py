@@ -9,9 +9,10 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtuna.so")
-SOURCES = [os.path.join(CSRC, "tuna_api.hip")]
+SOURCES = [os.path.join(CSRC, "tuna_api.hip"), os.path.join(CSRC, "moe_api.hip")]
 HEADERS = [os.path.join(CSRC, "tuna_kernels.h"), os.path.join(CSRC, "tuna_plan.h"),
-           os.path.join(os.path.dirname(HERE), "include", "tuna.h")]
+           os.path.join(CSRC, "moe_kernels.h"),
+           os.path.join(os.path.dirname(HERE), "include", "tuna.h"), os.path.join(os.path.dirname(HERE), "include", "tuna_moe.h")]
 
 
 def source_hash() -> str:
@@ -30,6 +31,7 @@ def hipcc_command(out: str) -> list:
             "-DTUNA_BUILD_ID=\"%s\"" % source_hash(),
             # packed-FP32 instructions are not wanted in any code object of this library
             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+            "-I" + os.path.join(os.path.dirname(HERE), "include"),
             "-Wall", "-Wno-unused-function", "-Wno-unused-command-line-argument",
             "-o", out] + SOURCES
 

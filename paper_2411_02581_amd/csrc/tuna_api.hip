@@ -2824,6 +2824,12 @@ int calibrate(hipStream_t s) {
 
 using namespace tuna;
 
+// For the entry points of tuna_moe.h, which keep no state of their own.
+namespace tuna_host {
+__attribute__((visibility("hidden"))) int ensure_device() { return tuna::ensure_device(); }
+__attribute__((visibility("hidden"))) void note_hip_error(int code) { sh.last_hip_error = code; }
+}
+
 extern "C" {
 
 // Options of a call: the caller's struct where given (checked), else the process-wide defaults.

@@ -1,0 +1,630 @@
+"""The operators of include/tuna_moe.h on the GPU against their definitions in 64 bits (moe_plain.py)."""
+import math
+
+import pytest
+import torch
+
+import moe_plain as plain
+import paper_2411_02581_amd as tuna
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+CODE = {"f32": tuna.TUNA_F32, "bf16": tuna.TUNA_BF16}
+KIND = {"f32": tuna.TUNA_SCALE_F32, "e8": tuna.TUNA_SCALE_E8}
+STORED = {"f32": torch.float32, "e8": torch.uint8}
+EPS = 2.0 ** -24                                                 # half a unit in the last place of a 32-bit value
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def ok(rc):
+    assert rc == tuna.TUNA_OK, tuna.tuna_strerror(rc)
+
+
+def strided(x, ld=None, shift=0, fill=None):
+    """A copy of the CPU matrix `x` on the GPU whose rows lie `ld` apart, `shift` elements behind the start of its memory."""
+    rows, cols = x.shape
+    ld = ld or cols
+    mem = torch.full((shift + rows * ld + 64,), 0, dtype=x.dtype, device=DEV) if fill is None else \
+        torch.full((shift + rows * ld + 64,), fill, dtype=x.dtype, device=DEV)
+    v = mem[shift:shift + rows * ld].view(rows, ld)[:, :cols]
+    v.copy_(x)
+    return v
+
+
+def rounding(dtype):
+    return 2.0 ** -8 if dtype == "bf16" else 2 * EPS             # of one value, once
+
+
+# ------------------------------------------------------------------------------------------------ routing
+
+
+def gpu_route(logits, k, renorm, plan, row_bytes=48, ld=None, dtype="f32"):
+    t, e = logits.shape
+    d = strided(logits, ld)
+    rc, size = tuna.tuna_moe_route_workspace(t, e, k, plan)
+    ok(rc)
+    ws = torch.full((size + 16,), 0x5A, dtype=torch.uint8, device=DEV)
+    experts = torch.full((t, k), 77, dtype=torch.int32, device=DEV)
+    weights = torch.full((t, k), 77.0, device=DEV)
+    slots = torch.full((t, k), 77, dtype=torch.int32, device=DEV)
+    rows = torch.full((e + 1,), 77, dtype=torch.int32, device=DEV)
+    mats = [torch.full((e, e), 77, dtype=ty, device=DEV) for ty in (torch.int32, torch.int64) * 2] if plan else [None] * 4
+    flags = tuna.TUNA_ROUTE_RENORM if renorm else 0
+    ok(tuna.tuna_moe_route(d, CODE[dtype], d.stride(0), t, e, k, flags, experts, weights, slots, rows, row_bytes, *mats, ws, size))
+    torch.cuda.synchronize()
+    assert bool((ws[size:] == 0x5A).all())
+    return d, experts, weights, slots, rows, mats
+
+
+def check_route(logits, k, renorm, plan, ld=None, dtype="f32"):
+    logits = logits.to(TYPES[dtype])
+    t, e = logits.shape
+    d, experts, weights, slots, rows, mats = gpu_route(logits, k, renorm, plan, 48, ld, dtype)
+    p, want, w = plain.route(logits, k, renorm)
+    assert torch.equal(experts.cpu().long(), want)
+    # expf within an ulp, a sum of up to 1024 in 32 bits (at most 20 roundings deep), a division: 24 half ulps are enough for each side
+    assert torch.allclose(weights.cpu().double(), w, rtol=48 * EPS, atol=1e-37)
+    got = [v.cpu().long() for v in (slots, rows, *(m for m in mats if m is not None))]
+    for a, b in zip(got, plain.places(want, e, plan, 48)):
+        assert torch.equal(a, b)
+    g = torch.randn(t, k, generator=gen(9))
+    dl = torch.full((t, e + 3), 5.0, dtype=TYPES[dtype], device=DEV)
+    ok(tuna.tuna_moe_route_grad(d, CODE[dtype], d.stride(0), t, e, k, tuna.TUNA_ROUTE_RENORM if renorm else 0, experts, weights, g.to(DEV), dl, e + 3))
+    torch.cuda.synchronize()
+    exact = plain.route_grad(p, want, w, g.double(), renorm)
+    # p (g - s): every factor within 64 half ulps of what is added, then the output's rounding
+    room = 64 * EPS * (p if not renorm else 1.0) * (g.abs().sum(1, keepdim=True) + 1)
+    assert bool(((dl[:, :e].cpu().double() - exact).abs() <= room + rounding(dtype) * exact.abs() + 1e-37).all())
+    assert bool((dl[:, e:] == 5.0).all())
+
+
+@pytest.mark.parametrize("t,e,k", [(1, 1, 1), (1, 8, 2), (3, 5, 5), (24, 64, 4), (65, 60, 6), (64, 65, 8), (130, 128, 8), (257, 200, 8), (70, 256, 16),
+                                   (40, 1000, 8), (33, 1024, 16)])
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("plan", [False, True])
+def test_route(t, e, k, renorm, plan):
+    check_route(torch.randn(t, e, generator=gen(t * e)) * 3, k, renorm, plan)
+
+
+@pytest.mark.parametrize("plan", [False, True])
+def test_route_bf16_ties_and_strides(plan):
+    x = torch.randint(-3, 4, (150, 60), generator=gen(1)).float()      # many equal logits, +0 and -0 among them
+    x[::3][x[::3] == 0] = -0.0
+    check_route(x, 4, True, plan, ld=77, dtype="bf16")
+
+
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_route_masks(renorm, dtype):
+    x = torch.randn(90, 70, generator=gen(2))
+    x[::2, :60] = -math.inf
+    x[1::9, 3] = math.nan
+    x[2::9] = -math.inf                                          # nothing is left
+    x[3::9, :68] = -math.inf                                     # fewer than k
+    x[4::9] = torch.finfo(torch.bfloat16).min                    # the type's lowest value is a logit like others
+    x[5::9] = math.nan
+    x[6::9, [5, 50]] = math.inf
+    x[7::9, 69] = 1e30
+    check_route(x, 4, renorm, False, dtype=dtype)
+    check_route(x, 4, renorm, True, dtype=dtype)
+
+
+def test_route_of_many_tokens_and_of_none():
+    """Shards of several batches with and without a plan; no token at all."""
+    x = torch.randn(3000, 8, generator=gen(3))
+    check_route(x, 2, True, True)
+    check_route(x, 2, False, False)
+    x = torch.zeros(70000, 4)                                    # every token the same: shards of more than 64 tokens without a plan
+    _, experts, _, slots, rows, _ = gpu_route(x, 1, True, False)
+    assert bool((experts == 0).all()) and torch.equal(slots[:, 0].cpu(), torch.arange(70000, dtype=torch.int32))
+    assert rows.cpu().tolist() == [0] + [70000] * 4
+    for plan in (False, True):
+        out = gpu_route(torch.zeros(0, 6), 2, True, plan)
+        assert out[4].cpu().tolist() == [0] * 7
+        if plan:
+            assert all(int(m.abs().sum()) == 0 for m in out[5])
+
+
+@pytest.mark.parametrize("renorm", [False, True])
+def test_route_grad_against_differences(renorm):
+    t, e, k, h = 6, 20, 3, 2.0 ** -6
+    x = torch.randn(t, e, generator=gen(4)).sort(1).values[:, torch.randperm(e, generator=gen(5))]
+    top = x.topk(k + 1, 1)
+    x[torch.arange(t), top.indices[:, k]] -= 0.5                 # the choice does not change within h
+    g = torch.randn(t, k, generator=gen(6))
+    _, experts, weights, *_ = gpu_route(x, k, renorm, False)
+    dl = torch.empty(t, e, device=DEV)
+    flags = tuna.TUNA_ROUTE_RENORM if renorm else 0
+    ok(tuna.tuna_moe_route_grad(x.to(DEV), 0, e, t, e, k, flags, experts, weights, g.to(DEV), dl, e))
+    names = experts.cpu()
+    for i in range(e):
+        side = []
+        for s in (h, -h):
+            y = x.clone()
+            y[:, i] += s
+            _, ex, w, *_ = gpu_route(y, k, renorm, False)
+            ex, w = ex.cpu(), w.cpu().double()
+            # the order of the chosen may change: by name
+            val = [sum(float(g[r, j]) * float(w[r, (ex[r] == names[r, j]).nonzero()[0, 0]]) for j in range(k)) for r in range(t)]
+            side.append(torch.tensor(val, dtype=torch.float64))
+        d = (side[0] - side[1]) / (2 * h)
+        # third derivative of a softmax is below 1: h^2 / 6 of sum |g|; rounding of the weights over h
+        room = (h * h / 6 + 64 * EPS / h) * g.abs().sum(1)
+        assert bool(((dl[:, i].cpu().double() - d).abs() <= room).all())
+
+
+# ------------------------------------------------------------------------------------------------ quantisation
+
+
+def wild(rows, cols, seed):
+    """Values of many magnitudes; infinities, NaN, zeros, a block of zeros, the smallest and the largest values."""
+    x = torch.randn(rows, cols, generator=gen(seed)) * torch.exp(4 * torch.randn(rows, 1, generator=gen(seed + 1)))
+    f = x.view(-1)
+    n = f.numel()
+    for v in (math.inf, -math.inf, math.nan, 0.0, -0.0, 1e-42, 3e38, -1e-30):
+        f[int(torch.randint(0, n, (1,), generator=gen(seed + int(abs(hash(str(v))) % 97))))] = v
+    if rows > 2:
+        x[1, :130] = 0
+        x[2] = 1e-40
+    return x
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 128), (3, 129), (7, 1000), (20, 256), (5, 4099), (130, 72)])
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantise(rows, cols, kind, dtype):
+    x = wild(rows, cols, rows + cols).to(TYPES[dtype])
+    want, ws = plain.quantise(x, kind)
+    for ld, shift in ((cols, 0), (cols + 3, 1), ((cols + 15) // 8 * 8, 0)):
+        d = strided(x, ld, shift)
+        q = torch.full((rows, ld), 0xA5, dtype=torch.uint8, device=DEV)
+        s = torch.zeros(rows, plain.blocks(cols) + 1, dtype=STORED[kind], device=DEV)
+        ok(tuna.tuna_fp8_quantize(d, CODE[dtype], ld, rows, cols, tuna.TUNA_ACT_NONE, None, 1, rows, q, ld, s, s.shape[1], KIND[kind]))
+        torch.cuda.synchronize()
+        assert torch.equal(s[:, :-1].cpu(), ws)
+        got, nan = q[:, :cols].cpu(), (want & 127) == 127
+        assert torch.equal((got & 127) == 127, nan) and torch.equal(got[~nan], want[~nan])
+        assert bool((q[:, cols:] == 0xA5).all()) and bool((s[:, -1] == 0).all())
+
+
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+def test_quantise_to_slots(kind):
+    t, h, k, out = 50, 520, 3, 149
+    x = torch.randn(t, h, generator=gen(7)).bfloat16()
+    slots = torch.randperm(t * k, generator=gen(8)).int()
+    slots[slots == 149] = -1
+    slots[5] = 1 << 30 if slots[5] != -1 else -1                 # outside: skipped
+    lost = [r for r in range(out) if r not in slots.tolist()]
+    nb, one = plain.blocks(h), 1 if kind == "e8" else 4
+    rec = torch.full((out, (h + nb * one + 15) // 16 * 16), 0xEE, dtype=torch.uint8, device=DEV)
+    scales = rec[:, h:h + nb * one].view(STORED[kind])
+    ok(tuna.tuna_fp8_quantize(x.to(DEV), tuna.TUNA_BF16, h, t, h, tuna.TUNA_ACT_NONE, slots.view(t, k).to(DEV), k, out, rec, rec.shape[1], scales,
+                              scales.stride(0), KIND[kind]))
+    torch.cuda.synchronize()
+    want, ws = plain.quantise(x, kind)
+    for p, r in enumerate(slots.tolist()):
+        if 0 <= r < out:
+            assert torch.equal(rec[r, :h].cpu(), want[p // k]) and torch.equal(scales[r].cpu(), ws[p // k])
+    for r in lost:
+        assert bool((rec[r] == 0xEE).all())
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 8), (33, 200), (9, 1031), (100, 384)])
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_swiglu_quantised_and_its_gradient(rows, cols, kind, dtype):
+    x = (torch.randn(rows, 2 * cols, generator=gen(rows)) * 3).to(TYPES[dtype])
+    x[0, 0], x[0, cols - 1] = 100.0, -100.0
+    dh = torch.randn(rows, cols, generator=gen(rows + 1)).to(TYPES[dtype])
+    ld = 2 * cols + (0 if cols % 8 == 0 else 5)
+    d, q = strided(x, ld), torch.zeros(rows, cols, dtype=torch.uint8, device=DEV)
+    s = torch.zeros(rows, plain.blocks(cols), dtype=STORED[kind], device=DEV)
+    ok(tuna.tuna_fp8_quantize(d, CODE[dtype], ld, rows, cols, tuna.TUNA_ACT_SWIGLU, None, 1, rows, q, cols, s, s.shape[1], KIND[kind]))
+    g = torch.zeros(rows, 2 * cols, dtype=TYPES[dtype], device=DEV)
+    ok(tuna.tuna_moe_swiglu_grad(d, CODE[dtype], ld, dh.to(DEV), cols, rows, cols, g, 2 * cols))
+    torch.cuda.synchronize()
+    h = plain.swiglu(x)
+    peak = torch.nn.functional.pad(h.abs(), (0, -cols % 128)).unflatten(-1, (-1, 128)).amax(-1)
+    got = plain.scale_values(s.cpu(), kind)
+    if kind == "f32":
+        assert torch.allclose(got, peak / 448, rtol=16 * EPS)    # exp, a sum, a division, two products: 16 half ulps
+    else:
+        assert bool((got >= peak / 448 * (1 - 16 * EPS)).all()) and bool((got <= peak / 224 * (1 + 16 * EPS)).all())
+    # half a step of e4m3: 1/16 of the value, or half the smallest step; a rounding either way on top
+    v = plain.wide(q.cpu(), s.cpu(), kind)
+    sc = got.repeat_interleave(128, -1)[:, :cols]
+    assert bool(((v - h).abs() <= torch.maximum(h.abs() / 16, sc * 2.0 ** -10) * (1 + 64 * EPS) + 1e-30).all())
+    exact = plain.swiglu_grad(x, dh)
+    gate, up = x.double().chunk(2, -1)
+    room = 32 * EPS * torch.cat([dh.double().abs() * up.abs() * (1 + gate.abs()), dh.double().abs() * gate.abs()], -1)
+    assert bool(((g.cpu().double() - exact).abs() <= room + rounding(dtype) * exact.abs() + 1e-37).all())
+
+
+def test_swiglu_grad_against_differences():
+    x, d, h = torch.randn(4, 40, generator=gen(11)), torch.randn(4, 20, generator=gen(12)), 1e-4
+    g = torch.zeros(4, 40, device=DEV)
+    ok(tuna.tuna_moe_swiglu_grad(x.to(DEV), 0, 40, d.to(DEV), 20, 4, 20, g, 40))
+    for i in range(40):
+        e = torch.zeros(40, dtype=torch.float64)
+        e[i] = h
+        diff = ((plain.swiglu(x.double() + e) - plain.swiglu(x.double() - e)) * d.double()).sum(1) / (2 * h)
+        assert torch.allclose(g[:, i].cpu().double(), diff, rtol=1e-5, atol=1e-6)
+
+
+ROWS = [[0, 1], [0, 128], [0, 300], [0, 0, 5, 5, 140, 300, 300], [0, 129, 257, 258]]
+
+
+@pytest.mark.parametrize("bounds", ROWS)
+@pytest.mark.parametrize("cols", [1, 130, 256])
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantise_columns(bounds, cols, kind, dtype):
+    m, groups = bounds[-1], len(bounds) - 1
+    x = wild(m, cols, m + cols).to(TYPES[dtype])
+    nb = plain.blocks(m) + groups - 1
+    for ld, ldq in ((cols, nb * 128), (cols + 5, nb * 128 + 7), ((cols + 7) // 8 * 8, nb * 128 + 16)):
+        want, ws, used = plain.quantise_columns(x, bounds, kind, (ldq + 127) // 128 * 128)
+        q = torch.full((cols, ldq), 0xA5, dtype=torch.uint8, device=DEV)
+        s = torch.zeros(cols, nb, dtype=STORED[kind], device=DEV)
+        rows = torch.tensor(bounds, dtype=torch.int32, device=DEV) if groups > 1 else None
+        d = strided(x, ld)
+        ok(tuna.tuna_fp8_quantize_columns(d, CODE[dtype], ld, m, cols, rows, groups, q, ldq, s, nb, KIND[kind]))
+        torch.cuda.synchronize()
+        assert torch.equal(s[:, :used].cpu(), ws[:, :used])
+        got, want = q[:, :used * 128].cpu(), want[:, :used * 128]
+        nan = (want & 127) == 127
+        assert torch.equal((got & 127) == 127, nan) and torch.equal(got[~nan], want[~nan])
+        assert bool((q[:, used * 128:] == 0xA5).all())
+
+
+# ------------------------------------------------------------------------------------------------ products
+
+
+def codes(rows, cols, seed):
+    return plain.to_e4m3(torch.randn(rows, cols, generator=gen(seed), dtype=torch.float64) * 60)
+
+
+def some_scales(shape, kind, seed):
+    s = torch.exp2(torch.randint(-6, 7, shape, generator=gen(seed)).float())
+    if kind == "e8":
+        return (torch.log2(s) + 127).to(torch.uint8)
+    return s * (1 + torch.rand(shape, generator=gen(seed + 1)))
+
+
+def check_product(got, a, b, dtype, k):
+    """Products are exact in 32 bits, a block's sum has at most 127 roundings, each block two products and a sum more: every one of them relative to
+    the sum of the magnitudes.  For an output in bf16 the 8-bit matrix cores cut each of eight neighbouring products at 2^-13 of the largest."""
+    size = a.abs() @ b.abs().t()
+    exact = a @ b.t()
+    room = (127 + 4 * plain.blocks(k)) * EPS * size + rounding(dtype) * exact.abs()
+    if dtype == "bf16":
+        c, d, cut = a.abs().to(DEV), b.abs().to(DEV), torch.zeros(*exact.shape, dtype=torch.float64, device=DEV)
+        for at in range(0, a.shape[1], 8):
+            cut += (c[:, None, at:at + 8] * d[None, :, at:at + 8]).amax(-1)
+        room += 8 * 2.0 ** -13 * cut.cpu()
+    assert bool(((got.cpu().double() - exact).abs() <= room + 1e-37).all())
+
+
+def product(m, n, k, bounds, kind, dtype, pad=0, shift=0):
+    groups = len(bounds) - 1
+    x, xs = codes(m, k, m + k), some_scales((m, plain.blocks(k)), kind, 1)
+    w, ws = codes(groups * n, k, n + k), some_scales((groups * plain.blocks(n), plain.blocks(k)), kind, 2)
+    dx, dw = strided(x, k + pad, shift, 0x7F), strided(w, k + pad, shift, 0x7F)    # NaN between the rows
+    y = torch.full((m, n + pad), 9.0, dtype=TYPES[dtype], device=DEV)
+    rows = torch.tensor(bounds, dtype=torch.int32, device=DEV) if groups > 1 else None
+    ok(tuna.tuna_fp8_matmul(dx, k + pad, xs.to(DEV), plain.blocks(k), dw, k + pad, n * (k + pad), ws.to(DEV), plain.blocks(k),
+                            plain.blocks(n) * plain.blocks(k), KIND[kind], rows, groups, y, CODE[dtype], n + pad, m, n, k))
+    torch.cuda.synchronize()
+    a = plain.wide(x, xs, kind)
+    b = plain.wide(w.view(groups, n, k), ws.view(groups, plain.blocks(n), plain.blocks(k)), kind, 128)
+    for g in range(groups):
+        i, j = bounds[g], bounds[g + 1]
+        check_product(y[i:j, :n], a[i:j], b[g], dtype, k)
+    assert bool((y[:, n:] == 9.0).all())
+    assert bool((y[bounds[-1]:] == 9.0).all()) and bool((y[:bounds[0]] == 9.0).all())
+
+
+SHAPES = [(1, 1, 1), (1, 16, 128), (3, 130, 129), (16, 64, 256), (17, 33, 100), (64, 256, 512), (65, 257, 640), (130, 144, 1040), (200, 384, 304), (300, 520, 2048),
+          (513, 300, 272), (40, 2064, 384), (640, 640, 128)]
+
+
+@pytest.mark.parametrize("m,n,k", SHAPES)
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_matmul(m, n, k, kind, dtype):
+    product(m, n, k, [0, m], kind, dtype)
+
+
+@pytest.mark.parametrize("m,n,k,pad,shift", [(33, 70, 200, 3, 1), (33, 70, 208, 16, 0), (33, 64, 208, 0, 8), (150, 131, 257, 0, 0), (270, 260, 384, 32, 16)])
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+def test_matmul_strides_and_alignment(m, n, k, pad, shift, kind):
+    product(m, n, k, [0, m], kind, "bf16", pad, shift)
+
+
+@pytest.mark.parametrize("bounds", [[0, 0, 5, 5, 140, 300, 300], [0, 1, 2, 3, 4], [3, 70, 290], [0, 256, 512, 770], [0, 0, 0, 900]] +
+                         [list(range(0, 71)), [0] * 65 + [9, 700]])
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+@pytest.mark.parametrize("n,k", [(144, 272), (300, 128)])
+def test_matmul_of_groups(bounds, kind, n, k):
+    product(bounds[-1] + 2, n, k, bounds, kind, "f32")
+
+
+def test_matmul_group_bounds_are_held_inside():
+    """Bounds that descend, are negative or pass the rows: clamped, nothing outside is touched."""
+    m, n, k = 40, 32, 128
+    x, w = codes(m, k, 1).to(DEV), codes(3 * n, k, 2).to(DEV)
+    one = torch.ones(m, 1, device=DEV)
+    y = torch.full((m + 8, n), 9.0, device=DEV)
+    rows = torch.tensor([-5, 1000, 10, 2000000000], dtype=torch.int32, device=DEV)
+    ok(tuna.tuna_fp8_matmul(x, k, one, 1, w, k, n * k, torch.ones(3, 1, device=DEV), 1, 1, 0, rows, 3, y, 0, n, m, n, k))
+    torch.cuda.synchronize()
+    assert bool((y[m:] == 9.0).all()) and bool((y[:m] != 9.0).any())
+
+
+def test_matmul_of_nothing():
+    y = torch.full((5, 6), 9.0, device=DEV)
+    ok(tuna.tuna_fp8_matmul(None, 0, None, 0, None, 0, 0, None, 0, 0, 0, None, 1, y, 0, 6, 5, 6, 0))       # a sum of no terms
+    torch.cuda.synchronize()
+    assert bool((y == 0).all())
+    ok(tuna.tuna_fp8_matmul(None, 0, None, 0, None, 0, 0, None, 0, 0, 0, None, 1, None, 0, 6, 0, 6, 128))
+
+
+def test_matmul_not_a_number_stays_in_its_row():
+    m, n, k = 70, 130, 256
+    x, w = codes(m, k, 3), codes(n, k, 4)
+    x[5, 17], w[9, 200] = 0x7F, 0xFF
+    y = torch.zeros(m, n, device=DEV)
+    ok(tuna.tuna_fp8_matmul(x.to(DEV), k, torch.ones(m, 2, device=DEV), 2, w.to(DEV), k, 0, torch.ones(2, 2, device=DEV), 2, 0, 0, None, 1, y, 0, n, m, n, k))
+    nan = y.cpu().isnan()
+    assert bool(nan[5].all()) and bool(nan[:, 9].all()) and int(nan.sum()) == m + n - 1
+
+
+@pytest.mark.parametrize("bounds", ROWS + [[0, 700], [0, 500, 500, 513]])
+@pytest.mark.parametrize("n,k", [(1, 1), (70, 130), (128, 264), (272, 300)])
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_grad_w(bounds, n, k, kind, dtype):
+    m, groups = bounds[-1], len(bounds) - 1
+    nb = plain.blocks(m) + groups - 1
+    ld = nb * 128 + (16 if n != 70 else 1)
+    dy, x = torch.randn(m, n, generator=gen(1)), torch.randn(m, k, generator=gen(2))
+    side = []
+    for v in (dy, x):
+        q, s, used = plain.quantise_columns(v, bounds, kind, (ld + 127) // 128 * 128)
+        q[:, used * 128:] = 0x7F                                 # what lies behind is not read
+        side.append((q[:, :ld].contiguous(), s[:, :nb].contiguous()))
+    rows = torch.tensor(bounds, dtype=torch.int32, device=DEV) if groups > 1 else None
+    dw = torch.full((groups, n, k + 2), 9.0, dtype=TYPES[dtype], device=DEV)
+    d = [v.to(DEV) for p in side for v in p]
+    ok(tuna.tuna_fp8_matmul_grad_w(d[0], ld, d[1], nb, d[2], ld, d[3], nb, KIND[kind], rows, groups, dw, CODE[dtype], k + 2, n * (k + 2), m, n, k))
+    torch.cuda.synchronize()
+    at = 0
+    for g in range(groups):
+        c = plain.blocks(bounds[g + 1] - bounds[g])
+        a, b = (plain.wide(q[:, at * 128:(at + c) * 128], s[:, at:at + c], kind) if c else torch.zeros(q.shape[0], 0).double() for q, s in side)
+        check_product(dw[g, :, :k], a, b, dtype, max(c, 1) * 128)
+        at += c
+    assert bool((dw[:, :, k:] == 9.0).all())
+
+
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+def test_products_are_each_others_gradients(kind):
+    """The product is linear in each side, so its difference in the direction of a side is the product itself: <y, dy> = <x, dx> = <w, dw>, with x, dy
+    of values that 8 bits hold in either direction."""
+    m, n, k = 256, 272, 384
+    grid = lambda seed, *s: torch.randint(-8, 9, s, generator=gen(seed)).double()  # noqa: E731
+    x, dy, w = grid(1, m, k), grid(2, m, n), grid(3, n, k)
+    x[::7], dy[::5] = 448 / 64, 448 / 64
+    to = lambda v: plain.to_e4m3(v).contiguous().to(DEV)  # noqa: E731
+    ones = lambda *s: torch.ones(*s, device=DEV) if kind == "f32" else torch.full(s, 127, dtype=torch.uint8, device=DEV)  # noqa: E731
+    y, dx, dw = torch.zeros(m, n, device=DEV), torch.zeros(m, k, device=DEV), torch.zeros(n, k, device=DEV)
+    ok(tuna.tuna_fp8_matmul(to(x), k, ones(m, 3), 3, to(w), k, 0, ones(3, 3), 3, 0, KIND[kind], None, 1, y, 0, n, m, n, k))
+    ok(tuna.tuna_fp8_matmul(to(dy), n, ones(m, 3), 3, to(w.t()), n, 0, ones(3, 3), 3, 0, KIND[kind], None, 1, dx, 0, k, m, k, n))
+    ok(tuna.tuna_fp8_matmul_grad_w(to(dy.t()), m, ones(n, 2), 2, to(x.t()), m, ones(k, 2), 2, KIND[kind], None, 1, dw, 0, k, 0, m, n, k))
+    torch.cuda.synchronize()
+    a = (y.cpu().double() * dy).sum()
+    assert a == (dx.cpu().double() * x).sum() == (dw.cpu().double() * w).sum()   # whole numbers below 2^24: exact
+    assert torch.equal(y.cpu().double(), x @ w.t())
+
+
+# ------------------------------------------------------------------------------------------------ the sum over the experts
+
+
+@pytest.mark.parametrize("t,k,cols", [(1, 1, 1), (5, 2, 8), (24, 4, 2048), (70, 8, 1003), (9, 16, 2600)])
+@pytest.mark.parametrize("yt", ["f32", "bf16"])
+@pytest.mark.parametrize("ot", ["f32", "bf16"])
+def test_combine_and_its_gradient(t, k, cols, yt, ot):
+    rows = max(1, t * k - 2)
+    y, dout = torch.randn(rows, cols, generator=gen(1)).to(TYPES[yt]), torch.randn(t, cols, generator=gen(2)).to(TYPES[ot])
+    w = torch.rand(t, k, generator=gen(3))
+    slots = torch.randperm(t * k, generator=gen(4)).int().view(t, k)
+    slots[slots >= rows] = -1 if t % 2 else 1 << 29              # absent
+    if t > 4:
+        slots[3] = -1
+    for ld in (cols, cols + 3, (cols + 7) // 8 * 8):
+        dy_, dd, out = strided(y, ld), strided(dout, ld), torch.full((t, ld), 9.0, dtype=TYPES[ot], device=DEV)
+        ok(tuna.tuna_moe_combine(dy_, CODE[yt], ld, rows, slots.to(DEV), w.to(DEV), t, k, cols, out, CODE[ot], ld))
+        g, dw = torch.full((rows, ld), 9.0, dtype=TYPES[yt], device=DEV), torch.full((t, k), 9.0, device=DEV)
+        ok(tuna.tuna_moe_combine_grad(dd, CODE[ot], ld, dy_, CODE[yt], ld, rows, slots.to(DEV), w.to(DEV), t, k, cols, g, ld, dw))
+        torch.cuda.synchronize()
+        exact, size = plain.combine(y, slots, w), plain.combine(y.abs(), slots, w)
+        assert bool(((out[:, :cols].cpu().double() - exact).abs() <= 2 * k * EPS * size + rounding(ot) * exact.abs() + 1e-37).all())
+        assert bool((out[:, cols:] == 9.0).all()) and bool((g[:, cols:] == 9.0).all())
+        seen = set()
+        for i in range(t):
+            for j in range(k):
+                r = int(slots[i, j])
+                if not 0 <= r < rows:
+                    assert float(dw[i, j]) == 0.0
+                    continue
+                seen.add(r)
+                want = float(w[i, j]) * dout[i].double()
+                assert bool(((g[r, :cols].cpu().double() - want).abs() <= (rounding(yt) + EPS) * want.abs() + 1e-37).all())
+                dot = float((dout[i].double() * y[r].double()).sum())
+                # a thread adds cols / 256 products and there are 8 more sums: far fewer roundings than cols / 16 + 40
+                assert abs(float(dw[i, j]) - dot) <= (cols / 16 + 40) * EPS * float((dout[i].double() * y[r].double()).abs().sum()) + 1e-37
+        for r in set(range(rows)) - seen:
+            assert bool((g[r] == 9.0).all())
+
+
+def test_combine_grad_against_differences():
+    """Linear in y and in the weights: differences over a step of one are the gradient."""
+    t, k, cols = 5, 2, 24
+    y, w, d = torch.randn(t * k, cols, generator=gen(1)), torch.rand(t, k, generator=gen(2)), torch.randn(t, cols, generator=gen(3))
+    slots = torch.randperm(t * k, generator=gen(4)).int().view(t, k)
+
+    def loss(y, w):
+        out = torch.empty(t, cols, device=DEV)
+        ok(tuna.tuna_moe_combine(y.to(DEV), 0, cols, t * k, slots.to(DEV), w.to(DEV), t, k, cols, out, 0, cols))
+        return (out.cpu().double() * d.double()).sum(1)
+
+    g, dw = torch.zeros(t * k, cols, device=DEV), torch.zeros(t, k, device=DEV)
+    ok(tuna.tuna_moe_combine_grad(d.to(DEV), 0, cols, y.to(DEV), 0, cols, t * k, slots.to(DEV), w.to(DEV), t, k, cols, g, cols, dw))
+    for j in range(k):
+        e = torch.zeros(t, k)
+        e[:, j] = 1
+        assert torch.allclose(dw[:, j].cpu().double(), loss(y, w + e) - loss(y, w), atol=1e-4)
+    for c in range(0, cols, 5):
+        e = torch.zeros(t * k, cols)
+        e[slots[:, 0].long(), c] = 1
+        assert torch.allclose(g[slots[:, 0].long(), c].cpu().double(), loss(y + e, w) - loss(y, w), atol=1e-4)
+
+
+# ------------------------------------------------------------------------------------------------ the layer for a few tokens
+
+
+def few(t, h, f, e, k, weights, kind="f32", renorm=True, dtype="bf16", logits=None, lt="f32", shift=0):
+    x = torch.randn(t, h, generator=gen(1)).bfloat16()
+    logits = (torch.randn(t, e, generator=gen(2)) * 2 if logits is None else logits).to(TYPES[lt])
+    dev, vals = [], []
+    for i, (r, c) in enumerate(((2 * f, h), (h, f))):
+        if weights == "f8":
+            q = codes(e * r, c, 3 + i)
+            s = some_scales((e, plain.blocks(r), plain.blocks(c)), "e8", 5 + i).float()
+            s = (s - 10).to(torch.uint8) if kind == "e8" else torch.exp2(s - 137) * (1 + torch.rand(s.shape, generator=gen(7 + i)))
+            vals.append(plain.wide(q.view(e, r, c), s, kind, 128))
+            dev += [q.to(DEV), s.to(DEV)]
+        else:
+            q = (torch.randn(e, r, c, generator=gen(3 + i)) * 0.1).bfloat16()
+            vals.append(q.double())
+            mem = torch.zeros(q.numel() + 64, dtype=torch.bfloat16, device=DEV)
+            v = mem[shift:shift + q.numel()].view(e, r, c)
+            v.copy_(q)
+            dev += [v, None]
+    rc, size = tuna.tuna_moe_few_workspace(t, h, f, e, k)
+    ok(rc)
+    ws = torch.full((size + 16,), 0xFF, dtype=torch.uint8, device=DEV)     # NaN where nothing is written
+    out = torch.full((t, h + 1), 9.0, dtype=TYPES[dtype], device=DEV)
+    dx, dl = strided(x, h + (8 if h % 8 == 0 else 1)), strided(logits, e + 2)
+    wt = tuna.TUNA_F8 if weights == "f8" else tuna.TUNA_BF16
+    for _ in range(2):
+        ok(tuna.tuna_moe_few(dx, dx.stride(0), t, h, dl, CODE[lt], e + 2, e, k, tuna.TUNA_ROUTE_RENORM if renorm else 0, *dev, f, wt, KIND[kind], out,
+                             CODE[dtype], h + 1, ws, size))
+    torch.cuda.synchronize()
+    assert bool((ws[size:] == 0xFF).all()) and bool((out[:, h:] == 9.0).all())
+    exact, size = plain.few(x, logits, k, renorm, *vals)
+    # an activation: sums of `h` terms twice, relative to the magnitudes added, which are at most some sqrt(h) times the sum; kept in two bf16 parts
+    # (2^-16); then sums of f terms: an error of 2^-13 of the magnitudes that the second product adds is far above all of them
+    assert bool(((out[:, :h].cpu().double() - exact).abs() <= 2.0 ** -13 * size + rounding(dtype) * exact.abs() + 1e-30).all())
+
+
+@pytest.mark.parametrize("t,h,f,e,k", [(1, 128, 64, 8, 2), (1, 256, 100, 60, 4), (2, 300, 48, 5, 5), (7, 384, 144, 16, 1), (17, 520, 72, 12, 4), (64, 256, 128, 8, 3),
+                                       (33, 136, 40, 100, 8), (64, 128, 32, 3, 2), (5, 1040, 1040, 4, 2)])
+@pytest.mark.parametrize("weights,kind", [("f8", "f32"), ("f8", "e8"), ("bf16", "f32")])
+def test_few(t, h, f, e, k, weights, kind):
+    few(t, h, f, e, k, weights, kind, renorm=t % 2 == 0)
+
+
+def test_few_types_and_alignment():
+    few(9, 200, 88, 10, 3, "f8", "f32", dtype="f32", lt="bf16")
+    few(9, 208, 80, 10, 3, "bf16", dtype="f32", shift=1)
+    few(9, 201, 83, 10, 3, "f8", "e8")
+    few(9, 201, 83, 10, 3, "bf16")
+
+
+@pytest.mark.parametrize("renorm", [False, True])
+def test_few_masks(renorm):
+    l = torch.randn(20, 12, generator=gen(8))
+    l[0] = -math.inf
+    l[1] = math.nan
+    l[2, 1:] = -math.inf
+    l[3, ::2] = -math.inf
+    l[4, 3] = math.inf
+    l[5] = 1.0
+    few(20, 144, 48, 12, 4, "f8", "f32", renorm, logits=l)
+    few(20, 144, 48, 12, 4, "f8", "f32", renorm, logits=torch.full((20, 12), -math.inf))
+
+
+def test_few_of_no_token():
+    ok(tuna.tuna_moe_few(None, 8, 0, 8, None, 0, 4, 4, 2, 0, None, None, None, None, 8, tuna.TUNA_BF16, 0, None, 0, 8, None, 0))
+
+
+# ------------------------------------------------------------------------------------------------ streams and graphs
+
+
+def test_on_a_stream_of_its_own_and_in_a_graph():
+    t, e, k, h = 40, 16, 2, 256
+    logits, y = torch.randn(t, e, device=DEV), torch.randn(t * k, h, device=DEV)
+    rc, size = tuna.tuna_moe_route_workspace(t, e, k, True)
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    new = lambda: [torch.zeros(t, k, dtype=torch.int32, device=DEV), torch.zeros(t, k, device=DEV), torch.zeros(t, k, dtype=torch.int32, device=DEV),  # noqa: E731
+                   torch.zeros(e + 1, dtype=torch.int32, device=DEV), torch.zeros(t, h, device=DEV)]
+    mats = [torch.zeros(e, e, dtype=ty, device=DEV) for ty in (torch.int32, torch.int64) * 2]
+
+    def step(o):
+        ok(tuna.tuna_moe_route(logits, 0, e, t, e, k, 1, *o[:4], 64, *mats, ws, size))
+        ok(tuna.tuna_moe_combine(y, 0, h, t * k, o[2], o[1], t, k, h, o[4], 0, h))
+
+    eager = new()
+    step(eager)
+    s, other = torch.cuda.Stream(), new()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step(other)
+        graph, kept = torch.cuda.CUDAGraph(), new()
+    s.synchronize()
+    with torch.cuda.graph(graph, stream=s):
+        step(kept)
+    for a, b in zip(eager, other):
+        assert torch.equal(a, b)
+    for n in range(3):
+        logits.copy_(torch.randn(t, e, generator=gen(n)))
+        step(eager)
+        for v in kept:
+            v.fill_(0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(eager, kept):
+            assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------------------------------------ the operators together
+
+
+@pytest.mark.parametrize("tokens,hidden,inner,experts,k,per_node", [(90, 384, 144, 12, 3, 4), (50, 272, 96, 8, 2, 0), (5, 128, 48, 16, 4, 0)])
+def test_a_layer_through_the_all_to_all(tokens, hidden, inner, experts, k, per_node):
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import expert_parallel
+    layer, x, logits, out, step = expert_parallel.main(tokens, hidden, inner, experts, k, per_node)
+    x, logits = x.cpu(), logits.cpu()
+    _, names, weights = plain.route(logits, k, True)
+    w1, w2 = (plain.wide(q.view(torch.uint8).cpu(), s.cpu(), "e8", 128) for q, s in ((layer.w1, layer.s1), (layer.w2, layer.s2)))
+    again = lambda v: plain.wide(*plain.quantise(v, "e8"), "e8")  # noqa: E731
+    want = torch.zeros(tokens, hidden, dtype=torch.float64)
+    xq = again(x)
+    for t in range(tokens):
+        for j in range(k):
+            e = int(names[t, j])
+            h = again(plain.swiglu((w1[e] @ xq[t]).bfloat16())[None])[0]
+            want[t] += weights[t, j] * (w2[e] @ h).bfloat16().double()
+    # the same roundings on both sides but where a value lies at a rounding's edge: a few in a hundred of the activations, by a step of bf16 (2^-8) and
+    # fewer by one of e4m3 (2^-3); and the last rounding
+    assert (out.cpu().double() - want).norm() <= 0.01 * want.norm()
+    exact, _ = plain.few(x[:step.shape[0]], logits[:step.shape[0]], k, True, w1, w2)
+    assert (step.cpu().double() - exact).norm() <= 2.0 ** -8 * exact.norm()
