@@ -683,6 +683,189 @@ __global__ __launch_bounds__(256) void k_product64(Product P) {
         }
 }
 
+// Sixteen bytes a lane (or a scale a lane, as a word) from memory straight into the LDS, lane after lane behind `to`.
+template <int BYTES> __device__ __forceinline__ void to_lds(const void* from, void* to) {
+    const auto* g = (const __attribute__((address_space(1))) void*)from;
+    auto* l = (__attribute__((address_space(3))) void*)to;
+    if constexpr (BYTES == 16) __builtin_amdgcn_global_load_lds(g, l, 16, 0, 0);
+    else if constexpr (BYTES == 4) __builtin_amdgcn_global_load_lds(g, l, 4, 0, 0);
+    else __builtin_amdgcn_global_load_lds(g, l, 1, 0, 0);
+}
+
+// Workgroups go to the eight XCDs in turn: each XCD gets a run of neighbouring tiles, whose operands meet in its L2.
+__device__ __forceinline__ unsigned xcd_run(unsigned id, unsigned total) {
+    const unsigned per = total / 8, more = total % 8, x = id % 8;
+    return x * per + (x < more ? x : more) + id / 8;
+}
+
+// The large form: a tile of BM x BN, WM x WN waves, blocks of 128 in turn through two halves of the LDS: while one is multiplied the next
+// one is on its way.  A row's sixteens lie in the LDS at their place xor (row mod 8), so that neighbouring rows' reads meet no bank twice;
+// the lanes load them in that order.
+template <int KIND, bool COLS, class OUT, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64, 2) void k_product(Product P, int m_tiles, int n_tiles) {
+    constexpr int W = WM * WN, MT = BM / (16 * WM), NT = BN / (16 * WN), LA = BM / 8 / W, LB = BN / 8 / W;
+    constexpr bool CORE8 = sizeof(OUT) == 2;
+    static_assert(LA * 8 * W == BM && LB * 8 * W == BN && (BM + BN) / 64 <= W, "");
+    __shared__ __align__(1024) uint8_t tile[2][(BM + BN) * kBlock];
+    __shared__ __align__(16) unsigned scale[2][BM + BN];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w / WN, wn = w % WN;
+    unsigned id = xcd_run(blockIdx.x, gridDim.x);
+    int group = 0;
+    if (COLS) { group = id / (m_tiles * n_tiles); id -= group * (m_tiles * n_tiles); }
+    // runs of four rows of tiles, column after column
+    const unsigned run = id / (4 * n_tiles), in_run = id - run * 4 * n_tiles, height = m_tiles - run * 4 < 4 ? m_tiles - run * 4 : 4;
+    const int ti = run * 4 + in_run % height, tj = in_run / height;
+    int64_t i0, i_end, kb0 = 0, kb1;
+    const int64_t j0 = (int64_t)tj * BN;
+    if (COLS) {
+        i0 = (int64_t)ti * BM;
+        i_end = i0 + BM < P.m ? i0 + BM : P.m;
+        int64_t count;
+        group_blocks(P.group_rows, group, P.k, kb0, count);
+        kb1 = kb0 + count;
+    } else {
+        const Place pl = find_tile(P.group_rows, P.groups, P.m, BM, ti);
+        if (pl.group < 0) return;
+        group = pl.group; i0 = pl.first; i_end = pl.end;
+        kb1 = blocks_of(P.k);
+    }
+    i0 = (int64_t)__builtin_amdgcn_readfirstlane((int)i0);
+    i_end = (int64_t)__builtin_amdgcn_readfirstlane((int)i_end);
+    group = __builtin_amdgcn_readfirstlane(group);
+    kb0 = __builtin_amdgcn_readfirstlane((int)kb0);
+    kb1 = __builtin_amdgcn_readfirstlane((int)kb1);
+    const uint8_t* a = P.a + i0 * P.lda;
+    const uint8_t* b = P.b + (COLS ? 0 : group * P.b_group) + j0 * P.ldb;
+    const int rows_a = (int)(i_end - i0), rows_b = (int)(P.n - j0 < BN ? P.n - j0 : BN);
+    const int sixteen = ((lane & 7) ^ (lane >> 3)) * 16;
+    unsigned at_a[LA], at_b[LB];
+#pragma unroll
+    for (int j = 0; j < LA; ++j) {
+        const int r = (w * LA + j) * 8 + (lane >> 3);
+        at_a[j] = (unsigned)((r < rows_a ? r : rows_a - 1) * P.lda) + sixteen;
+    }
+#pragma unroll
+    for (int j = 0; j < LB; ++j) {
+        const int r = (w * LB + j) * 8 + (lane >> 3);
+        at_b[j] = (unsigned)((r < rows_b ? r : rows_b - 1) * P.ldb) + sixteen;
+    }
+    const uint8_t* at_s = nullptr;                                // this lane's row of scales
+    constexpr int SS = KIND == TUNA_SCALE_E8 ? 1 : 4;
+    if (w < BM / 64) {
+        const int r = w * 64 + lane;
+        at_s = (const uint8_t*)P.as + (i0 + (r < rows_a ? r : rows_a - 1)) * P.ld_as * SS;
+    } else if (w < (BM + BN) / 64) {
+        const int r = w * 64 + lane - BM;
+        const int64_t row = j0 + (r < rows_b ? r : rows_b - 1);
+        at_s = (const uint8_t*)P.bs + ((COLS ? 0 : group * P.bs_group) + (COLS ? row : row / kBlock) * P.ld_bs) * SS;
+    }
+    auto issue = [&](int64_t kb, int half) {
+        const int left = (int)(P.k - kb * kBlock < kBlock ? P.k - kb * kBlock : kBlock);
+        const uint8_t *ga = a + kb * kBlock, *gb = b + kb * kBlock;
+        uint8_t *la = tile[half] + w * LA * 1024, *lb = tile[half] + BM * kBlock + w * LB * 1024;
+        if (COLS || left == kBlock) {
+#pragma unroll
+            for (int j = 0; j < LA; ++j) to_lds<16>(ga + at_a[j], la + j * 1024);
+#pragma unroll
+            for (int j = 0; j < LB; ++j) to_lds<16>(gb + at_b[j], lb + j * 1024);
+        } else {                                                  // the row ends inside the block: zeros behind it
+            const v4u zero = {0u, 0u, 0u, 0u};
+            if (sixteen < left) {
+#pragma unroll
+                for (int j = 0; j < LA; ++j) to_lds<16>(ga + at_a[j], la + j * 1024);
+#pragma unroll
+                for (int j = 0; j < LB; ++j) to_lds<16>(gb + at_b[j], lb + j * 1024);
+            } else {
+#pragma unroll
+                for (int j = 0; j < LA; ++j) *(v4u*)(la + j * 1024 + lane * 16) = zero;
+#pragma unroll
+                for (int j = 0; j < LB; ++j) *(v4u*)(lb + j * 1024 + lane * 16) = zero;
+            }
+        }
+        if (w < (BM + BN) / 64) to_lds<SS>(at_s + kb * SS, &scale[half][w * 64]);
+    };
+    v4f acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    if (kb0 < kb1) issue(kb0, 0);
+    const int r = lane & 15, c0 = (((lane >> 4) * 2) ^ (r & 7)) * 16, c1 = (((lane >> 4) * 2 + 1) ^ (r & 7)) * 16;
+    int half = 0;
+    for (int64_t kb = kb0; kb < kb1; ++kb, half ^= 1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (kb + 1 < kb1) issue(kb + 1, half ^ 1);
+        const uint8_t *ta = tile[half] + (wm * MT * 16 + r) * kBlock, *tb = tile[half] + (BM + wn * NT * 16 + r) * kBlock;
+        const unsigned *sa = scale[half] + wm * MT * 16, *sb = scale[half] + BM + wn * NT * 16;
+        auto fragment = [&](const uint8_t* t) {
+            const v4u x = *(const v4u*)(t + c0), y = *(const v4u*)(t + c1);
+            return v8i{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+        };
+        v8i fb[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) fb[j] = fragment(tb + j * 16 * kBlock);
+        if (CORE8 && KIND == TUNA_SCALE_E8) {
+            unsigned kbs[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) kbs[j] = sb[j * 16 + r];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const v8i fa = fragment(ta + i * 16 * kBlock);
+                const unsigned ka = sa[i * 16 + r];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = mma<KIND>(fb[j], fa, acc[i][j], kbs[j], ka);
+            }
+        } else {
+            // by columns every row of b has a scale of its own, else these rows share one
+            v4f kbs[NT];
+            float one = 1.f;
+            if (COLS) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) kbs[j][q] = scale_float<KIND>(sb[j * 16 + (lane >> 4) * 4 + q]);
+            } else {
+                one = scale_float<KIND>(sb[0]);
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const v8i fa = fragment(ta + i * 16 * kBlock);
+                const float ka = scale_float<KIND>(sa[i * 16 + r]) * one;
+                const v4f zero = {0.f, 0.f, 0.f, 0.f};
+                v4f p[NT];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) p[j] = CORE8 ? mma<TUNA_SCALE_F32>(fb[j], fa, zero, 0, 0) : mma_wide(fb[j], fa, zero);
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[i][j][q] += COLS ? p[j][q] * kbs[j][q] * ka : p[j][q] * ka;
+            }
+        }
+    }
+    const bool even = P.n % 4 == 0 && P.ldo % 4 == 0 && P.out_group % 4 == 0 && ((uintptr_t)P.out & (4 * sizeof(OUT) - 1)) == 0;
+    OUT* out = (OUT*)P.out + (COLS ? group * P.out_group : 0);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t row = i0 + (wm * MT + i) * 16 + r;
+        if (row >= i_end) continue;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int64_t col = j0 + (wn * NT + j) * 16 + (lane >> 4) * 4;
+            if (col >= P.n) continue;
+            OUT* o = out + row * P.ldo + col;
+            const v4f v = acc[i][j];
+            if (even) {
+                if (sizeof(OUT) == 2) *(v2u*)o = v2u{(unsigned)to_bf16(v[0]) | (unsigned)to_bf16(v[1]) << 16, (unsigned)to_bf16(v[2]) | (unsigned)to_bf16(v[3]) << 16};
+                else *(v4f*)o = v;
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) if (col + q < P.n) store1(o + q, v[q]);
+            }
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ the sum over a token's experts
 
 template <class Y, class O, bool WIDE>
