@@ -41,7 +41,6 @@ inline int launched() {
 template <class F> inline void with_type(int type, F f) {
     if (type == TUNA_F32) f((float*)nullptr); else f((unsigned short*)nullptr);
 }
-template <int V> struct Int { static constexpr int value = V; };
 template <class F> inline void with_bool(bool b, F f) { if (b) f(Int<1>{}); else f(Int<0>{}); }
 template <class T> using Pointee = typename std::remove_pointer<T>::type;
 
@@ -404,18 +403,29 @@ int tuna_moe_few(const void* x, int64_t ldx, int64_t n_tokens, int64_t hidden, c
     F.hi = (unsigned short*)at; at += pairs * F.ld_h * 2;
     F.lo = (unsigned short*)at;
     const bool wide = rows_wide(x, 2, ldx) && on(w1, 16) && on(w2, 16) && (hidden * wsz) % 16 == 0 && (inner * wsz) % 16 == 0;
-    const dim3 g1((unsigned)ceil_div(inner, 16), (unsigned)n_experts), g2((unsigned)ceil_div(hidden, 16));
+    // one token: its k experts' rows alone; else all experts', most of which may have nothing to do.  Few pairs: the waves of a workgroup share
+    // 16 columns, so that there are workgroups enough for the device; many: each wave has 16, and fewer workgroups look for their tokens
+    const bool one = n_tokens == 1, split = one || (int64_t)pairs * ceil_div(inner, 64) < 1024;
+    const dim3 g1((unsigned)ceil_div(inner, split ? 16 : 16 * kFewFirst), (unsigned)(one ? k : n_experts)), g2((unsigned)ceil_div(hidden, 16));
+    const size_t sums = (size_t)kFewSecond * n_tokens * 16 * 4;
     with_bool(wide, [&](auto wd) {
         auto both = [&](auto* wp, auto kind) {
             using W = Pointee<decltype(wp)>;
             with_type(logits_type, [&](auto* l) {
                 using L = Pointee<decltype(l)>;
-                LAUNCH((k_few_first<L, W, kind.value, wd.value != 0>), g1, 256, F);
+                if (one) LAUNCH((k_few_first<L, W, kind.value, wd.value != 0, 1, true, true>), g1, 256, F);
+                else if (split) LAUNCH((k_few_first<L, W, kind.value, wd.value != 0, 1, true, false>), g1, 256, F);
+                else if (n_tokens <= 16) LAUNCH((k_few_first<L, W, kind.value, wd.value != 0, 1, false, false>), g1, 256, F);
+                else LAUNCH((k_few_first<L, W, kind.value, wd.value != 0, 2, false, false>), g1, 256, F);
             });
-            with_type(out_type, [&](auto* o) {
-                using O = Pointee<decltype(o)>;
-                LAUNCH((k_few_second<W, kind.value, wd.value != 0, O>), g2, 256, F);
-            });
+            auto second = [&](auto mt) {
+                with_type(out_type, [&](auto* o) {
+                    using O = Pointee<decltype(o)>;
+                    hipLaunchKernelGGL((k_few_second<W, kind.value, wd.value != 0, mt.value, O>), g2, dim3(kFewSecond * 64), sums, (hipStream_t)stream, F);
+                });
+            };
+            if (n_tokens <= 16) second(Int<1>{});
+            else second(Int<4>{});
         };
         if (weight_type == TUNA_BF16) both((unsigned short*)nullptr, Int<-1>{});
         else if (scale_type == TUNA_SCALE_E8) both((uint8_t*)nullptr, Int<TUNA_SCALE_E8>{});

@@ -15,6 +15,7 @@ typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 typedef __bf16 v2b __attribute__((ext_vector_type(2)));
 
 constexpr int kBlock = 128;            // values that share a scale
+template <int V> struct Int { static constexpr int value = V; };
 constexpr int kLanes = 64;
 
 __device__ __forceinline__ int64_t blocks_of(int64_t n) { return (n + kBlock - 1) / kBlock; }
@@ -78,6 +79,16 @@ template <bool WIDE> __device__ __forceinline__ void store8(unsigned short* p, i
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) if (i < left) p[i] = to_bf16(v[i]);
+}
+
+// Eight 16-bit values of which `left` exist, as they lie; zeros behind them.
+template <bool WIDE> __device__ __forceinline__ v4u bits8(const unsigned short* p, int64_t left) {
+    v4u a = {0u, 0u, 0u, 0u};
+    if (WIDE && left >= 8) return *(const v4u*)p;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < left) a[i >> 1] |= (unsigned)p[i] << (16 * (i & 1));
+    return a;
 }
 
 // Sixteen 8-bit values of which `left` exist; zeros behind them.  WIDE: on 16 bytes, and rows of whole sixteens.
@@ -933,26 +944,38 @@ struct Few {
     int32_t* chosen; float* share; unsigned short* hi; unsigned short* lo; int64_t ld_h;
 };
 
-constexpr int kFewWaves = 4;
-
-// Eight neighbours of a row of weights as bf16, which holds every e4m3 exactly.
-template <bool WIDE> __device__ __forceinline__ v8b weights8(const unsigned short* p, int64_t left) {
-    v4u a = {0u, 0u, 0u, 0u};
-    if (WIDE && left >= 8) a = *(const v4u*)p;
-    else
+// The parts of 128 neighbours of a row that one of four lanes holds, as they lie in memory, and eight of them at a time as bf16, which holds
+// every e4m3 exactly.  at(h, part): where the eight number h of lane `part` start.  Every load takes 64 bytes of a row in a piece.  FULL: all of
+// it is inside the row, so that the loads hang on no condition and are under way together.
+template <class W> struct Part;
+template <> struct Part<uint8_t> {
+    v4u v[2];
+    static __device__ __forceinline__ int at(int h, int part) { return (h >> 1) * 64 + part * 16 + (h & 1) * 8; }
+    template <bool WIDE, bool FULL> __device__ __forceinline__ void load(const uint8_t* p, int part, int64_t left) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < left) a[i >> 1] |= (unsigned)p[i] << (16 * (i & 1));
+        for (int i = 0; i < 2; ++i)
+            v[i] = FULL ? *(const v4u*)(p + i * 64 + part * 16) : chunk16<WIDE>(p + i * 64 + part * 16, left - (i * 64 + part * 16));
+    }
+    __device__ __forceinline__ v8b eight(int h) const { return widen8(v[h >> 1][(h & 1) * 2], v[h >> 1][(h & 1) * 2 + 1]); }
+};
+template <> struct Part<unsigned short> {
+    v4u v[4];
+    static __device__ __forceinline__ int at(int h, int part) { return h * 32 + part * 8; }
+    template <bool WIDE, bool FULL> __device__ __forceinline__ void load(const unsigned short* p, int part, int64_t left) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = FULL ? *(const v4u*)(p + at(i, part)) : bits8<WIDE>(p + at(i, part), left - at(i, part));
+    }
+    __device__ __forceinline__ v8b eight(int h) const {
+        v8b r;
+        __builtin_memcpy(&r, &v[h], 16);
+        return r;
+    }
+};
+template <bool WIDE, bool FULL> __device__ __forceinline__ v8b row8(const unsigned short* p, int64_t left) {
+    const v4u a = FULL ? *(const v4u*)p : bits8<WIDE>(p, left);
     v8b r;
     __builtin_memcpy(&r, &a, 16);
     return r;
-}
-template <bool WIDE> __device__ __forceinline__ v8b weights8(const uint8_t* p, int64_t left) {
-    v2u a = {0u, 0u};
-    if (WIDE && left >= 8) a = *(const v2u*)p;
-    else
-#pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < left) a[i >> 2] |= (unsigned)p[i] << (8 * (i & 3));
-    return widen8(a[0], a[1]);
 }
 
 template <int KIND> __device__ __forceinline__ float scale_value(const void* s, int64_t i) {
@@ -960,190 +983,362 @@ template <int KIND> __device__ __forceinline__ float scale_value(const void* s, 
     return scale_float<KIND>(scale_at<KIND>(s, i));
 }
 
-// First kernel: workgroup (16 columns of the gate and of the up half, expert).  The workgroup finds the tokens that chose its expert: an
-// expert is among the k first of a token when fewer than k eligible logits come before its own, which is a count and no sort.
-template <class L, class W, int KIND, bool WIDE>
-__global__ __launch_bounds__(256) void k_few_first(Few F) {
+constexpr int kFewFirst = 4;           // waves of a workgroup of the first kernel: they share the length of the sums
+constexpr int kFewSecond = 16;         // and of the second: they share the experts
+constexpr int kFewStep = 2;            // blocks of 128 that a wave has in registers, while the next ones are on their way
+
+// First kernel: a workgroup makes 16 activations, or 64, of one expert (as many rows of the gate half and of the up half) for all tokens that
+// chose it, 16 MT of them at a time.  ONE: there is one token, and blockIdx.y counts its chosen experts; else blockIdx.y is the expert, and its tokens
+// are found without a sort: it is among the k first of a token when fewer than k eligible logits come before its own.
+template <class L, class W, int KIND, bool WIDE, int MT, bool SPLIT, bool ONE>
+__global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
     __shared__ int rank_of[TUNA_MOE_FEW_TOKENS];                  // how many come before this expert, or -1: not chosen
     __shared__ float share_of[TUNA_MOE_FEW_TOKENS];
     __shared__ int list[TUNA_MOE_FEW_TOKENS];
-    __shared__ float sums[kFewWaves][2][4][256];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, e = blockIdx.y;
+    __shared__ float sums[SPLIT ? kFewFirst : 1][2][256];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const bool first = blockIdx.x == 0;
-    for (int t = w; t < F.tokens; t += kFewWaves) {
-        const L* row = (const L*)F.logits + t * F.ld_logits;
-        const float own = load1(row + e);
-        const unsigned key = logit_key(own);
-        int before = 0, eligible = 0;
-        for (int i0 = 0; i0 < F.experts; i0 += 64) {
-            const int i = i0 + lane;
-            const unsigned o = i < F.experts ? logit_key(load1(row + i)) : 0u;
-            before += __popcll(__ballot(o > key || (o == key && i < e)));
-            eligible += __popcll(__ballot(o != 0));
+    int e = blockIdx.y, n;
+    auto share_in = [&](const L* row, float own) {                // of the softmax over all eligible experts
+        float top = -__builtin_inff(), sum = 0.f;
+        for (int i = lane; i < F.experts; i += 64) { const float l = load1(row + i); if (logit_key(l)) top = fmaxf(top, l); }
+        for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        for (int i = lane; i < F.experts; i += 64) sum += exp_share(load1(row + i), top);
+        return exp_share(own, top) / wave_sum(sum);
+    };
+    if (ONE) {
+        const L* row = (const L*)F.logits;
+        constexpr int PER = TUNA_MOE_MAX_EXPERTS / 64;
+        unsigned key[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) key[i] = i * 64 + lane < F.experts ? logit_key(load1(row + i * 64 + lane)) : 0u;
+        e = -1;
+        for (int j = 0; j <= (int)blockIdx.y; ++j) {
+            unsigned m = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) m = key[i] > m ? key[i] : m;
+#pragma unroll
+            for (int d = 32; d; d >>= 1) { const unsigned o = __shfl_xor(m, d); m = o > m ? o : m; }
+            e = -1;
+            if (m == 0) break;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const unsigned long long b = __ballot(e < 0 && key[i] == m);
+                if (b) {
+                    const int l = __ffsll((long long)b) - 1;
+                    e = i * 64 + l;
+                    if (lane == l) key[i] = 0;
+                }
+            }
         }
-        const bool in = key != 0 && before < F.k;
-        float share = 0.f;
-        if (first && (in || e == 0)) {
-            float top = -__builtin_inff(), sum = 0.f;
-            for (int i = lane; i < F.experts; i += 64) { const float l = load1(row + i); if (logit_key(l)) top = fmaxf(top, l); }
-            for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-            for (int i = lane; i < F.experts; i += 64) sum += exp_share(load1(row + i), top);
-            sum = wave_sum(sum);
-            share = in ? exp_share(own, top) / sum : 0.f;
+        e = __builtin_amdgcn_readfirstlane(e);
+        n = e < 0 ? 0 : 1;
+        if (first && w == 0) {
+            const float s = n ? share_in(row, load1(row + e)) : 0.f;
+            if (lane == 0) { F.chosen[blockIdx.y] = e; F.share[blockIdx.y] = s; }
         }
-        if (lane == 0) { rank_of[t] = in ? before : -1; share_of[t] = share; }
-        // a token with fewer than k eligible experts: its last places are empty
-        if (first && e == 0 && lane < F.k && lane >= eligible) F.chosen[t * F.k + lane] = -1;
-    }
-    __syncthreads();
-    int n;
-    {
+        if (n == 0) return;
+        if (tid == 0) { list[0] = 0; rank_of[0] = blockIdx.y; }
+    } else {
+        constexpr int TOGETHER = 4;                               // tokens whose logits are under way together
+        for (int t0 = w * TOGETHER; t0 < F.tokens; t0 += kFewFirst * TOGETHER) {
+            float own[TOGETHER];
+            int before[TOGETHER] = {}, eligible[TOGETHER] = {};
+            const L* row[TOGETHER];
+#pragma unroll
+            for (int q = 0; q < TOGETHER; ++q) {
+                const int t = t0 + q < F.tokens ? t0 + q : F.tokens - 1;
+                row[q] = (const L*)F.logits + t * F.ld_logits;
+                own[q] = load1(row[q] + e);
+            }
+            for (int i0 = 0; i0 < F.experts; i0 += 64) {
+                const int i = i0 + lane, at = i < F.experts ? i : F.experts - 1;
+                float l[TOGETHER];
+#pragma unroll
+                for (int q = 0; q < TOGETHER; ++q) l[q] = load1(row[q] + at);
+#pragma unroll
+                for (int q = 0; q < TOGETHER; ++q) {
+                    const unsigned key = logit_key(own[q]), o = i < F.experts ? logit_key(l[q]) : 0u;
+                    before[q] += __popcll(__ballot(o > key || (o == key && i < e)));
+                    eligible[q] += __popcll(__ballot(o != 0));
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < TOGETHER; ++q) {
+                const int t = t0 + q;
+                if (t >= F.tokens) break;
+                const bool in = logit_key(own[q]) != 0 && before[q] < F.k;
+                float share = 0.f;
+                if (first && in) share = share_in(row[q], own[q]);
+                if (lane == 0) { rank_of[t] = in ? before[q] : -1; share_of[t] = share; }
+                // a token with fewer than k eligible experts: its last places are empty
+                if (first && e == 0 && lane < F.k && lane >= eligible[q]) F.chosen[t * F.k + lane] = -1;
+            }
+        }
+        __syncthreads();
         const bool in = lane < F.tokens && rank_of[lane] >= 0;
         const unsigned long long b = __ballot(in);
         n = __popcll(b);
-        if (w == 0 && in) list[__popcll(b & ((1ull << lane) - 1))] = lane;
-        if (first && w == 0 && in) { F.chosen[lane * F.k + rank_of[lane]] = e; F.share[lane * F.k + rank_of[lane]] = share_of[lane]; }
+        if (w == 0 && in) {
+            list[__popcll(b & ((1ull << lane) - 1))] = lane;
+            if (first) { F.chosen[lane * F.k + rank_of[lane]] = e; F.share[lane * F.k + rank_of[lane]] = share_of[lane]; }
+        }
+        if (n == 0) return;
     }
-    if (n == 0) return;
     __syncthreads();
-    const int64_t f0 = (int64_t)blockIdx.x * 16;
+    // SPLIT: the waves share the length of one 16 columns' sums; else each wave has 16 columns of its own
+    const int64_t f0 = SPLIT ? (int64_t)blockIdx.x * 16 : ((int64_t)blockIdx.x * kFewFirst + w) * 16;
     const int c = lane & 15, part = lane >> 4;
     const int64_t col = f0 + c < F.inner ? f0 + c : F.inner - 1;
-    const W* wg = (const W*)F.w1 + ((int64_t)e * 2 * F.inner + col) * F.hidden;
+    const W* wg = (const W*)F.w1 + (int64_t)e * 2 * F.inner * F.hidden;
     const W* wu = wg + F.inner * F.hidden;
-    const int64_t nb = blocks_of(F.hidden), sg = ((int64_t)e * blocks_of(2 * F.inner) + col / kBlock) * nb,
+    const int64_t at_w = col * F.hidden, nb = blocks_of(F.hidden), sg = ((int64_t)e * blocks_of(2 * F.inner) + col / kBlock) * nb,
                   su = ((int64_t)e * blocks_of(2 * F.inner) + (F.inner + col) / kBlock) * nb;
-    for (int t0 = 0; t0 < n; t0 += 64) {                           // (at most 64 tokens: once)
-        const int mt = (n - t0 + 15) / 16;
-        v4f gate[4] = {}, up[4] = {};
-        const unsigned short* rows[4];
+    // whole steps in a pipeline; blocks behind them (all, for rows that do not start on 16 bytes) one at a time
+    const int64_t steps = WIDE ? F.hidden / (kBlock * kFewStep) : 0;
+    for (int t0 = 0; t0 < n; t0 += MT * 16) {                     // more than 16 MT tokens of one expert read its weights again
+        v4f gate[MT], up[MT];
+        unsigned at_x[MT];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
+        for (int s = 0; s < MT; ++s) {
+            gate[s] = up[s] = v4f{0.f, 0.f, 0.f, 0.f};
+            // places without a token repeat the last one: a row of the sums depends on its own token alone
             const int i = t0 + s * 16 + c;
-            rows[s] = i < n ? F.x + list[i] * F.ldx : nullptr;
+            at_x[s] = (unsigned)list[i < n ? i : n - 1];
         }
-        for (int64_t b = w; b < nb; b += kFewWaves) {
-            v4f g[4] = {}, u[4] = {};
+        // one block: `full` as the parts were loaded
+        auto multiply = [&](const Part<W>& pg, const Part<W>& pu, float kg, float ku, int64_t at, auto full) {
+            v4f g[MT], u[MT];
+            v8b a[MT][4];
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                const int64_t at = b * kBlock + part * 32 + h * 8;
-                const v8b bg = weights8<WIDE>(wg + at, F.hidden - at), bu = weights8<WIDE>(wu + at, F.hidden - at);
+            for (int s = 0; s < MT; ++s) {
+                g[s] = u[s] = v4f{0.f, 0.f, 0.f, 0.f};
+                const unsigned short* row = F.x + at_x[s] * F.ldx + at;
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    if (s >= mt) break;
-                    v8b a = {};
-                    if (rows[s]) a = weights8<WIDE>(rows[s] + at, F.hidden - at);
-                    g[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, bg, g[s], 0, 0, 0);
-                    u[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, bu, u[s], 0, 0, 0);
+                for (int h = 0; h < 4; ++h) {
+                    const int k = Part<W>::at(h, part);
+                    a[s][h] = row8<WIDE, full.value != 0>(row + k, F.hidden - at - k);
                 }
             }
-            const float kg = scale_value<KIND>(F.s1, sg + b), ku = scale_value<KIND>(F.s1, su + b);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) { gate[s] += g[s] * kg; up[s] += u[s] * ku; }
-        }
-        __syncthreads();
+            for (int h = 0; h < 4; ++h) {
+                const v8b bg = pg.eight(h), bu = pu.eight(h);
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sums[w][0][s][(part * 4 + i) * 16 + c] = gate[s][i];
-                sums[w][1][s][(part * 4 + i) * 16 + c] = up[s][i];
+                for (int s = 0; s < MT; ++s) {
+                    g[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s][h], bg, g[s], 0, 0, 0);
+                    u[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s][h], bu, u[s], 0, 0, 0);
+                }
             }
-        __syncthreads();
-        for (int s = 0; s < mt; ++s) {
-            float a = 0.f, b = 0.f;
-            for (int q = 0; q < kFewWaves; ++q) { a += sums[q][0][s][tid]; b += sums[q][1][s][tid]; }
-            const int i = t0 + s * 16 + (tid >> 4);
-            const int64_t f = f0 + (tid & 15);
-            if (i < n && f < F.inner) {
-                const int t = list[i];
-                const float v = a * silu_gate(a) * b;
-                const unsigned short hi = to_bf16(v);
-                const int64_t to = (int64_t)(t * F.k + rank_of[t]) * F.ld_h + f;
-                F.hi[to] = hi;
-                F.lo[to] = fabsf(v) < __builtin_inff() ? to_bf16(v - bf16_bits(hi)) : (unsigned short)0;
+#pragma unroll
+            for (int s = 0; s < MT; ++s) { gate[s] += g[s] * kg; up[s] += u[s] * ku; }
+        };
+        struct Step { Part<W> g[kFewStep], u[kFewStep]; float kg[kFewStep], ku[kFewStep]; };
+        auto fetch = [&](Step& st, int64_t step) {
+#pragma unroll
+            for (int i = 0; i < kFewStep; ++i) {
+                const int64_t b = step * kFewStep + i;
+                st.g[i].template load<WIDE, true>(wg + b * kBlock + at_w, part, 0);
+                st.u[i].template load<WIDE, true>(wu + b * kBlock + at_w, part, 0);
+                st.kg[i] = scale_value<KIND>(F.s1, sg + b);
+                st.ku[i] = scale_value<KIND>(F.s1, su + b);
+            }
+        };
+        auto use = [&](const Step& st, int64_t step) {
+#pragma unroll
+            for (int i = 0; i < kFewStep; ++i) multiply(st.g[i], st.u[i], st.kg[i], st.ku[i], (step * kFewStep + i) * kBlock, Int<1>{});
+        };
+        constexpr int stride = SPLIT ? kFewFirst : 1;
+        if constexpr (WIDE) {
+            Step st[2];
+            int64_t b = SPLIT ? w : 0;
+            if (b < steps) fetch(st[0], b);
+            for (; b < steps; b += 2 * stride) {
+                if (b + stride < steps) fetch(st[1], b + stride);
+                use(st[0], b);
+                if (b + stride >= steps) break;
+                if (b + 2 * stride < steps) fetch(st[0], b + 2 * stride);
+                use(st[1], b + stride);
+            }
+        }
+        for (int64_t b = steps * kFewStep + (SPLIT ? w : 0); b < nb; b += stride) {
+            Part<W> g, u;
+            const int64_t at = b * kBlock;
+            g.template load<WIDE, false>(wg + at + at_w, part, F.hidden - at);
+            u.template load<WIDE, false>(wu + at + at_w, part, F.hidden - at);
+            multiply(g, u, scale_value<KIND>(F.s1, sg + b), scale_value<KIND>(F.s1, su + b), at, Int<0>{});
+        }
+        auto keep = [&](int i, int64_t f, float x, float y) {     // activation f of token number i of the list
+            if (i >= n || f >= F.inner) return;
+            const int t = list[i];
+            const float v = x * silu_gate(x) * y;
+            const unsigned short hi = to_bf16(v);
+            const int64_t to = (int64_t)(t * F.k + rank_of[t]) * F.ld_h + f;
+            F.hi[to] = hi;
+            F.lo[to] = fabsf(v) < __builtin_inff() ? to_bf16(v - bf16_bits(hi)) : (unsigned short)0;
+        };
+#pragma unroll
+        for (int s = 0; s < MT; ++s) {
+            if (t0 + s * 16 >= n) break;
+            if (SPLIT) {
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sums[w][0][(part * 4 + i) * 16 + c] = gate[s][i];
+                    sums[w][1][(part * 4 + i) * 16 + c] = up[s][i];
+                }
+                __syncthreads();
+                float x = 0.f, y = 0.f;
+                for (int q = 0; q < kFewFirst; ++q) { x += sums[q][0][tid]; y += sums[q][1][tid]; }
+                keep(t0 + s * 16 + (tid >> 4), f0 + (tid & 15), x, y);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) keep(t0 + s * 16 + part * 4 + i, f0 + c, gate[s][i], up[s][i]);
             }
         }
     }
 }
 
-// Second kernel: a workgroup per 16 columns of the result, for all tokens and experts; the waves take the chosen experts in turn and
-// every wave's sums are added up in the waves' order.
-template <class W, int KIND, bool WIDE, class OUT>
-__global__ __launch_bounds__(256) void k_few_second(Few F) {
-    __shared__ int pairs[TUNA_MOE_FEW_TOKENS * TUNA_MOE_MAX_K];
+// Second kernel: a workgroup per 16 columns of the result, for all tokens and chosen experts.  The chosen experts' blocks, two at a time, are one
+// sequence, of which every wave has a run; a wave's sums are its own, and at the end they are added up in the waves' order.
+template <class W, int KIND, bool WIDE, int MT, class OUT>
+__global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
+    extern __shared__ float shared[];                             // [kFewSecond][tokens][16] sums
+    __shared__ int pair_of[TUNA_MOE_FEW_TOKENS * TUNA_MOE_MAX_K]; // pairs by expert
     __shared__ float weight[TUNA_MOE_FEW_TOKENS * TUNA_MOE_MAX_K];
-    __shared__ unsigned active[TUNA_MOE_MAX_EXPERTS / 32];
-    __shared__ float sums[kFewWaves][TUNA_MOE_FEW_TOKENS][16];
-    __shared__ int mine[kFewWaves][TUNA_MOE_FEW_TOKENS];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    __shared__ int first_of[TUNA_MOE_MAX_EXPERTS];                // of the chosen experts: where their pairs start, and how many
+    __shared__ int count_of[TUNA_MOE_MAX_EXPERTS];
+    __shared__ int expert_of[TUNA_MOE_FEW_TOKENS * TUNA_MOE_MAX_K];
+    __shared__ int n_active;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int np = F.tokens * F.k;
-    for (int i = tid; i < TUNA_MOE_MAX_EXPERTS / 32; i += 256) active[i] = 0;
-    for (int i = tid; i < kFewWaves * TUNA_MOE_FEW_TOKENS * 16; i += 256) (&sums[0][0][0])[i] = 0.f;
+    float* sums = shared + w * F.tokens * 16;
+    for (int i = lane; i < F.tokens * 16; i += 64) sums[i] = 0.f;
+    for (int i = tid; i < F.experts; i += kFewSecond * 64) count_of[i] = 0;
     __syncthreads();
-    for (int i = tid; i < np; i += 256) {
-        const int e = F.chosen[i];
-        pairs[i] = e;
-        if (e >= 0) atomicOr(&active[e >> 5], 1u << (e & 31));
-        float s = e < 0 ? 0.f : F.share[i];
-        if (F.renorm && e >= 0) {
+    const int mine = tid < np ? F.chosen[tid] : -1;               // np <= 1024: a pair a thread
+    if (mine >= 0) atomicAdd(&count_of[mine], 1);
+    if (tid < np) {
+        float s = mine < 0 ? 0.f : F.share[tid];
+        if (F.renorm && mine >= 0) {
+            const int t0 = tid / F.k * F.k;
             float total = 0.f;
-            for (int j = i / F.k * F.k; j < i / F.k * F.k + F.k; ++j) if (F.chosen[j] >= 0) total += F.share[j];
+            for (int j = t0; j < t0 + F.k; ++j) if (F.chosen[j] >= 0) total += F.share[j];
             s /= total;
         }
-        weight[i] = s;
+        weight[tid] = s;
     }
+    __syncthreads();
+    if (w == 0) {                                                 // the chosen experts in order, and where their pairs start
+        int active = 0, pairs = 0;
+        for (int e0 = 0; e0 < F.experts; e0 += 64) {
+            const int cnt = e0 + lane < F.experts ? count_of[e0 + lane] : 0;
+            const unsigned long long b = __ballot(cnt > 0);
+            const int inc = wave_scan(cnt, lane);
+            if (cnt > 0) {
+                expert_of[active + __popcll(b & ((1ull << lane) - 1))] = e0 + lane;
+                first_of[e0 + lane] = pairs + inc - cnt;
+            }
+            active += __popcll(b);
+            pairs += __shfl(inc, 63);
+        }
+        if (lane == 0) n_active = active;
+    }
+    __syncthreads();
+    for (int i = tid; i < F.experts; i += kFewSecond * 64) count_of[i] = 0;
+    __syncthreads();
+    // the order of an expert's pairs changes no sum: each has its own row
+    if (mine >= 0) pair_of[first_of[mine] + atomicAdd(&count_of[mine], 1)] = tid;
     __syncthreads();
     const int64_t c0 = (int64_t)blockIdx.x * 16;
     const int c = lane & 15, part = lane >> 4;
     const int64_t col = c0 + c < F.hidden ? c0 + c : F.hidden - 1;
-    const int64_t nb = blocks_of(F.inner);
-    int turn = 0;
-    for (int wd = 0; wd < (F.experts + 31) / 32; ++wd) {
-        for (unsigned bits = active[wd]; bits; bits &= bits - 1, ++turn) {
-            if (turn % kFewWaves != w) continue;
-            const int e = wd * 32 + __builtin_ctz(bits);
-            int n = 0;
-            for (int p0 = 0; p0 < np; p0 += 64) {                  // this expert's pairs, in order of the token
-                const bool in = p0 + lane < np && pairs[p0 + lane] == e;
-                const unsigned long long b = __ballot(in);
-                if (in) mine[w][n + __popcll(b & ((1ull << lane) - 1))] = p0 + lane;
-                n += __popcll(b);
-            }
-            wave_lds_done();
-            const W* row = (const W*)F.w2 + ((int64_t)e * F.hidden + col) * F.inner;
-            const int64_t s2 = ((int64_t)e * blocks_of(F.hidden) + col / kBlock) * nb;
-            for (int t0 = 0; t0 < n; t0 += 16) {
-                const int64_t p = t0 + c < n ? mine[w][t0 + c] : -1;
-                v4f acc = {};
-                for (int64_t b = 0; b < nb; ++b) {
-                    v4f y = {};
+    const int64_t nb = blocks_of(F.inner), nbh = blocks_of(F.hidden);
+    // whole steps of all chosen experts in a pipeline; the blocks behind them (all, for rows that do not start on 16 bytes) one at a time
+    const int per = WIDE ? (int)(F.inner / (kBlock * kFewStep)) : 0;
+    const int64_t total = (int64_t)n_active * per;
+    const int lo = (int)(total * w / kFewSecond), hi = (int)(total * (w + 1) / kFewSecond);
+    v4f acc[MT];
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        const int64_t at = b * kBlock + part * 32 + h * 8;
-                        const v8b bw = weights8<WIDE>(row + at, F.inner - at);
-                        v8b hi = {}, lo = {};
-                        if (p >= 0) {
-                            hi = weights8<true>(F.hi + p * F.ld_h + at, F.inner - at);
-                            lo = weights8<true>(F.lo + p * F.ld_h + at, F.inner - at);
-                        }
-                        y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, bw, y, 0, 0, 0);
-                        y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, bw, y, 0, 0, 0);
-                    }
-                    acc += y * scale_value<KIND>(F.s2, s2 + b);
-                }
+    for (int s = 0; s < MT; ++s) acc[s] = v4f{0.f, 0.f, 0.f, 0.f};
+    // one block of the expert whose `n` pairs start at p0; `ends`: its sums go to the tokens'
+    auto multiply = [&](const Part<W>& v, float scale, int64_t at, int p0, int n, bool ends, auto full) {
+#pragma unroll
+        for (int s = 0; s < MT; ++s) {
+            if (s * 16 >= n) break;
+            // places without a pair repeat the last one
+            const int64_t at_h = pair_of[p0 + (s * 16 + c < n ? s * 16 + c : n - 1)] * F.ld_h + at;
+            v8b x[4], z[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const int k = Part<W>::at(h, part);
+                x[h] = row8<true, full.value != 0>(F.hi + at_h + k, F.inner - at - k);
+                z[h] = row8<true, full.value != 0>(F.lo + at_h + k, F.inner - at - k);
+            }
+            v4f y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const v8b bw = v.eight(h);
+                y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[h], bw, y, 0, 0, 0);
+                y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(z[h], bw, y, 0, 0, 0);
+            }
+            acc[s] += y * scale;
+            if (ends) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int at = t0 + part * 4 + i;
-                    if (at < n) sums[w][mine[w][at] / F.k][c] += weight[mine[w][at]] * acc[i];
+                    const int r = s * 16 + part * 4 + i;
+                    if (r < n) {
+                        const int p = pair_of[p0 + r];
+                        sums[p / F.k * 16 + c] += weight[p] * acc[s][i];
+                    }
                 }
+                acc[s] = v4f{0.f, 0.f, 0.f, 0.f};
             }
+        }
+        if (ends) wave_lds_done();
+    };
+    if constexpr (WIDE) {
+        struct Step { Part<W> v[kFewStep]; float k[kFewStep]; int e; };
+        const int64_t at_w = col * F.inner, at_s = col / kBlock * nb;
+        auto fetch = [&](Step& st, int unit) {
+            const int a = unit / per, step = unit - a * per;
+            st.e = __builtin_amdgcn_readfirstlane(expert_of[a]);
+            const W* base = (const W*)F.w2 + (int64_t)st.e * F.hidden * F.inner + step * (kFewStep * kBlock);
+            const int64_t s2 = (int64_t)st.e * nbh * nb + step * kFewStep + at_s;
+#pragma unroll
+            for (int i = 0; i < kFewStep; ++i) {
+                st.v[i].template load<WIDE, true>(base + i * kBlock + at_w, part, 0);
+                st.k[i] = scale_value<KIND>(F.s2, s2 + i);
+            }
+        };
+        auto use = [&](const Step& st, int unit) {
+            const int step = unit % per, p0 = __builtin_amdgcn_readfirstlane(first_of[st.e]), n = __builtin_amdgcn_readfirstlane(count_of[st.e]);
+#pragma unroll
+            for (int i = 0; i < kFewStep; ++i)
+                multiply(st.v[i], st.k[i], (int64_t)(step * kFewStep + i) * kBlock, p0, n, i + 1 == kFewStep && (unit + 1 == hi || step + 1 == per), Int<1>{});
+        };
+        Step st[2];
+        if (lo < hi) fetch(st[0], lo);
+        for (int u = lo; u < hi; u += 2) {
+            if (u + 1 < hi) fetch(st[1], u + 1);
+            use(st[0], u);
+            if (u + 1 >= hi) break;
+            if (u + 2 < hi) fetch(st[0], u + 2);
+            use(st[1], u + 1);
+        }
+    }
+    for (int a = w; a < n_active; a += kFewSecond) {
+        const int e = __builtin_amdgcn_readfirstlane(expert_of[a]);
+        const int p0 = __builtin_amdgcn_readfirstlane(first_of[e]), n = __builtin_amdgcn_readfirstlane(count_of[e]);
+        for (int64_t b = (int64_t)per * kFewStep; b < nb; ++b) {
+            Part<W> v;
+            v.template load<WIDE, false>((const W*)F.w2 + ((int64_t)e * F.hidden + col) * F.inner + b * kBlock, part, F.inner - b * kBlock);
+            multiply(v, scale_value<KIND>(F.s2, ((int64_t)e * nbh + col / kBlock) * nb + b), b * kBlock, p0, n, b + 1 == nb, Int<0>{});
         }
     }
     __syncthreads();
-    for (int i = tid; i < F.tokens * 16; i += 256) {
+    for (int i = tid; i < F.tokens * 16; i += kFewSecond * 64) {
         float s = 0.f;
-        for (int q = 0; q < kFewWaves; ++q) s += sums[q][i >> 4][i & 15];
+        for (int q = 0; q < kFewSecond; ++q) s += shared[q * F.tokens * 16 + i];
         if (c0 + (i & 15) < F.hidden) store1((OUT*)F.out + (i >> 4) * F.ld_out + c0 + (i & 15), s);
     }
 }
