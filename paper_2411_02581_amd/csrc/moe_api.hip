@@ -386,7 +386,7 @@ int tuna_moe_few(const void* x, int64_t ldx, int64_t n_tokens, int64_t hidden, c
     if (!w1 || !w2 || !on(w1, wsz) || !on(w2, wsz)) return TUNA_ERR_ARG;
     if (weight_type == TUNA_F8 && (!is_scale(scale_type) || !s1 || !s2 || !on(s1, scale_size(scale_type)) || !on(s2, scale_size(scale_type)))) return TUNA_ERR_ARG;
     if (weight_type != TUNA_F8 && (s1 || s2)) return TUNA_ERR_ARG;
-    if (ceil_div(inner, 16) > kMaxRows / 256 || ceil_div(hidden, 16) > kMaxRows / 256) return TUNA_ERR_TOO_LARGE;
+    if (ldx > kMaxRows / 64 || ceil_div(inner, 16) > kMaxRows / 256 || ceil_div(hidden, 16) > kMaxRows / 256) return TUNA_ERR_TOO_LARGE;
     if (!workspace || !on(workspace, 16)) return TUNA_ERR_ARG;
     if (workspace_bytes < need) return TUNA_ERR_WORKSPACE_TOO_SMALL;
     const int rc = tuna_host::ensure_device();
@@ -415,17 +415,13 @@ int tuna_moe_few(const void* x, int64_t ldx, int64_t n_tokens, int64_t hidden, c
                 using L = Pointee<decltype(l)>;
                 if (one) LAUNCH((k_few_first<L, W, kind.value, wd.value != 0, 1, true, true>), g1, 256, F);
                 else if (split) LAUNCH((k_few_first<L, W, kind.value, wd.value != 0, 1, true, false>), g1, 256, F);
-                else if (n_tokens <= 16) LAUNCH((k_few_first<L, W, kind.value, wd.value != 0, 1, false, false>), g1, 256, F);
+                else if (pairs <= (size_t)n_experts * 8) LAUNCH((k_few_first<L, W, kind.value, wd.value != 0, 1, false, false>), g1, 256, F);
                 else LAUNCH((k_few_first<L, W, kind.value, wd.value != 0, 2, false, false>), g1, 256, F);
             });
-            auto second = [&](auto mt) {
-                with_type(out_type, [&](auto* o) {
-                    using O = Pointee<decltype(o)>;
-                    hipLaunchKernelGGL((k_few_second<W, kind.value, wd.value != 0, mt.value, O>), g2, dim3(kFewSecond * 64), sums, (hipStream_t)stream, F);
-                });
-            };
-            if (n_tokens <= 16) second(Int<1>{});
-            else second(Int<4>{});
+            with_type(out_type, [&](auto* o) {
+                using O = Pointee<decltype(o)>;
+                hipLaunchKernelGGL((k_few_second<W, kind.value, wd.value != 0, O>), g2, dim3(kFewSecond * 64), sums, (hipStream_t)stream, F);
+            });
         };
         if (weight_type == TUNA_BF16) both((unsigned short*)nullptr, Int<-1>{});
         else if (scale_type == TUNA_SCALE_E8) both((uint8_t*)nullptr, Int<TUNA_SCALE_E8>{});

@@ -984,7 +984,7 @@ template <int KIND> __device__ __forceinline__ float scale_value(const void* s, 
 }
 
 constexpr int kFewFirst = 4;           // waves of a workgroup of the first kernel: they share the length of the sums
-constexpr int kFewSecond = 16;         // and of the second: they share the experts
+constexpr int kFewSecond = 8;         // and of the second: they share the experts
 constexpr int kFewStep = 2;            // blocks of 128 that a wave has in registers, while the next ones are on their way
 
 // First kernel: a workgroup makes 16 activations, or 64, of one expert (as many rows of the gate half and of the up half) for all tokens that
@@ -1102,24 +1102,29 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
 #pragma unroll
         for (int s = 0; s < MT; ++s) {
             gate[s] = up[s] = v4f{0.f, 0.f, 0.f, 0.f};
-            // places without a token repeat the last one: a row of the sums depends on its own token alone
             const int i = t0 + s * 16 + c;
-            at_x[s] = (unsigned)list[i < n ? i : n - 1];
+            at_x[s] = i < n ? (unsigned)(list[i] * F.ldx) + Part<W>::at(0, part) : ~0u;
         }
-        // one block: `full` as the parts were loaded
-        auto multiply = [&](const Part<W>& pg, const Part<W>& pu, float kg, float ku, int64_t at, auto full) {
-            v4f g[MT], u[MT];
-            v8b a[MT][4];
+        // the tokens' parts of one block
+        auto load_x = [&](v8b (&a)[MT][4], int64_t at, auto full) {
 #pragma unroll
             for (int s = 0; s < MT; ++s) {
-                g[s] = u[s] = v4f{0.f, 0.f, 0.f, 0.f};
-                const unsigned short* row = F.x + at_x[s] * F.ldx + at;
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    const int k = Part<W>::at(h, part);
-                    a[s][h] = row8<WIDE, full.value != 0>(row + k, F.hidden - at - k);
+                for (int h = 0; h < 4; ++h) a[s][h] = v8b{};
+                if (at_x[s] != ~0u) {                             // places without a token are zeros, and cost no loads
+                    const unsigned short* row = F.x + at;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        const int k = Part<W>::at(h, 0);
+                        a[s][h] = row8<WIDE, full.value != 0>(row + k + at_x[s], F.hidden - at - k - Part<W>::at(0, part));
+                    }
                 }
             }
+        };
+        auto multiply = [&](const v8b (&a)[MT][4], const Part<W>& pg, const Part<W>& pu, float kg, float ku) {
+            v4f g[MT], u[MT];
+#pragma unroll
+            for (int s = 0; s < MT; ++s) g[s] = u[s] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
                 const v8b bg = pg.eight(h), bu = pu.eight(h);
@@ -1143,21 +1148,26 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
                 st.ku[i] = scale_value<KIND>(F.s1, su + b);
             }
         };
-        auto use = [&](const Step& st, int64_t step) {
-#pragma unroll
-            for (int i = 0; i < kFewStep; ++i) multiply(st.g[i], st.u[i], st.kg[i], st.ku[i], (step * kFewStep + i) * kBlock, Int<1>{});
-        };
         constexpr int stride = SPLIT ? kFewFirst : 1;
+        // loads come back in the order they were made: a step's tokens are asked for ahead of the next step's weights, which stay under way
+        auto use = [&](const Step& st, int64_t step, Step& next) {
+            v8b a[kFewStep][MT][4];
+#pragma unroll
+            for (int i = 0; i < kFewStep; ++i) load_x(a[i], (step * kFewStep + i) * kBlock, Int<1>{});
+            __builtin_amdgcn_sched_barrier(0);
+            if (step + stride < steps) fetch(next, step + stride);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < kFewStep; ++i) multiply(a[i], st.g[i], st.u[i], st.kg[i], st.ku[i]);
+        };
         if constexpr (WIDE) {
             Step st[2];
             int64_t b = SPLIT ? w : 0;
             if (b < steps) fetch(st[0], b);
             for (; b < steps; b += 2 * stride) {
-                if (b + stride < steps) fetch(st[1], b + stride);
-                use(st[0], b);
+                use(st[0], b, st[1]);
                 if (b + stride >= steps) break;
-                if (b + 2 * stride < steps) fetch(st[0], b + 2 * stride);
-                use(st[1], b + stride);
+                use(st[1], b + stride, st[0]);
             }
         }
         for (int64_t b = steps * kFewStep + (SPLIT ? w : 0); b < nb; b += stride) {
@@ -1165,7 +1175,9 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
             const int64_t at = b * kBlock;
             g.template load<WIDE, false>(wg + at + at_w, part, F.hidden - at);
             u.template load<WIDE, false>(wu + at + at_w, part, F.hidden - at);
-            multiply(g, u, scale_value<KIND>(F.s1, sg + b), scale_value<KIND>(F.s1, su + b), at, Int<0>{});
+            v8b a[MT][4];
+            load_x(a, at, Int<0>{});
+            multiply(a, g, u, scale_value<KIND>(F.s1, sg + b), scale_value<KIND>(F.s1, su + b));
         }
         auto keep = [&](int i, int64_t f, float x, float y) {     // activation f of token number i of the list
             if (i >= n || f >= F.inner) return;
@@ -1198,141 +1210,156 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
     }
 }
 
-// Second kernel: a workgroup per 16 columns of the result, for all tokens and chosen experts.  The chosen experts' blocks, two at a time, are one
-// sequence, of which every wave has a run; a wave's sums are its own, and at the end they are added up in the waves' order.
-template <class W, int KIND, bool WIDE, int MT, class OUT>
+// Second kernel: a workgroup per 16 columns of the result, for all tokens and chosen experts.  A task is a chosen expert with up to 16 of its
+// pairs (more of them read its weights again); the tasks' steps are one sequence, of which every wave has a run; a wave's sums are its own,
+// and at the end they are added up in the waves' order.
+template <class W, int KIND, bool WIDE, class OUT>
 __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
     extern __shared__ float shared[];                             // [kFewSecond][tokens][16] sums
-    __shared__ int pair_of[TUNA_MOE_FEW_TOKENS * TUNA_MOE_MAX_K]; // pairs by expert
-    __shared__ float weight[TUNA_MOE_FEW_TOKENS * TUNA_MOE_MAX_K];
-    __shared__ int first_of[TUNA_MOE_MAX_EXPERTS];                // of the chosen experts: where their pairs start, and how many
-    __shared__ int count_of[TUNA_MOE_MAX_EXPERTS];
-    __shared__ int expert_of[TUNA_MOE_FEW_TOKENS * TUNA_MOE_MAX_K];
-    __shared__ int n_active;
+    constexpr int PAIRS = TUNA_MOE_FEW_TOKENS * TUNA_MOE_MAX_K;
+    __shared__ int pair_of[PAIRS];                                // pairs by expert
+    __shared__ float weight[PAIRS];
+    __shared__ int first_of[TUNA_MOE_MAX_EXPERTS], count_of[TUNA_MOE_MAX_EXPERTS];
+    __shared__ int task_expert[PAIRS], task_first[PAIRS], task_count[PAIRS];
+    __shared__ int n_tasks;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int np = F.tokens * F.k;
     float* sums = shared + w * F.tokens * 16;
     for (int i = lane; i < F.tokens * 16; i += 64) sums[i] = 0.f;
     for (int i = tid; i < F.experts; i += kFewSecond * 64) count_of[i] = 0;
     __syncthreads();
-    const int mine = tid < np ? F.chosen[tid] : -1;               // np <= 1024: a pair a thread
-    if (mine >= 0) atomicAdd(&count_of[mine], 1);
-    if (tid < np) {
-        float s = mine < 0 ? 0.f : F.share[tid];
-        if (F.renorm && mine >= 0) {
-            const int t0 = tid / F.k * F.k;
+    for (int i = tid; i < np; i += kFewSecond * 64) {
+        const int e = F.chosen[i];
+        if (e >= 0) atomicAdd(&count_of[e], 1);
+        float s = e < 0 ? 0.f : F.share[i];
+        if (F.renorm && e >= 0) {
+            const int t0 = i / F.k * F.k;
             float total = 0.f;
             for (int j = t0; j < t0 + F.k; ++j) if (F.chosen[j] >= 0) total += F.share[j];
             s /= total;
         }
-        weight[tid] = s;
+        weight[i] = s;
     }
     __syncthreads();
-    if (w == 0) {                                                 // the chosen experts in order, and where their pairs start
-        int active = 0, pairs = 0;
+    if (w == 0) {                                                 // the tasks in order of their experts
+        int tasks = 0, pairs = 0;
         for (int e0 = 0; e0 < F.experts; e0 += 64) {
             const int cnt = e0 + lane < F.experts ? count_of[e0 + lane] : 0;
-            const unsigned long long b = __ballot(cnt > 0);
-            const int inc = wave_scan(cnt, lane);
+            const int inc = wave_scan(cnt, lane), parts = (cnt + 15) / 16, inc_parts = wave_scan(parts, lane);
             if (cnt > 0) {
-                expert_of[active + __popcll(b & ((1ull << lane) - 1))] = e0 + lane;
                 first_of[e0 + lane] = pairs + inc - cnt;
+                count_of[e0 + lane] = 0;
+                for (int i = 0; i < parts; ++i) {
+                    const int at = tasks + inc_parts - parts + i;
+                    task_expert[at] = e0 + lane;
+                    task_first[at] = pairs + inc - cnt + i * 16;
+                    task_count[at] = cnt - i * 16 < 16 ? cnt - i * 16 : 16;
+                }
             }
-            active += __popcll(b);
+            tasks += __shfl(inc_parts, 63);
             pairs += __shfl(inc, 63);
         }
-        if (lane == 0) n_active = active;
+        if (lane == 0) n_tasks = tasks;
     }
     __syncthreads();
-    for (int i = tid; i < F.experts; i += kFewSecond * 64) count_of[i] = 0;
-    __syncthreads();
     // the order of an expert's pairs changes no sum: each has its own row
-    if (mine >= 0) pair_of[first_of[mine] + atomicAdd(&count_of[mine], 1)] = tid;
+    for (int i = tid; i < np; i += kFewSecond * 64) {
+        const int e = F.chosen[i];
+        if (e >= 0) pair_of[first_of[e] + atomicAdd(&count_of[e], 1)] = i;
+    }
     __syncthreads();
     const int64_t c0 = (int64_t)blockIdx.x * 16;
     const int c = lane & 15, part = lane >> 4;
     const int64_t col = c0 + c < F.hidden ? c0 + c : F.hidden - 1;
     const int64_t nb = blocks_of(F.inner), nbh = blocks_of(F.hidden);
-    // whole steps of all chosen experts in a pipeline; the blocks behind them (all, for rows that do not start on 16 bytes) one at a time
+    // whole steps of all tasks in a pipeline; the blocks behind them (all, for rows that do not start on 16 bytes) one at a time
     const int per = WIDE ? (int)(F.inner / (kBlock * kFewStep)) : 0;
-    const int64_t total = (int64_t)n_active * per;
+    const int64_t total = (int64_t)n_tasks * per;
     const int lo = (int)(total * w / kFewSecond), hi = (int)(total * (w + 1) / kFewSecond);
-    v4f acc[MT];
+    v4f acc = {0.f, 0.f, 0.f, 0.f};
+    // one block of a task's activations, in two parts
+    struct Act { v8b x[4], z[4]; };
+    auto load_h = [&](Act& a, int task, int64_t at, auto full) {
 #pragma unroll
-    for (int s = 0; s < MT; ++s) acc[s] = v4f{0.f, 0.f, 0.f, 0.f};
-    // one block of the expert whose `n` pairs start at p0; `ends`: its sums go to the tokens'
-    auto multiply = [&](const Part<W>& v, float scale, int64_t at, int p0, int n, bool ends, auto full) {
-#pragma unroll
-        for (int s = 0; s < MT; ++s) {
-            if (s * 16 >= n) break;
-            // places without a pair repeat the last one
-            const int64_t at_h = pair_of[p0 + (s * 16 + c < n ? s * 16 + c : n - 1)] * F.ld_h + at;
-            v8b x[4], z[4];
+        for (int h = 0; h < 4; ++h) a.x[h] = a.z[h] = v8b{};
+        if (c < task_count[task]) {                               // places without a pair are zeros, and cost no loads
+            const int64_t at_h = pair_of[task_first[task] + c] * F.ld_h + at;
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
                 const int k = Part<W>::at(h, part);
-                x[h] = row8<true, full.value != 0>(F.hi + at_h + k, F.inner - at - k);
-                z[h] = row8<true, full.value != 0>(F.lo + at_h + k, F.inner - at - k);
-            }
-            v4f y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                const v8b bw = v.eight(h);
-                y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[h], bw, y, 0, 0, 0);
-                y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(z[h], bw, y, 0, 0, 0);
-            }
-            acc[s] += y * scale;
-            if (ends) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = s * 16 + part * 4 + i;
-                    if (r < n) {
-                        const int p = pair_of[p0 + r];
-                        sums[p / F.k * 16 + c] += weight[p] * acc[s][i];
-                    }
-                }
-                acc[s] = v4f{0.f, 0.f, 0.f, 0.f};
+                a.x[h] = row8<true, full.value != 0>(F.hi + at_h + k, F.inner - at - k);
+                a.z[h] = row8<true, full.value != 0>(F.lo + at_h + k, F.inner - at - k);
             }
         }
-        if (ends) wave_lds_done();
+    };
+    auto multiply = [&](const Act& a, const Part<W>& v, float scale) {
+        v4f y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const v8b bw = v.eight(h);
+            y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.x[h], bw, y, 0, 0, 0);
+            y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.z[h], bw, y, 0, 0, 0);
+        }
+        acc += y * scale;
+    };
+    auto keep = [&](int task) {                                   // to the tokens' sums
+        const int n = task_count[task], p0 = task_first[task];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = part * 4 + i;
+            if (r < n) {
+                const int p = pair_of[p0 + r];
+                sums[p / F.k * 16 + c] += weight[p] * acc[i];
+            }
+        }
+        acc = v4f{0.f, 0.f, 0.f, 0.f};
+        wave_lds_done();
     };
     if constexpr (WIDE) {
-        struct Step { Part<W> v[kFewStep]; float k[kFewStep]; int e; };
+        struct Step { Part<W> v[kFewStep]; float k[kFewStep]; };
         const int64_t at_w = col * F.inner, at_s = col / kBlock * nb;
         auto fetch = [&](Step& st, int unit) {
-            const int a = unit / per, step = unit - a * per;
-            st.e = __builtin_amdgcn_readfirstlane(expert_of[a]);
-            const W* base = (const W*)F.w2 + (int64_t)st.e * F.hidden * F.inner + step * (kFewStep * kBlock);
-            const int64_t s2 = (int64_t)st.e * nbh * nb + step * kFewStep + at_s;
+            const int task = unit / per, step = unit - task * per, e = __builtin_amdgcn_readfirstlane(task_expert[task]);
+            const W* base = (const W*)F.w2 + (int64_t)e * F.hidden * F.inner + step * (kFewStep * kBlock);
+            const int64_t s2 = (int64_t)e * nbh * nb + step * kFewStep + at_s;
 #pragma unroll
             for (int i = 0; i < kFewStep; ++i) {
                 st.v[i].template load<WIDE, true>(base + i * kBlock + at_w, part, 0);
                 st.k[i] = scale_value<KIND>(F.s2, s2 + i);
             }
         };
-        auto use = [&](const Step& st, int unit) {
-            const int step = unit % per, p0 = __builtin_amdgcn_readfirstlane(first_of[st.e]), n = __builtin_amdgcn_readfirstlane(count_of[st.e]);
+        // a step's activations are asked for ahead of the next step's weights, as above
+        auto use = [&](const Step& st, int unit, Step& next) {
+            const int task = unit / per, step = unit - task * per;
+            Act a[kFewStep];
 #pragma unroll
-            for (int i = 0; i < kFewStep; ++i)
-                multiply(st.v[i], st.k[i], (int64_t)(step * kFewStep + i) * kBlock, p0, n, i + 1 == kFewStep && (unit + 1 == hi || step + 1 == per), Int<1>{});
+            for (int i = 0; i < kFewStep; ++i) load_h(a[i], task, (int64_t)(step * kFewStep + i) * kBlock, Int<1>{});
+            __builtin_amdgcn_sched_barrier(0);
+            if (unit + 1 < hi) fetch(next, unit + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < kFewStep; ++i) multiply(a[i], st.v[i], st.k[i]);
+            if (unit + 1 == hi || step + 1 == per) keep(task);    // the wave's last of this task
         };
         Step st[2];
         if (lo < hi) fetch(st[0], lo);
         for (int u = lo; u < hi; u += 2) {
-            if (u + 1 < hi) fetch(st[1], u + 1);
-            use(st[0], u);
+            use(st[0], u, st[1]);
             if (u + 1 >= hi) break;
-            if (u + 2 < hi) fetch(st[0], u + 2);
-            use(st[1], u + 1);
+            use(st[1], u + 1, st[0]);
         }
     }
-    for (int a = w; a < n_active; a += kFewSecond) {
-        const int e = __builtin_amdgcn_readfirstlane(expert_of[a]);
-        const int p0 = __builtin_amdgcn_readfirstlane(first_of[e]), n = __builtin_amdgcn_readfirstlane(count_of[e]);
-        for (int64_t b = (int64_t)per * kFewStep; b < nb; ++b) {
-            Part<W> v;
-            v.template load<WIDE, false>((const W*)F.w2 + ((int64_t)e * F.hidden + col) * F.inner + b * kBlock, part, F.inner - b * kBlock);
-            multiply(v, scale_value<KIND>(F.s2, ((int64_t)e * nbh + col / kBlock) * nb + b), b * kBlock, p0, n, b + 1 == nb, Int<0>{});
+    if (per * kFewStep < nb) {
+        for (int task = w; task < n_tasks; task += kFewSecond) {
+            const int e = __builtin_amdgcn_readfirstlane(task_expert[task]);
+            for (int64_t b = (int64_t)per * kFewStep; b < nb; ++b) {
+                Part<W> v;
+                v.template load<WIDE, false>((const W*)F.w2 + ((int64_t)e * F.hidden + col) * F.inner + b * kBlock, part, F.inner - b * kBlock);
+                Act a;
+                load_h(a, task, b * kBlock, Int<0>{});
+                multiply(a, v, scale_value<KIND>(F.s2, ((int64_t)e * nbh + col / kBlock) * nb + b));
+            }
+            keep(task);
         }
     }
     __syncthreads();
