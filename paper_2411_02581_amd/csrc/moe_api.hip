@@ -380,18 +380,18 @@ int tuna_moe_few(const void* x, int64_t ldx, int64_t n_tokens, int64_t hidden, c
     if (rw != TUNA_OK) return rw;
     if ((flags & ~TUNA_ROUTE_RENORM) || !is_float(logits_type) || !is_float(out_type) || (weight_type != TUNA_F8 && weight_type != TUNA_BF16)) return TUNA_ERR_ARG;
     if (n_tokens == 0 || hidden == 0) return TUNA_OK;
+    const size_t pairs = (size_t)n_tokens * k;
     if (inner < 1 || !rows_ok(x, 2, ldx, hidden) || !rows_ok(logits, size_of(logits_type), ld_logits, n_experts) || !rows_ok(out, size_of(out_type), ld_out, hidden))
         return TUNA_ERR_ARG;
     const int wsz = size_of(weight_type);
     if (!w1 || !w2 || !on(w1, wsz) || !on(w2, wsz)) return TUNA_ERR_ARG;
     if (weight_type == TUNA_F8 && (!is_scale(scale_type) || !s1 || !s2 || !on(s1, scale_size(scale_type)) || !on(s2, scale_size(scale_type)))) return TUNA_ERR_ARG;
     if (weight_type != TUNA_F8 && (s1 || s2)) return TUNA_ERR_ARG;
-    if (ldx > kMaxRows / 64 || ceil_div(inner, 16) > kMaxRows / 256 || ceil_div(hidden, 16) > kMaxRows / 256) return TUNA_ERR_TOO_LARGE;
+    if (ldx > (1 << 24) || (int64_t)pairs * (inner + 8) > (1 << 30) || ceil_div(inner, 16) > kMaxRows / 256 || ceil_div(hidden, 16) > kMaxRows / 256) return TUNA_ERR_TOO_LARGE;
     if (!workspace || !on(workspace, 16)) return TUNA_ERR_ARG;
     if (workspace_bytes < need) return TUNA_ERR_WORKSPACE_TOO_SMALL;
     const int rc = tuna_host::ensure_device();
     if (rc != TUNA_OK) return rc;
-    const size_t pairs = (size_t)n_tokens * k;
     char* at = (char*)workspace;
     Few F;
     F.x = (const unsigned short*)x; F.ldx = ldx; F.tokens = (int)n_tokens; F.hidden = hidden;
@@ -402,7 +402,8 @@ int tuna_moe_few(const void* x, int64_t ldx, int64_t n_tokens, int64_t hidden, c
     F.share = (float*)at; at += align16(pairs * 4);
     F.hi = (unsigned short*)at; at += pairs * F.ld_h * 2;
     F.lo = (unsigned short*)at;
-    const bool wide = rows_wide(x, 2, ldx) && on(w1, 16) && on(w2, 16) && (hidden * wsz) % 16 == 0 && (inner * wsz) % 16 == 0;
+    const bool wide = rows_wide(x, 2, ldx) && on(w1, 16) && on(w2, 16) && (hidden * wsz) % 16 == 0 && (inner * wsz) % 16 == 0 &&
+                      hidden <= ((int64_t)1 << 31) / inner / wsz;        // a lane's offset in an expert's half is 32 bits
     // one token: its k experts' rows alone; else all experts', most of which may have nothing to do.  Few pairs: the waves of a workgroup share
     // 16 columns, so that there are workgroups enough for the device; many: each wave has 16, and fewer workgroups look for their tokens
     const bool one = n_tokens == 1, split = one || (int64_t)pairs * ceil_div(inner, 64) < 1024;
@@ -420,7 +421,8 @@ int tuna_moe_few(const void* x, int64_t ldx, int64_t n_tokens, int64_t hidden, c
             });
             with_type(out_type, [&](auto* o) {
                 using O = Pointee<decltype(o)>;
-                hipLaunchKernelGGL((k_few_second<W, kind.value, wd.value != 0, O>), g2, dim3(kFewSecond * 64), sums, (hipStream_t)stream, F);
+                if (one) hipLaunchKernelGGL((k_few_second<W, kind.value, wd.value != 0, O, true>), g2, dim3(kFewSecond * 64), sums, (hipStream_t)stream, F);
+                else hipLaunchKernelGGL((k_few_second<W, kind.value, wd.value != 0, O, false>), g2, dim3(kFewSecond * 64), sums, (hipStream_t)stream, F);
             });
         };
         if (weight_type == TUNA_BF16) both((unsigned short*)nullptr, Int<-1>{});

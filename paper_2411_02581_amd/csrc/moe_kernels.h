@@ -945,25 +945,32 @@ struct Few {
 };
 
 // The parts of 128 neighbours of a row that one of four lanes holds, as they lie in memory, and eight of them at a time as bf16, which holds
-// every e4m3 exactly.  at(h, part): where the eight number h of lane `part` start.  Every load takes 64 bytes of a row in a piece.  FULL: all of
-// it is inside the row, so that the loads hang on no condition and are under way together.
+// every e4m3 exactly.  at(h, part): where the eight number h of lane `part` start.  Every load takes 64 bytes of a row in a piece.  whole(): all of it
+// is inside the row, so that the loads hang on no condition; the address is a wave's base and a lane's 32-bit offset in bytes.
 template <class W> struct Part;
 template <> struct Part<uint8_t> {
     v4u v[2];
     static __device__ __forceinline__ int at(int h, int part) { return (h >> 1) * 64 + part * 16 + (h & 1) * 8; }
-    template <bool WIDE, bool FULL> __device__ __forceinline__ void load(const uint8_t* p, int part, int64_t left) {
+    __device__ __forceinline__ void whole(const uint8_t* base, unsigned off) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            v[i] = FULL ? *(const v4u*)(p + i * 64 + part * 16) : chunk16<WIDE>(p + i * 64 + part * 16, left - (i * 64 + part * 16));
+        for (int i = 0; i < 2; ++i) v[i] = *(const v4u*)(base + i * 64 + (size_t)off);
+    }
+    template <bool WIDE> __device__ __forceinline__ void load(const uint8_t* p, int part, int64_t left) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) v[i] = chunk16<WIDE>(p + i * 64 + part * 16, left - (i * 64 + part * 16));
     }
     __device__ __forceinline__ v8b eight(int h) const { return widen8(v[h >> 1][(h & 1) * 2], v[h >> 1][(h & 1) * 2 + 1]); }
 };
 template <> struct Part<unsigned short> {
     v4u v[4];
     static __device__ __forceinline__ int at(int h, int part) { return h * 32 + part * 8; }
-    template <bool WIDE, bool FULL> __device__ __forceinline__ void load(const unsigned short* p, int part, int64_t left) {
+    __device__ __forceinline__ void whole(const unsigned short* base, unsigned off) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = FULL ? *(const v4u*)(p + at(i, part)) : bits8<WIDE>(p + at(i, part), left - at(i, part));
+        for (int i = 0; i < 4; ++i) v[i] = *(const v4u*)((const uint8_t*)base + i * 64 + (size_t)off);
+    }
+    template <bool WIDE> __device__ __forceinline__ void load(const unsigned short* p, int part, int64_t left) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = bits8<WIDE>(p + at(i, part), left - at(i, part));
     }
     __device__ __forceinline__ v8b eight(int h) const {
         v8b r;
@@ -971,8 +978,7 @@ template <> struct Part<unsigned short> {
         return r;
     }
 };
-template <bool WIDE, bool FULL> __device__ __forceinline__ v8b row8(const unsigned short* p, int64_t left) {
-    const v4u a = FULL ? *(const v4u*)p : bits8<WIDE>(p, left);
+__device__ __forceinline__ v8b as_bf16(const v4u& a) {
     v8b r;
     __builtin_memcpy(&r, &a, 16);
     return r;
@@ -985,7 +991,36 @@ template <int KIND> __device__ __forceinline__ float scale_value(const void* s, 
 
 constexpr int kFewFirst = 4;           // waves of a workgroup of the first kernel: they share the length of the sums
 constexpr int kFewSecond = 8;         // and of the second: they share the experts
-constexpr int kFewStep = 2;            // blocks of 128 that a wave has in registers, while the next ones are on their way
+constexpr int kFewAhead1 = 3;          // blocks of 128 that a wave of the first kernel has in registers or on their way: weights and tokens
+constexpr int kFewAhead2 = 4;          // and of the second: weights and activations
+
+// Units lo .. hi - 1: each is fetched AHEAD - 1 units before it is used.  In the loop no load hangs on a condition, so that a wait for one unit's
+// leaves the later ones' under way.  MANY: the loop runs to the end, where it fetches the last unit again; else the end is a loop of its own,
+// which costs registers and spares short runs those loads (one token: both kernels 23.1 us with them, 18.2 without).
+template <int AHEAD, bool MANY, class S, class FETCH, class USE> __device__ __forceinline__ void pipeline(S (&st)[AHEAD], int lo, int hi, FETCH fetch, USE use) {
+    if (MANY && lo >= hi) return;
+#pragma unroll
+    for (int d = 0; d < AHEAD - 1; ++d) if (MANY || lo + d < hi) fetch(st[d], lo + d < hi ? lo + d : hi - 1);
+    int v = lo;
+    for (; MANY ? v < hi : v + 2 * AHEAD - 2 < hi; v += AHEAD) {
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d) {
+            const int next = v + d + AHEAD - 1;
+            fetch(st[(d + AHEAD - 1) % AHEAD], !MANY || next < hi ? next : hi - 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if (!MANY || v + d < hi) use(st[d], v + d);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    if (!MANY)
+        for (; v < hi; v += AHEAD) {
+#pragma unroll
+            for (int d = 0; d < AHEAD; ++d) {
+                if (v + d + AHEAD - 1 < hi) fetch(st[(d + AHEAD - 1) % AHEAD], v + d + AHEAD - 1);
+                if (v + d < hi) use(st[d], v + d);
+            }
+        }
+}
 
 // First kernel: a workgroup makes 16 activations, or 64, of one expert (as many rows of the gate half and of the up half) for all tokens that
 // chose it, 16 MT of them at a time.  ONE: there is one token, and blockIdx.y counts its chosen experts; else blockIdx.y is the expert, and its tokens
@@ -993,11 +1028,11 @@ constexpr int kFewStep = 2;            // blocks of 128 that a wave has in regis
 template <class L, class W, int KIND, bool WIDE, int MT, bool SPLIT, bool ONE>
 __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
     __shared__ int rank_of[TUNA_MOE_FEW_TOKENS];                  // how many come before this expert, or -1: not chosen
-    __shared__ float share_of[TUNA_MOE_FEW_TOKENS];
     __shared__ int list[TUNA_MOE_FEW_TOKENS];
     __shared__ float sums[SPLIT ? kFewFirst : 1][2][256];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63;
     const bool first = blockIdx.x == 0;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     int e = blockIdx.y, n;
     auto share_in = [&](const L* row, float own) {                // of the softmax over all eligible experts
         float top = -__builtin_inff(), sum = 0.f;
@@ -1068,21 +1103,28 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
                 const int t = t0 + q;
                 if (t >= F.tokens) break;
                 const bool in = logit_key(own[q]) != 0 && before[q] < F.k;
-                float share = 0.f;
-                if (first && in) share = share_in(row[q], own[q]);
-                if (lane == 0) { rank_of[t] = in ? before[q] : -1; share_of[t] = share; }
+                if (lane == 0) rank_of[t] = in ? before[q] : -1;
                 // a token with fewer than k eligible experts: its last places are empty
                 if (first && e == 0 && lane < F.k && lane >= eligible[q]) F.chosen[t * F.k + lane] = -1;
             }
         }
         __syncthreads();
+        if (first) {
+#pragma unroll 1
+            for (int t = w; t < F.tokens; t += kFewFirst)
+                if (rank_of[t] >= 0) {
+                    const L* row = (const L*)F.logits + t * F.ld_logits;
+                    const float s = share_in(row, load1(row + e));
+                    if (lane == 0) {
+                        F.chosen[t * F.k + rank_of[t]] = e;
+                        F.share[t * F.k + rank_of[t]] = s;
+                    }
+                }
+        }
         const bool in = lane < F.tokens && rank_of[lane] >= 0;
         const unsigned long long b = __ballot(in);
         n = __popcll(b);
-        if (w == 0 && in) {
-            list[__popcll(b & ((1ull << lane) - 1))] = lane;
-            if (first) { F.chosen[lane * F.k + rank_of[lane]] = e; F.share[lane * F.k + rank_of[lane]] = share_of[lane]; }
-        }
+        if (w == 0 && in) list[__popcll(b & ((1ull << lane) - 1))] = lane;
         if (n == 0) return;
     }
     __syncthreads();
@@ -1094,8 +1136,9 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
     const W* wu = wg + F.inner * F.hidden;
     const int64_t at_w = col * F.hidden, nb = blocks_of(F.hidden), sg = ((int64_t)e * blocks_of(2 * F.inner) + col / kBlock) * nb,
                   su = ((int64_t)e * blocks_of(2 * F.inner) + (F.inner + col) / kBlock) * nb;
-    // whole steps in a pipeline; blocks behind them (all, for rows that do not start on 16 bytes) one at a time
-    const int64_t steps = WIDE ? F.hidden / (kBlock * kFewStep) : 0;
+    const unsigned off_w = (unsigned)(at_w * sizeof(W)) + part * 16;
+    // whole blocks in a pipeline; what is behind them (all, for rows that do not start on 16 bytes) one block at a time
+    const int whole = WIDE ? (int)(F.hidden / kBlock) : 0;
     for (int t0 = 0; t0 < n; t0 += MT * 16) {                     // more than 16 MT tokens of one expert read its weights again
         v4f gate[MT], up[MT];
         unsigned at_x[MT];
@@ -1103,7 +1146,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
         for (int s = 0; s < MT; ++s) {
             gate[s] = up[s] = v4f{0.f, 0.f, 0.f, 0.f};
             const int i = t0 + s * 16 + c;
-            at_x[s] = i < n ? (unsigned)(list[i] * F.ldx) + Part<W>::at(0, part) : ~0u;
+            at_x[s] = i < n ? (unsigned)(list[i] * F.ldx) : ~0u;
         }
         // the tokens' parts of one block
         auto load_x = [&](v8b (&a)[MT][4], int64_t at, auto full) {
@@ -1112,11 +1155,12 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
 #pragma unroll
                 for (int h = 0; h < 4; ++h) a[s][h] = v8b{};
                 if (at_x[s] != ~0u) {                             // places without a token are zeros, and cost no loads
-                    const unsigned short* row = F.x + at;
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
                         const int k = Part<W>::at(h, 0);
-                        a[s][h] = row8<WIDE, full.value != 0>(row + k + at_x[s], F.hidden - at - k - Part<W>::at(0, part));
+                        const unsigned lane_at = at_x[s] + Part<W>::at(0, part);
+                        if (full.value) a[s][h] = as_bf16(*(const v4u*)((const uint8_t*)(F.x + at + k) + (size_t)(lane_at * 2)));
+                        else a[s][h] = as_bf16(bits8<WIDE>(F.x + at + k + lane_at, F.hidden - at - k - Part<W>::at(0, part)));
                     }
                 }
             }
@@ -1137,44 +1181,26 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
 #pragma unroll
             for (int s = 0; s < MT; ++s) { gate[s] += g[s] * kg; up[s] += u[s] * ku; }
         };
-        struct Step { Part<W> g[kFewStep], u[kFewStep]; float kg[kFewStep], ku[kFewStep]; };
-        auto fetch = [&](Step& st, int64_t step) {
-#pragma unroll
-            for (int i = 0; i < kFewStep; ++i) {
-                const int64_t b = step * kFewStep + i;
-                st.g[i].template load<WIDE, true>(wg + b * kBlock + at_w, part, 0);
-                st.u[i].template load<WIDE, true>(wu + b * kBlock + at_w, part, 0);
-                st.kg[i] = scale_value<KIND>(F.s1, sg + b);
-                st.ku[i] = scale_value<KIND>(F.s1, su + b);
-            }
-        };
-        constexpr int stride = SPLIT ? kFewFirst : 1;
-        // loads come back in the order they were made: a step's tokens are asked for ahead of the next step's weights, which stay under way
-        auto use = [&](const Step& st, int64_t step, Step& next) {
-            v8b a[kFewStep][MT][4];
-#pragma unroll
-            for (int i = 0; i < kFewStep; ++i) load_x(a[i], (step * kFewStep + i) * kBlock, Int<1>{});
-            __builtin_amdgcn_sched_barrier(0);
-            if (step + stride < steps) fetch(next, step + stride);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < kFewStep; ++i) multiply(a[i], st.g[i], st.u[i], st.kg[i], st.ku[i]);
-        };
+        constexpr int stride = SPLIT ? kFewFirst : 1, skip = SPLIT;
         if constexpr (WIDE) {
-            Step st[2];
-            int64_t b = SPLIT ? w : 0;
-            if (b < steps) fetch(st[0], b);
-            for (; b < steps; b += 2 * stride) {
-                use(st[0], b, st[1]);
-                if (b + stride >= steps) break;
-                use(st[1], b + stride, st[0]);
-            }
+            struct Ahead { Part<W> g, u; float kg, ku; v8b a[MT][4]; };
+            Ahead st[kFewAhead1];
+            const int units = (whole - skip * w + stride - 1) / stride;
+            auto fetch = [&](Ahead& t, int unit) {
+                const int64_t b = unit * stride + skip * w;
+                t.g.whole(wg + b * kBlock, off_w);
+                t.u.whole(wu + b * kBlock, off_w);
+                t.kg = scale_value<KIND>(F.s1, sg + b);
+                t.ku = scale_value<KIND>(F.s1, su + b);
+                load_x(t.a, b * kBlock, Int<1>{});
+            };
+            pipeline<kFewAhead1, !SPLIT>(st, 0, units, fetch, [&](const Ahead& t, int) { multiply(t.a, t.g, t.u, t.kg, t.ku); });
         }
-        for (int64_t b = steps * kFewStep + (SPLIT ? w : 0); b < nb; b += stride) {
+        for (int64_t b = whole + skip * w; b < nb; b += stride) {
             Part<W> g, u;
             const int64_t at = b * kBlock;
-            g.template load<WIDE, false>(wg + at + at_w, part, F.hidden - at);
-            u.template load<WIDE, false>(wu + at + at_w, part, F.hidden - at);
+            g.template load<WIDE>(wg + at + at_w, part, F.hidden - at);
+            u.template load<WIDE>(wu + at + at_w, part, F.hidden - at);
             v8b a[MT][4];
             load_x(a, at, Int<0>{});
             multiply(a, g, u, scale_value<KIND>(F.s1, sg + b), scale_value<KIND>(F.s1, su + b));
@@ -1213,7 +1239,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
 // Second kernel: a workgroup per 16 columns of the result, for all tokens and chosen experts.  A task is a chosen expert with up to 16 of its
 // pairs (more of them read its weights again); the tasks' steps are one sequence, of which every wave has a run; a wave's sums are its own,
 // and at the end they are added up in the waves' order.
-template <class W, int KIND, bool WIDE, class OUT>
+template <class W, int KIND, bool WIDE, class OUT, bool ONE>
 __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
     extern __shared__ float shared[];                             // [kFewSecond][tokens][16] sums
     constexpr int PAIRS = TUNA_MOE_FEW_TOKENS * TUNA_MOE_MAX_K;
@@ -1226,54 +1252,66 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
     const int np = F.tokens * F.k;
     float* sums = shared + w * F.tokens * 16;
     for (int i = lane; i < F.tokens * 16; i += 64) sums[i] = 0.f;
-    for (int i = tid; i < F.experts; i += kFewSecond * 64) count_of[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < np; i += kFewSecond * 64) {
-        const int e = F.chosen[i];
-        if (e >= 0) atomicAdd(&count_of[e], 1);
-        float s = e < 0 ? 0.f : F.share[i];
-        if (F.renorm && e >= 0) {
-            const int t0 = i / F.k * F.k;
-            float total = 0.f;
-            for (int j = t0; j < t0 + F.k; ++j) if (F.chosen[j] >= 0) total += F.share[j];
-            s /= total;
+    if (ONE) {                                                    // a task is a pair, in order; the pairs without an expert are the last
+        if (w == 0) {
+            const int e = lane < np ? F.chosen[lane] : -1;
+            float s = e < 0 ? 0.f : F.share[lane];
+            if (F.renorm) s /= wave_sum(s);
+            if (lane < np) { pair_of[lane] = lane; weight[lane] = s; task_expert[lane] = e; task_first[lane] = lane; task_count[lane] = 1; }
+            const int there = __popcll(__ballot(e >= 0));
+            if (lane == 0) n_tasks = there;
         }
-        weight[i] = s;
-    }
-    __syncthreads();
-    if (w == 0) {                                                 // the tasks in order of their experts
-        int tasks = 0, pairs = 0;
-        for (int e0 = 0; e0 < F.experts; e0 += 64) {
-            const int cnt = e0 + lane < F.experts ? count_of[e0 + lane] : 0;
-            const int inc = wave_scan(cnt, lane), parts = (cnt + 15) / 16, inc_parts = wave_scan(parts, lane);
-            if (cnt > 0) {
-                first_of[e0 + lane] = pairs + inc - cnt;
-                count_of[e0 + lane] = 0;
-                for (int i = 0; i < parts; ++i) {
-                    const int at = tasks + inc_parts - parts + i;
-                    task_expert[at] = e0 + lane;
-                    task_first[at] = pairs + inc - cnt + i * 16;
-                    task_count[at] = cnt - i * 16 < 16 ? cnt - i * 16 : 16;
-                }
+        __syncthreads();
+    } else {
+        for (int i = tid; i < F.experts; i += kFewSecond * 64) count_of[i] = 0;
+        __syncthreads();
+        for (int i = tid; i < np; i += kFewSecond * 64) {
+            const int e = F.chosen[i];
+            if (e >= 0) atomicAdd(&count_of[e], 1);
+            float s = e < 0 ? 0.f : F.share[i];
+            if (F.renorm && e >= 0) {
+                const int t0 = i / F.k * F.k;
+                float total = 0.f;
+                for (int j = t0; j < t0 + F.k; ++j) if (F.chosen[j] >= 0) total += F.share[j];
+                s /= total;
             }
-            tasks += __shfl(inc_parts, 63);
-            pairs += __shfl(inc, 63);
+            weight[i] = s;
         }
-        if (lane == 0) n_tasks = tasks;
+        __syncthreads();
+        if (w == 0) {                                                 // the tasks in order of their experts
+            int tasks = 0, pairs = 0;
+            for (int e0 = 0; e0 < F.experts; e0 += 64) {
+                const int cnt = e0 + lane < F.experts ? count_of[e0 + lane] : 0;
+                const int inc = wave_scan(cnt, lane), parts = (cnt + 15) / 16, inc_parts = wave_scan(parts, lane);
+                if (cnt > 0) {
+                    first_of[e0 + lane] = pairs + inc - cnt;
+                    count_of[e0 + lane] = 0;
+                    for (int i = 0; i < parts; ++i) {
+                        const int at = tasks + inc_parts - parts + i;
+                        task_expert[at] = e0 + lane;
+                        task_first[at] = pairs + inc - cnt + i * 16;
+                        task_count[at] = cnt - i * 16 < 16 ? cnt - i * 16 : 16;
+                    }
+                }
+                tasks += __shfl(inc_parts, 63);
+                pairs += __shfl(inc, 63);
+            }
+            if (lane == 0) n_tasks = tasks;
+        }
+        __syncthreads();
+        // the order of an expert's pairs changes no sum: each has its own row
+        for (int i = tid; i < np; i += kFewSecond * 64) {
+            const int e = F.chosen[i];
+            if (e >= 0) pair_of[first_of[e] + atomicAdd(&count_of[e], 1)] = i;
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    // the order of an expert's pairs changes no sum: each has its own row
-    for (int i = tid; i < np; i += kFewSecond * 64) {
-        const int e = F.chosen[i];
-        if (e >= 0) pair_of[first_of[e] + atomicAdd(&count_of[e], 1)] = i;
-    }
-    __syncthreads();
     const int64_t c0 = (int64_t)blockIdx.x * 16;
     const int c = lane & 15, part = lane >> 4;
     const int64_t col = c0 + c < F.hidden ? c0 + c : F.hidden - 1;
     const int64_t nb = blocks_of(F.inner), nbh = blocks_of(F.hidden);
-    // whole steps of all tasks in a pipeline; the blocks behind them (all, for rows that do not start on 16 bytes) one at a time
-    const int per = WIDE ? (int)(F.inner / (kBlock * kFewStep)) : 0;
+    // whole blocks of all tasks in a pipeline; what is behind them (all, for rows that do not start on 16 bytes) one block at a time
+    const int per = WIDE ? (int)(F.inner / kBlock) : 0;
     const int64_t total = (int64_t)n_tasks * per;
     const int lo = (int)(total * w / kFewSecond), hi = (int)(total * (w + 1) / kFewSecond);
     v4f acc = {0.f, 0.f, 0.f, 0.f};
@@ -1283,12 +1321,18 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
 #pragma unroll
         for (int h = 0; h < 4; ++h) a.x[h] = a.z[h] = v8b{};
         if (c < task_count[task]) {                               // places without a pair are zeros, and cost no loads
-            const int64_t at_h = pair_of[task_first[task] + c] * F.ld_h + at;
+            const unsigned lane_at = (unsigned)(pair_of[task_first[task] + c] * F.ld_h) + Part<W>::at(0, part);
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-                const int k = Part<W>::at(h, part);
-                a.x[h] = row8<true, full.value != 0>(F.hi + at_h + k, F.inner - at - k);
-                a.z[h] = row8<true, full.value != 0>(F.lo + at_h + k, F.inner - at - k);
+                const int k = Part<W>::at(h, 0);
+                if (full.value) {
+                    a.x[h] = as_bf16(*(const v4u*)((const uint8_t*)(F.hi + at + k) + (size_t)(lane_at * 2)));
+                    a.z[h] = as_bf16(*(const v4u*)((const uint8_t*)(F.lo + at + k) + (size_t)(lane_at * 2)));
+                } else {
+                    const int64_t left = F.inner - at - k - Part<W>::at(0, part);
+                    a.x[h] = as_bf16(bits8<true>(F.hi + at + k + lane_at, left));
+                    a.z[h] = as_bf16(bits8<true>(F.lo + at + k + lane_at, left));
+                }
             }
         }
     };
@@ -1316,45 +1360,32 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
         wave_lds_done();
     };
     if constexpr (WIDE) {
-        struct Step { Part<W> v[kFewStep]; float k[kFewStep]; };
-        const int64_t at_w = col * F.inner, at_s = col / kBlock * nb;
-        auto fetch = [&](Step& st, int unit) {
-            const int task = unit / per, step = unit - task * per, e = __builtin_amdgcn_readfirstlane(task_expert[task]);
-            const W* base = (const W*)F.w2 + (int64_t)e * F.hidden * F.inner + step * (kFewStep * kBlock);
-            const int64_t s2 = (int64_t)e * nbh * nb + step * kFewStep + at_s;
-#pragma unroll
-            for (int i = 0; i < kFewStep; ++i) {
-                st.v[i].template load<WIDE, true>(base + i * kBlock + at_w, part, 0);
-                st.k[i] = scale_value<KIND>(F.s2, s2 + i);
-            }
+        struct Ahead { Part<W> v; float k; Act a; };
+        struct Cursor { int task, block; };                       // a place in the sequence
+        const int64_t at_s = col / kBlock * nb;
+        const unsigned off_w = (unsigned)(col * F.inner * sizeof(W)) + part * 16;
+        auto step = [&](Cursor& q) { if (++q.block == per) { q.block = 0; ++q.task; } };
+        Cursor now = {per ? lo / per : 0, per ? lo % per : 0}, far = now;
+        auto fetch = [&](Ahead& t, int) {
+            const int e = __builtin_amdgcn_readfirstlane(task_expert[far.task]);
+            t.v.whole((const W*)F.w2 + (int64_t)e * F.hidden * F.inner + far.block * kBlock, off_w);
+            t.k = scale_value<KIND>(F.s2, (int64_t)e * nbh * nb + far.block + at_s);
+            load_h(t.a, far.task, far.block * kBlock, Int<1>{});
+            step(far);
         };
-        // a step's activations are asked for ahead of the next step's weights, as above
-        auto use = [&](const Step& st, int unit, Step& next) {
-            const int task = unit / per, step = unit - task * per;
-            Act a[kFewStep];
-#pragma unroll
-            for (int i = 0; i < kFewStep; ++i) load_h(a[i], task, (int64_t)(step * kFewStep + i) * kBlock, Int<1>{});
-            __builtin_amdgcn_sched_barrier(0);
-            if (unit + 1 < hi) fetch(next, unit + 1);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < kFewStep; ++i) multiply(a[i], st.v[i], st.k[i]);
-            if (unit + 1 == hi || step + 1 == per) keep(task);    // the wave's last of this task
-        };
-        Step st[2];
-        if (lo < hi) fetch(st[0], lo);
-        for (int u = lo; u < hi; u += 2) {
-            use(st[0], u, st[1]);
-            if (u + 1 >= hi) break;
-            use(st[1], u + 1, st[0]);
-        }
+        Ahead st[kFewAhead2];
+        pipeline<kFewAhead2, false>(st, lo, hi, fetch, [&](const Ahead& t, int u) {
+            multiply(t.a, t.v, t.k);
+            if (u + 1 == hi || now.block + 1 == per) keep(now.task);      // the wave's last of this task
+            step(now);
+        });
     }
-    if (per * kFewStep < nb) {
+    if (per < nb) {
         for (int task = w; task < n_tasks; task += kFewSecond) {
             const int e = __builtin_amdgcn_readfirstlane(task_expert[task]);
-            for (int64_t b = (int64_t)per * kFewStep; b < nb; ++b) {
+            for (int64_t b = per; b < nb; ++b) {
                 Part<W> v;
-                v.template load<WIDE, false>((const W*)F.w2 + ((int64_t)e * F.hidden + col) * F.inner + b * kBlock, part, F.inner - b * kBlock);
+                v.template load<WIDE>((const W*)F.w2 + ((int64_t)e * F.hidden + col) * F.inner + b * kBlock, part, F.inner - b * kBlock);
                 Act a;
                 load_h(a, task, b * kBlock, Int<0>{});
                 multiply(a, v, scale_value<KIND>(F.s2, ((int64_t)e * nbh + col / kBlock) * nb + b));
