@@ -228,13 +228,14 @@ bool product_wide(const Product& P, bool cols) {
 
 template <int BM, int BN, int WM, int WN, int KIND, bool COLS, class OUT> void launch_tiles(const Product& P, void* stream) {
     const int64_t nt = ceil_div(P.n, BN), mt = COLS ? ceil_div(P.m, BM) : ceil_div(P.m, BM) + P.groups - 1;
-    LAUNCH((k_product<KIND, COLS, OUT, BM, BN, WM, WN>), dim3((unsigned)(mt * nt * (COLS ? P.groups : 1))), WM * WN * 64, P, (int)mt, (int)nt);
+    const int64_t grid = COLS ? ceil_div(mt * nt, 8) * 8 * P.groups : ceil_div(mt * nt, 8) * 8;
+    LAUNCH((k_product<KIND, COLS, OUT, BM, BN, WM, WN>), dim3((unsigned)grid), WM * WN * 64, P, (int)mt, (int)nt);
 }
 
 // Tiles of the large form: offsets inside a tile are 32 bits, tiles are counted in 31.
 bool product_large(const Product& P, bool cols) {
     const int64_t nt = ceil_div(P.n, 256), mt = ceil_div(P.m, 128) + (cols ? 0 : P.groups - 1);
-    return product_wide(P, cols) && P.lda < (1 << 22) && P.ldb < (1 << 22) && mt * nt <= kMaxRows / (cols ? P.groups : 1) && P.m > 64 && P.n > 64;
+    return product_wide(P, cols) && P.lda < (1 << 22) && P.ldb < (1 << 22) && mt * nt + 8 <= kMaxRows / (cols ? P.groups : 1) && P.m > 64 && P.n > 64;
 }
 
 int launch_product(const Product& P, int kind, bool cols, int out_type, void* stream) {
@@ -244,7 +245,7 @@ int launch_product(const Product& P, int kind, bool cols, int out_type, void* st
             with_bool(kind == TUNA_SCALE_E8, [&](auto sk) {
                 with_bool(cols, [&](auto cl) {
                     if constexpr (sizeof(O) == 2)
-                        if (P.m / P.groups >= 512) return launch_tiles<256, 256, 2, 4, sk.value, cl.value != 0, O>(P, stream);
+                        if (P.m / P.groups >= 256) return launch_tiles<256, 256, 2, 4, sk.value, cl.value != 0, O>(P, stream);
                     launch_tiles<128, 256, 2, 4, sk.value, cl.value != 0, O>(P, stream);
                 });
             });

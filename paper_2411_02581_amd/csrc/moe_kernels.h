@@ -703,10 +703,25 @@ template <int BYTES> __device__ __forceinline__ void to_lds(const void* from, vo
     else __builtin_amdgcn_global_load_lds(g, l, 1, 0, 0);
 }
 
-// Workgroups go to the eight XCDs in turn: each XCD gets a run of neighbouring tiles, whose operands meet in its L2.
-__device__ __forceinline__ unsigned xcd_run(unsigned id, unsigned total) {
-    const unsigned per = total / 8, more = total % 8, x = id % 8;
-    return x * per + (x < more ? x : more) + id / 8;
+// Workgroups go to the eight XCDs in turn: each XCD gets a run of neighbouring tiles, whose operands meet in its L2.  The tile of workgroup `id`
+// among `total`, or -1 (there may be more workgroups than tiles).
+__device__ __forceinline__ int xcd_run(unsigned id, unsigned total) {
+    const unsigned per = total / 8, more = total % 8, x = id % 8, at = id / 8;
+    return at < per + (x < more ? 1 : 0) ? (int)(x * per + (x < more ? x : more) + at) : -1;
+}
+
+// How many tiles of `size` rows the groups have.
+__device__ __forceinline__ int count_tiles(const int32_t* group_rows, int groups, int64_t m, int size) {
+    if (!group_rows) return (int)((m + size - 1) / size);
+    int n = 0;
+    for (int g = threadIdx.x & 63; g < groups; g += 64) {
+        int64_t a, b;
+        group_bounds(group_rows, g, m, a, b);
+        n += (int)((b - a + size - 1) / size);
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
+    return n;
 }
 
 // The large form: a tile of BM x BN, WM x WN waves, blocks of 128 in turn through two halves of the LDS: while one is multiplied the next
@@ -720,11 +735,19 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(Product P, int m_ti
     __shared__ __align__(1024) uint8_t tile[2][(BM + BN) * kBlock];
     __shared__ __align__(16) unsigned scale[2][BM + BN];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w / WN, wn = w % WN;
-    unsigned id = xcd_run(blockIdx.x, gridDim.x);
-    int group = 0;
-    if (COLS) { group = id / (m_tiles * n_tiles); id -= group * (m_tiles * n_tiles); }
+    int group = 0, id;
+    if (COLS) {                                                   // every XCD has an eighth of each group, for groups are of any length
+        const unsigned share = (m_tiles * n_tiles + 7) / 8, at = blockIdx.x / 8;
+        group = at / share;
+        id = blockIdx.x % 8 * share + at % share;
+        if (id >= m_tiles * n_tiles) return;
+    } else {
+        m_tiles = __builtin_amdgcn_readfirstlane(count_tiles(P.group_rows, P.groups, P.m, BM));
+        id = xcd_run(blockIdx.x, (unsigned)m_tiles * n_tiles);
+        if (id < 0) return;
+    }
     // runs of four rows of tiles, column after column
-    const unsigned run = id / (4 * n_tiles), in_run = id - run * 4 * n_tiles, height = m_tiles - run * 4 < 4 ? m_tiles - run * 4 : 4;
+    const int run = id / (4 * n_tiles), in_run = id - run * 4 * n_tiles, height = m_tiles - run * 4 < 4 ? m_tiles - run * 4 : 4;
     const int ti = run * 4 + in_run % height, tj = in_run / height;
     int64_t i0, i_end, kb0 = 0, kb1;
     const int64_t j0 = (int64_t)tj * BN;
