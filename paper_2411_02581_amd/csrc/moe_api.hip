@@ -235,10 +235,32 @@ template <int BM, int BN, int WM, int WN, int KIND, bool COLS, class OUT> void l
 // Tiles of the large form: offsets inside a tile are 32 bits, tiles are counted in 31.
 bool product_large(const Product& P, bool cols) {
     const int64_t nt = ceil_div(P.n, 256), mt = ceil_div(P.m, 128) + (cols ? 0 : P.groups - 1);
-    return product_wide(P, cols) && P.lda < (1 << 22) && P.ldb < (1 << 22) && mt * nt + 8 <= kMaxRows / (cols ? P.groups : 1) && P.m > 64 && P.n > 64;
+    return product_wide(P, cols) && P.lda < (1 << 22) && P.ldb < (1 << 22) && mt * nt + 8 <= kMaxRows / (cols ? P.groups : 1) && P.n > 64;
+}
+
+// Few rows a group: each workgroup reads 16 rows of the weights.
+bool product_thin(const Product& P, bool cols) {
+    return !cols && product_wide(P, cols) && P.m <= (int64_t)P.groups * 64 && ceil_div(P.m, 16) + P.groups <= kMaxGridY && ceil_div(P.n, 16) <= kMaxRows / 512;
 }
 
 int launch_product(const Product& P, int kind, bool cols, int out_type, void* stream) {
+    if (product_thin(P, cols)) {
+        with_type(out_type, [&](auto* o) {
+            using O = Pointee<decltype(o)>;
+            with_bool(kind == TUNA_SCALE_E8, [&](auto sk) {
+                auto rows = [&](auto mt) {
+                    const dim3 grid((unsigned)ceil_div(P.n, 16), (unsigned)(ceil_div(P.m, 16 * mt.value) + P.groups - 1));
+                    LAUNCH((k_product_thin<sk.value, O, mt.value>), grid, kThinWaves * 64, P);
+                };
+                // more rows than a group has on average, for groups are uneven
+                const int64_t each = P.groups == 1 ? P.m : ceil_div(P.m * 3, P.groups * 2);
+                if (each <= 16) rows(Int<1>{});
+                else if (each <= 32) rows(Int<2>{});
+                else rows(Int<4>{});
+            });
+        });
+        return launched();
+    }
     if (product_large(P, cols)) {
         with_type(out_type, [&](auto* o) {
             using O = Pointee<decltype(o)>;

@@ -569,6 +569,34 @@ __global__ __launch_bounds__(256) void k_swiglu_grad(const T* x, int64_t ldx, co
     store8<WIDE>(dx + r * ld_dx + cols + c, left, u);
 }
 
+// Units lo .. hi - 1: each is fetched AHEAD - 1 units before it is used.  In the loop no load hangs on a condition, so that a wait for one unit's
+// leaves the later ones' under way.  MANY: the loop runs to the end, where it fetches the last unit again; else the end is a loop of its own,
+// which costs registers and spares short runs those loads (one token: both kernels 23.1 us with them, 18.2 without).
+template <int AHEAD, bool MANY, class S, class FETCH, class USE> __device__ __forceinline__ void pipeline(S (&st)[AHEAD], int lo, int hi, FETCH fetch, USE use) {
+    if (MANY && lo >= hi) return;
+#pragma unroll
+    for (int d = 0; d < AHEAD - 1; ++d) if (MANY || lo + d < hi) fetch(st[d], lo + d < hi ? lo + d : hi - 1);
+    int v = lo;
+    for (; MANY ? v < hi : v + 2 * AHEAD - 2 < hi; v += AHEAD) {
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d) {
+            const int next = v + d + AHEAD - 1;
+            fetch(st[(d + AHEAD - 1) % AHEAD], !MANY || next < hi ? next : hi - 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if (!MANY || v + d < hi) use(st[d], v + d);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    if (!MANY)
+        for (; v < hi; v += AHEAD) {
+#pragma unroll
+            for (int d = 0; d < AHEAD; ++d) {
+                if (v + d + AHEAD - 1 < hi) fetch(st[(d + AHEAD - 1) % AHEAD], v + d + AHEAD - 1);
+                if (v + d < hi) use(st[d], v + d);
+            }
+        }
+}
+
 // ------------------------------------------------------------------------------------------------ products in 8 bits
 
 // Operands of a product out[i, j] = sum over k of a[i, k] * b[j, k].  Rows a are the activations (or dy transposed), rows b the weights
@@ -610,6 +638,17 @@ __device__ __forceinline__ v4f mma_wide(v8i b, v8i a, v4f c) {
 template <int KIND> __device__ __forceinline__ v4f mma(v8i b, v8i a, v4f c, unsigned sb, unsigned sa) {
     if (KIND == TUNA_SCALE_E8) return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 0, 0, 0, (int)sb, 0, (int)sa);
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 0, 0, 0, 127, 0, 127);
+}
+
+// Up to four neighbours of a row of the result, in one store where all exist and lie on their size.
+template <class OUT> __device__ __forceinline__ void store_four(OUT* o, const v4f& v, int n) {
+    if (n == 4 && ((uintptr_t)o & (4 * sizeof(OUT) - 1)) == 0) {
+        if constexpr (sizeof(OUT) == 2) *(v2u*)o = v2u{(unsigned)to_bf16(v[0]) | (unsigned)to_bf16(v[1]) << 16, (unsigned)to_bf16(v[2]) | (unsigned)to_bf16(v[3]) << 16};
+        else *(v4f*)o = v;
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) if (q < n) store1(o + q, v[q]);
 }
 
 // Which matrix cores: the 8-bit ones add eight neighbouring products at a time, each cut at 2^-13 of the largest one's power of two
@@ -877,7 +916,6 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(Product P, int m_ti
             }
         }
     }
-    const bool even = P.n % 4 == 0 && P.ldo % 4 == 0 && P.out_group % 4 == 0 && ((uintptr_t)P.out & (4 * sizeof(OUT) - 1)) == 0;
     OUT* out = (OUT*)P.out + (COLS ? group * P.out_group : 0);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
@@ -887,17 +925,85 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(Product P, int m_ti
         for (int j = 0; j < NT; ++j) {
             const int64_t col = j0 + (wn * NT + j) * 16 + (lane >> 4) * 4;
             if (col >= P.n) continue;
-            OUT* o = out + row * P.ldo + col;
-            const v4f v = acc[i][j];
-            if (even) {
-                if (sizeof(OUT) == 2) *(v2u*)o = v2u{(unsigned)to_bf16(v[0]) | (unsigned)to_bf16(v[1]) << 16, (unsigned)to_bf16(v[2]) | (unsigned)to_bf16(v[3]) << 16};
-                else *(v4f*)o = v;
-            } else {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) if (col + q < P.n) store1(o + q, v[q]);
-            }
+            store_four(out + row * P.ldo + col, acc[i][j], (int)(P.n - col < 4 ? P.n - col : 4));
         }
     }
+}
+
+// The form for few rows, which reads the weights once and little else: a workgroup has 16 rows of b and 16 MT rows of a, its waves share the
+// blocks of the length, operands go from memory to registers, and the waves' sums are added up in their order.
+constexpr int kThinWaves = 8;
+
+template <int KIND, class OUT, int MT>
+__global__ __launch_bounds__(kThinWaves * 64) void k_product_thin(Product P) {
+    constexpr bool CORE8 = sizeof(OUT) == 2;
+    __shared__ v4f sums[kThinWaves][MT][64];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Place pl = find_tile(P.group_rows, P.groups, P.m, 16 * MT, blockIdx.y);
+    if (pl.group < 0) return;
+    const int group = __builtin_amdgcn_readfirstlane(pl.group);
+    const int64_t i0 = pl.first, i_end = pl.end, j0 = (int64_t)blockIdx.x * 16;
+    const int r = lane & 15, part = lane >> 4;
+    const int64_t rb = j0 + r < P.n ? j0 + r : P.n - 1;
+    const uint8_t* b = P.b + group * P.b_group + rb * P.ldb;
+    const int64_t bs = group * P.bs_group + rb / kBlock * P.ld_bs;
+    const uint8_t* a[MT];
+    int64_t as[MT];
+#pragma unroll
+    for (int s = 0; s < MT; ++s) {
+        const int64_t ra = i0 + s * 16 + r < i_end ? i0 + s * 16 + r : i_end - 1;
+        a[s] = P.a + ra * P.lda;
+        as[s] = ra * P.ld_as;
+    }
+    v4f acc[MT];
+#pragma unroll
+    for (int s = 0; s < MT; ++s) acc[s] = v4f{0.f, 0.f, 0.f, 0.f};
+    struct Ahead { v8i b, a[MT]; unsigned sb, sa[MT]; };
+    // a lane's 32 bytes of a block: sixteen in each half, so that a load takes 64 bytes of a row in a piece
+    auto both = [&](const v4u& x, const v4u& y) { return v8i{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]}; };
+    auto fetch = [&](Ahead& t, int64_t kb, auto full) {
+        const int64_t at = kb * kBlock + part * 16, left = P.k - at;
+        auto row = [&](const uint8_t* p) {
+            if (full.value) return both(*(const v4u*)(p + at), *(const v4u*)(p + at + 64));
+            return both(chunk16<true>(p + at, left), chunk16<true>(p + at + 64, left - 64));
+        };
+        t.b = row(b);
+        t.sb = scale_at<KIND>(P.bs, bs + kb);
+#pragma unroll
+        for (int s = 0; s < MT; ++s) {
+            t.a[s] = row(a[s]);
+            t.sa[s] = scale_at<KIND>(P.as, as[s] + kb);
+        }
+    };
+    auto use = [&](const Ahead& t) {
+#pragma unroll
+        for (int s = 0; s < MT; ++s) {
+            if (CORE8 && KIND == TUNA_SCALE_E8) {
+                acc[s] = mma<KIND>(t.b, t.a[s], acc[s], t.sb, t.sa[s]);
+            } else {
+                // the 16 rows of b lie in one block of 128 and share their scale
+                const v4f zero = {0.f, 0.f, 0.f, 0.f};
+                acc[s] += (CORE8 ? mma<TUNA_SCALE_F32>(t.b, t.a[s], zero, 0, 0) : mma_wide(t.b, t.a[s], zero)) *
+                          (scale_float<KIND>(t.sa[s]) * scale_float<KIND>(t.sb));
+            }
+        }
+    };
+    const int whole = (int)(P.k / kBlock), units = (whole - w + kThinWaves - 1) / kThinWaves;
+    Ahead st[3];
+    pipeline<3, false>(st, 0, units, [&](Ahead& t, int u) { fetch(t, u * kThinWaves + w, Int<1>{}); }, [&](const Ahead& t, int) { use(t); });
+    if (whole * (int64_t)kBlock < P.k && whole % kThinWaves == w) {
+        fetch(st[0], whole, Int<0>{});
+        use(st[0]);
+    }
+#pragma unroll
+    for (int s = 0; s < MT; ++s) sums[w][s][lane] = acc[s];
+    __syncthreads();
+    if (w >= MT) return;
+    v4f v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int q = 0; q < kThinWaves; ++q) v += sums[q][w][lane];
+    const int64_t row = i0 + w * 16 + r, col = j0 + part * 4;
+    if (row < i_end && col < P.n) store_four((OUT*)P.out + row * P.ldo + col, v, (int)(P.n - col < 4 ? P.n - col : 4));
 }
 
 // ------------------------------------------------------------------------------------------------ the sum over a token's experts
@@ -1016,34 +1122,6 @@ constexpr int kFewFirst = 4;           // waves of a workgroup of the first kern
 constexpr int kFewSecond = 8;         // and of the second: they share the experts
 constexpr int kFewAhead1 = 3;          // blocks of 128 that a wave of the first kernel has in registers or on their way: weights and tokens
 constexpr int kFewAhead2 = 4;          // and of the second: weights and activations
-
-// Units lo .. hi - 1: each is fetched AHEAD - 1 units before it is used.  In the loop no load hangs on a condition, so that a wait for one unit's
-// leaves the later ones' under way.  MANY: the loop runs to the end, where it fetches the last unit again; else the end is a loop of its own,
-// which costs registers and spares short runs those loads (one token: both kernels 23.1 us with them, 18.2 without).
-template <int AHEAD, bool MANY, class S, class FETCH, class USE> __device__ __forceinline__ void pipeline(S (&st)[AHEAD], int lo, int hi, FETCH fetch, USE use) {
-    if (MANY && lo >= hi) return;
-#pragma unroll
-    for (int d = 0; d < AHEAD - 1; ++d) if (MANY || lo + d < hi) fetch(st[d], lo + d < hi ? lo + d : hi - 1);
-    int v = lo;
-    for (; MANY ? v < hi : v + 2 * AHEAD - 2 < hi; v += AHEAD) {
-#pragma unroll
-        for (int d = 0; d < AHEAD; ++d) {
-            const int next = v + d + AHEAD - 1;
-            fetch(st[(d + AHEAD - 1) % AHEAD], !MANY || next < hi ? next : hi - 1);
-            __builtin_amdgcn_sched_barrier(0);
-            if (!MANY || v + d < hi) use(st[d], v + d);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    }
-    if (!MANY)
-        for (; v < hi; v += AHEAD) {
-#pragma unroll
-            for (int d = 0; d < AHEAD; ++d) {
-                if (v + d + AHEAD - 1 < hi) fetch(st[(d + AHEAD - 1) % AHEAD], v + d + AHEAD - 1);
-                if (v + d < hi) use(st[d], v + d);
-            }
-        }
-}
 
 // First kernel: a workgroup makes 16 activations, or 64, of one expert (as many rows of the gate half and of the up half) for all tokens that
 // chose it, 16 MT of them at a time.  ONE: there is one token, and blockIdx.y counts its chosen experts; else blockIdx.y is the expert, and its tokens
