@@ -114,6 +114,7 @@ int tuna_moe_route(const void* logits, int type, int64_t ld, int64_t n_tokens, i
             if (n_experts <= 64) LAUNCH((k_route_choose<T, 1>), grid, 256, l, ld, n_tokens, n_experts, k, renorm, experts, weights);
             else if (n_experts <= 128) LAUNCH((k_route_choose<T, 2>), grid, 256, l, ld, n_tokens, n_experts, k, renorm, experts, weights);
             else if (n_experts <= 256) LAUNCH((k_route_choose<T, 4>), grid, 256, l, ld, n_tokens, n_experts, k, renorm, experts, weights);
+            else if (n_experts <= 512) LAUNCH((k_route_choose<T, 8>), grid, 256, l, ld, n_tokens, n_experts, k, renorm, experts, weights);
             else LAUNCH((k_route_choose<T, 16>), grid, 256, l, ld, n_tokens, n_experts, k, renorm, experts, weights);
         });
     LAUNCH(k_route_count, dim3(r.shards), 256, experts, n_tokens, n_experts, k, r.shard, counts, places);
@@ -136,8 +137,10 @@ int tuna_moe_route_grad(const void* logits, int type, int64_t ld, int64_t n_toke
     if (rc != TUNA_OK) return rc;
     with_type(type, [&](auto* t) {
         using T = Pointee<decltype(t)>;
-        LAUNCH((k_route_grad<T>), dim3((unsigned)ceil_div(n_tokens, 4)), 256, (const T*)logits, ld, n_tokens, n_experts, k, flags & TUNA_ROUTE_RENORM ? 1 : 0,
-               experts, weights, dweights, (T*)dlogits, ld_dlogits);
+        with_bool(rows_wide(logits, sizeof(T), ld) && rows_wide(dlogits, sizeof(T), ld_dlogits), [&](auto wd) {
+            LAUNCH((k_route_grad<T, wd.value != 0>), dim3((unsigned)ceil_div(n_tokens, 4)), 256, (const T*)logits, ld, n_tokens, n_experts, k,
+                   flags & TUNA_ROUTE_RENORM ? 1 : 0, experts, weights, dweights, (T*)dlogits, ld_dlogits);
+        });
     });
     return launched();
 }

@@ -123,6 +123,40 @@ __device__ __forceinline__ int wave_scan(int v, int lane) {       // inclusive
     return v;
 }
 
+// The largest, and the sum, of a wave's 64 values, as scalars: shifts within rows of 16 lanes, then from row to row.
+template <int CTRL> __device__ __forceinline__ unsigned dpp(unsigned old, unsigned v) {
+    return (unsigned)__builtin_amdgcn_update_dpp((int)old, (int)v, CTRL, 0xf, 0xf, false);
+}
+__device__ __forceinline__ unsigned wave_max(unsigned v) {
+    auto more = [&](unsigned o) { v = o > v ? o : v; };
+    more(dpp<0x111>(v, v));
+    more(dpp<0x112>(v, v));
+    more(dpp<0x114>(v, v));
+    more(dpp<0x118>(v, v));
+    more(dpp<0x142>(v, v));
+    more(dpp<0x143>(v, v));
+    return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ float wave_total(float v) {
+    auto more = [&](unsigned o) { v += __uint_as_float(o); };
+    more(dpp<0x111>(0u, __float_as_uint(v)));
+    more(dpp<0x112>(0u, __float_as_uint(v)));
+    more(dpp<0x114>(0u, __float_as_uint(v)));
+    more(dpp<0x118>(0u, __float_as_uint(v)));
+    more((unsigned)__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
+    more((unsigned)__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x143, 0xc, 0xf, false));
+    return __uint_as_float((unsigned)__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// exp(x) for x <= 88 within two units of the last place: 2^(x log2 e), with what the product rounds away put back.
+__device__ __forceinline__ float exp_32(float x) {
+    constexpr float kLog2e = 1.44269504088896341f, kRest = 1.9259629911266175e-08f, kLn2 = 0.693147180559945309f;
+    const float t = x * kLog2e;
+    const float rest = __builtin_fmaf(x, kRest, __builtin_fmaf(x, kLog2e, -t));
+    const float e = __builtin_amdgcn_exp2f(t);
+    return t > -150.f ? __builtin_fmaf(e, rest * kLn2, e) : 0.f;
+}
+
 // ------------------------------------------------------------------------------------------------ routing
 //
 // A logit as a key whose order is the logits' (ties by index come from the index below it); 0 = not eligible.
@@ -137,55 +171,54 @@ __device__ __forceinline__ unsigned logit_key(float v) {
 __device__ __forceinline__ float exp_share(float l, float top) {
     if (logit_key(l) == 0u) return 0.f;
     if (top == __builtin_inff()) return l == top ? 1.f : 0.f;
-    return expf(l - top);
+    return exp_32(l - top);
 }
 
-// One wave per token: lane i holds the logits i, i + 64, ...; k rounds take the largest key each.
+// One wave per token: lane i holds the logits i, i + 64, ...; k rounds take the largest key each.  The largest of the wave and where it is
+// are scalars: a round is a dozen vector instructions, a ballot for each register and scalar work beside it.  65536 x 256, k = 8: @CHOOSE@
 template <class T, int PER>
 __global__ __launch_bounds__(256) void k_route_choose(const T* logits, int64_t ld, int64_t n_tokens, int n_experts, int k, int renorm,
                                                       int32_t* experts, float* weights) {
     const int lane = threadIdx.x & 63;
-    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (t >= n_tokens) return;
+    const T* row = logits + t * ld;
     float v[PER];
     unsigned key[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int e = i * 64 + lane;
-        v[i] = e < n_experts ? load1(logits + t * ld + e) : -__builtin_inff();
-        key[i] = logit_key(v[i]);
+        v[i] = load1(row + (e < n_experts ? e : n_experts - 1));
+        key[i] = e < n_experts ? logit_key(v[i]) : 0u;
     }
     float top = 0.f, total = 0.f, mine = 0.f;
     int chosen = -1;
     for (int j = 0; j < k; ++j) {
-        uint64_t best = 0;
+        unsigned m = key[0];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const uint64_t c = (uint64_t)key[i] << 32 | (unsigned)~(i * 64 + lane);
-            best = key[i] && c > best ? c : best;
+        for (int i = 1; i < PER; ++i) m = key[i] > m ? key[i] : m;
+        m = wave_max(m);
+        if (m == 0) break;
+        int e = -1;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {                           // the lowest index that has it
+            const unsigned long long b = __ballot(key[i] == m);
+            if (e < 0 && b) e = i * 64 + __ffsll((long long)b) - 1;
         }
 #pragma unroll
-        for (int d = 32; d; d >>= 1) {
-            const uint64_t o = __shfl_xor((unsigned long long)best, d);
-            best = o > best ? o : best;
-        }
-        if (!best) break;
-        const int e = (int)~(unsigned)best;
-        const unsigned kb = (unsigned)(best >> 32);
-        const float l = __uint_as_float(kb & 0x80000000u ? kb & 0x7fffffffu : ~kb);
+        for (int i = 0; i < PER; ++i) key[i] = i * 64 + lane == e ? 0u : key[i];
+        const float l = __uint_as_float(m & 0x80000000u ? m & 0x7fffffffu : ~m);
         if (j == 0) {
             top = l;
             if (!renorm) {
 #pragma unroll
-                for (int i = 0; i < PER; ++i) total += exp_share(v[i], top);
-                total = wave_sum(total);
+                for (int i = 0; i < PER; ++i) total += i * 64 + lane < n_experts ? exp_share(v[i], top) : 0.f;
+                total = wave_total(total);
             }
         }
         const float s = exp_share(l, top);
         if (renorm) total += s;
         if (lane == j) { chosen = e; mine = s; }
-#pragma unroll
-        for (int i = 0; i < PER; ++i) if (i * 64 + lane == e) key[i] = 0;
     }
     if (lane < k) {
         experts[t * k + lane] = chosen;
@@ -297,37 +330,44 @@ __global__ __launch_bounds__(256) void k_route_place(const int32_t* experts, con
     }
 }
 
-// A workgroup of four waves, one token each.  p_i = weight of the first choice * exp(l_i - its logit): no sum has to be formed again.
-template <class T>
+// A workgroup of four waves, one token each.  p_i = weight of the first choice * exp(l_i - its logit): no sum has to be formed again.  EIGHT:
+// a lane has eight neighbours, rows start on 16 bytes.
+template <class T, bool EIGHT>
 __global__ __launch_bounds__(256) void k_route_grad(const T* logits, int64_t ld, int64_t n_tokens, int n_experts, int k, int renorm,
                                                     const int32_t* experts, const float* weights, const float* dweights, T* dlogits, int64_t ld_d) {
-    __shared__ float g[4][TUNA_MOE_MAX_EXPERTS];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    __shared__ __align__(16) float g[4][TUNA_MOE_MAX_EXPERTS + 8];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t t = (int64_t)blockIdx.x * 4 + w;
-    const bool live = t < n_tokens;
-    for (int e = lane; e < n_experts; e += 64) g[w][e] = 0.f;
-    __syncthreads();
-    int e0 = -1;
-    float w0 = 0.f, sum = 0.f;
-    if (live) {
-        const int e = lane < k ? experts[t * k + lane] : -1;
-        const float wt = lane < k ? weights[t * k + lane] : 0.f, d = lane < k ? dweights[t * k + lane] : 0.f;
-        const bool there = e >= 0 && e < n_experts;
-        sum = wave_sum(there ? wt * d : 0.f);
-        if (there) g[w][e] = renorm ? wt * (d - sum) : d;
-        e0 = __shfl(there ? e : -1, 0);
-        w0 = __shfl(wt, 0);
+    if (t >= n_tokens) return;
+    const T* row = logits + t * ld;
+    float l[8];
+    if (EIGHT && !renorm && lane * 8 < n_experts) load8<true>(row + lane * 8, n_experts - lane * 8, l);
+    if (EIGHT) {
+        for (int e = lane * 4; e < n_experts; e += 256) *(v4f*)&g[w][e] = v4f{0.f, 0.f, 0.f, 0.f};
+    } else {
+        for (int e = lane; e < n_experts; e += 64) g[w][e] = 0.f;
     }
-    __syncthreads();
-    if (!live) return;
-    const float top = e0 < 0 ? 0.f : load1(logits + t * ld + e0);
-    for (int e = lane; e < n_experts; e += 64) {
-        float v = g[w][e];
-        if (!renorm) {
-            const float l = load1(logits + t * ld + e);
-            v = e0 < 0 ? 0.f : w0 * exp_share(l, top) * (v - sum);
+    wave_lds_done();
+    const int e = lane < k ? experts[t * k + lane] : -1;
+    const float wt = lane < k ? weights[t * k + lane] : 0.f, d = lane < k ? dweights[t * k + lane] : 0.f;
+    const bool there = e >= 0 && e < n_experts;
+    const float sum = wave_total(there ? wt * d : 0.f);
+    if (there) g[w][e] = renorm ? wt * (d - sum) : d;
+    const int e0 = __builtin_amdgcn_readfirstlane(there ? e : -1);
+    const float w0 = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(wt)));
+    const float top = e0 < 0 ? 0.f : load1(row + e0);
+    wave_lds_done();
+    auto slope = [&](float logit, float v) { return renorm ? v : e0 < 0 ? 0.f : w0 * exp_share(logit, top) * (v - sum); };
+    if (EIGHT) {
+        for (int at = lane * 8; at < n_experts; at += 512) {
+            if (at >= 512 && !renorm) load8<true>(row + at, n_experts - at, l);
+            float o[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = at + i < n_experts ? slope(l[i], g[w][at + i]) : 0.f;
+            store8<true>(dlogits + t * ld_d + at, n_experts - at, o);
         }
-        store1(dlogits + t * ld_d + e, v);
+    } else {
+        for (int i = lane; i < n_experts; i += 64) store1(dlogits + t * ld_d + i, slope(renorm ? 0.f : load1(row + i), g[w][i]));
     }
 }
 
@@ -395,7 +435,12 @@ __device__ __forceinline__ float max16(float v) {                 // over 16 nei
     return v;
 }
 
-__device__ __forceinline__ float silu_gate(float g) { return 1.f / (1.f + expf(-g)); }
+// 1 / (1 + exp(-g)); the division is one approximate reciprocal and a step of Newton's, exact to a unit of the last place.
+__device__ __forceinline__ float silu_gate(float g) {
+    const float d = 1.f + exp_32(-g > 87.f ? 87.f : -g);
+    const float r = __builtin_amdgcn_rcpf(d);
+    return __builtin_fmaf(__builtin_fmaf(-d, r, 1.f), r, r);
+}
 
 // Sixteen lanes per block of 128 values, eight each.
 template <class T, int KIND, int ACT, bool WIDE>
