@@ -167,6 +167,8 @@ __device__ __forceinline__ unsigned logit_key(float v) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
+__device__ __forceinline__ float key_logit(unsigned key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+
 // exp(l - top) for eligible logits; where the largest is +inf, only those at +inf have a share.
 __device__ __forceinline__ float exp_share(float l, float top) {
     if (logit_key(l) == 0u) return 0.f;
@@ -191,8 +193,8 @@ __global__ __launch_bounds__(256) void k_route_choose(const T* logits, int64_t l
         v[i] = load1(row + (e < n_experts ? e : n_experts - 1));
         key[i] = e < n_experts ? logit_key(v[i]) : 0u;
     }
-    float top = 0.f, total = 0.f, mine = 0.f;
-    int chosen = -1;
+    unsigned first = 0;                                           // the largest key of all
+    int chosen = -1, best = 0;                                    // lane j: the choice number j and its key
     for (int j = 0; j < k; ++j) {
         unsigned m = key[0];
 #pragma unroll
@@ -201,25 +203,25 @@ __global__ __launch_bounds__(256) void k_route_choose(const T* logits, int64_t l
         if (m == 0) break;
         int e = -1;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {                           // the lowest index that has it
+        for (int i = PER - 1; i >= 0; --i) {                      // the lowest index that has it
             const unsigned long long b = __ballot(key[i] == m);
-            if (e < 0 && b) e = i * 64 + __ffsll((long long)b) - 1;
+            e = b ? i * 64 + __ffsll((long long)b) - 1 : e;
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) key[i] = i * 64 + lane == e ? 0u : key[i];
-        const float l = __uint_as_float(m & 0x80000000u ? m & 0x7fffffffu : ~m);
-        if (j == 0) {
-            top = l;
-            if (!renorm) {
-#pragma unroll
-                for (int i = 0; i < PER; ++i) total += i * 64 + lane < n_experts ? exp_share(v[i], top) : 0.f;
-                total = wave_total(total);
-            }
-        }
-        const float s = exp_share(l, top);
-        if (renorm) total += s;
-        if (lane == j) { chosen = e; mine = s; }
+        first = j == 0 ? m : first;
+        chosen = lane == j ? e : chosen;
+        best = lane == j ? (int)m : best;
     }
+    const float top = key_logit(first);
+    const float mine = chosen < 0 ? 0.f : exp_share(key_logit((unsigned)best), top);
+    float total = mine;
+    if (!renorm) {
+        total = 0.f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) total += i * 64 + lane < n_experts ? exp_share(v[i], top) : 0.f;
+    }
+    total = wave_total(total);
     if (lane < k) {
         experts[t * k + lane] = chosen;
         weights[t * k + lane] = chosen < 0 ? 0.f : mine / total;
