@@ -106,17 +106,27 @@ int tuna_moe_route(const void* logits, int type, int64_t ld, int64_t n_tokens, i
     char* ws = (char*)workspace;
     int32_t *counts = (int32_t*)(ws + r.counts), *before = (int32_t*)(ws + r.before), *totals = (int32_t*)(ws + r.totals), *places = (int32_t*)(ws + r.places);
     const int renorm = flags & TUNA_ROUTE_RENORM ? 1 : 0;
+    // a wave holds a token's logits in registers, as many as there may be of them
+    auto held = [&](auto f) {
+        if (n_experts <= 64) f(Int<1>{});
+        else if (n_experts <= 128) f(Int<2>{});
+        else if (n_experts <= 256) f(Int<4>{});
+        else if (n_experts <= 512) f(Int<8>{});
+        else f(Int<16>{});
+    };
+    // up to 64 tokens one workgroup is as fast as the device: what counts is that there is one launch
+    const bool small = !plan && n_tokens > 0 && n_tokens <= 64;
     if (n_tokens > 0)
         with_type(type, [&](auto* t) {
             using T = Pointee<decltype(t)>;
-            const dim3 grid((unsigned)ceil_div(n_tokens, 4));
-            const T* l = (const T*)logits;
-            if (n_experts <= 64) LAUNCH((k_route_choose<T, 1>), grid, 256, l, ld, n_tokens, n_experts, k, renorm, experts, weights);
-            else if (n_experts <= 128) LAUNCH((k_route_choose<T, 2>), grid, 256, l, ld, n_tokens, n_experts, k, renorm, experts, weights);
-            else if (n_experts <= 256) LAUNCH((k_route_choose<T, 4>), grid, 256, l, ld, n_tokens, n_experts, k, renorm, experts, weights);
-            else if (n_experts <= 512) LAUNCH((k_route_choose<T, 8>), grid, 256, l, ld, n_tokens, n_experts, k, renorm, experts, weights);
-            else LAUNCH((k_route_choose<T, 16>), grid, 256, l, ld, n_tokens, n_experts, k, renorm, experts, weights);
+            held([&](auto per) {
+                if (small) LAUNCH((k_route_small<T, per.value>), dim3(1), 1024, (const T*)logits, ld, (int)n_tokens, n_experts, k, renorm, experts, weights, slots,
+                                  expert_rows);
+                else LAUNCH((k_route_choose<T, per.value>), dim3((unsigned)ceil_div(n_tokens, 4)), 256, (const T*)logits, ld, n_tokens, n_experts, k, renorm,
+                            experts, weights);
+            });
         });
+    if (small) return launched();
     LAUNCH(k_route_count, dim3(r.shards), 256, experts, n_tokens, n_experts, k, r.shard, counts, places);
     LAUNCH(k_route_columns, dim3(n_experts), 256, counts, r.shards, n_experts, before, totals);
     LAUNCH(k_route_place, dim3(r.shards), 256, experts, counts, before, totals, n_tokens, n_experts, k, r.shard, r.shards, places, slots, expert_rows,

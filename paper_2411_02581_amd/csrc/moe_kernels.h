@@ -178,13 +178,9 @@ __device__ __forceinline__ float exp_share(float l, float top) {
 
 // One wave per token: lane i holds the logits i, i + 64, ...; k rounds take the largest key each.  The largest of the wave and where it is
 // are scalars: a round is a dozen vector instructions, a ballot for each register and scalar work beside it.  65536 x 256, k = 8: @CHOOSE@
+// Lane j < k receives choice number j (-1: none) and its weight.
 template <class T, int PER>
-__global__ __launch_bounds__(256) void k_route_choose(const T* logits, int64_t ld, int64_t n_tokens, int n_experts, int k, int renorm,
-                                                      int32_t* experts, float* weights) {
-    const int lane = threadIdx.x & 63;
-    const int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (t >= n_tokens) return;
-    const T* row = logits + t * ld;
+__device__ __forceinline__ void choose(const T* row, int n_experts, int k, int renorm, int lane, int& chosen, float& weight) {
     float v[PER];
     unsigned key[PER];
 #pragma unroll
@@ -194,7 +190,8 @@ __global__ __launch_bounds__(256) void k_route_choose(const T* logits, int64_t l
         key[i] = e < n_experts ? logit_key(v[i]) : 0u;
     }
     unsigned first = 0;                                           // the largest key of all
-    int chosen = -1, best = 0;                                    // lane j: the choice number j and its key
+    int best = 0;                                                 // lane j: the key of choice number j
+    chosen = -1;
     for (int j = 0; j < k; ++j) {
         unsigned m = key[0];
 #pragma unroll
@@ -222,9 +219,64 @@ __global__ __launch_bounds__(256) void k_route_choose(const T* logits, int64_t l
         for (int i = 0; i < PER; ++i) total += i * 64 + lane < n_experts ? exp_share(v[i], top) : 0.f;
     }
     total = wave_total(total);
+    weight = chosen < 0 ? 0.f : mine / total;
+}
+
+template <class T, int PER>
+__global__ __launch_bounds__(256) void k_route_choose(const T* logits, int64_t ld, int64_t n_tokens, int n_experts, int k, int renorm,
+                                                      int32_t* experts, float* weights) {
+    const int lane = threadIdx.x & 63;
+    const int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (t >= n_tokens) return;
+    int e;
+    float weight;
+    choose<T, PER>(logits + t * ld, n_experts, k, renorm, lane, e, weight);
     if (lane < k) {
-        experts[t * k + lane] = chosen;
-        weights[t * k + lane] = chosen < 0 ? 0.f : mine / total;
+        experts[t * k + lane] = e;
+        weights[t * k + lane] = weight;
+    }
+}
+
+// Everything for up to 64 tokens without a plan, in one workgroup: sixteen waves choose, then every expert has a word with a bit per token.
+// One launch in place of four: 24 tokens of 64 experts @SMALL@
+template <class T, int PER>
+__global__ __launch_bounds__(1024) void k_route_small(const T* logits, int64_t ld, int n_tokens, int n_experts, int k, int renorm, int32_t* experts,
+                                                      float* weights, int32_t* slots, int32_t* expert_rows) {
+    __shared__ unsigned long long word[TUNA_MOE_MAX_EXPERTS];
+    __shared__ int first[TUNA_MOE_MAX_EXPERTS + 1];
+    __shared__ int part[16];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    word[tid] = 0;                                                // a thread per expert there can be
+    __syncthreads();
+    int mine[4];                                                  // lane j: the choice number j of the wave's tokens w, w + 16, ...
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int t = i * 16 + w;
+        mine[i] = -1;
+        if (t >= n_tokens) break;
+        float weight;
+        choose<T, PER>(logits + t * ld, n_experts, k, renorm, lane, mine[i], weight);
+        if (lane < k) {
+            experts[t * k + lane] = mine[i];
+            weights[t * k + lane] = weight;
+            if (mine[i] >= 0) atomicOr(&word[mine[i]], 1ull << t);
+        }
+    }
+    __syncthreads();
+    const int count = __popcll(word[tid]), inc = wave_scan(count, lane);
+    if (lane == 63) part[w] = inc;
+    __syncthreads();
+    int at = inc - count;
+    for (int i = 0; i < w; ++i) at += part[i];
+    first[tid] = at;
+    if (tid < n_experts) expert_rows[tid] = at;
+    if (tid == n_experts - 1) expert_rows[n_experts] = at + count;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int t = i * 16 + w;
+        if (t >= n_tokens) break;
+        if (lane < k) slots[t * k + lane] = mine[i] < 0 ? -1 : first[mine[i]] + __popcll(word[mine[i]] & ((1ull << t) - 1));
     }
 }
 
