@@ -427,24 +427,22 @@ __global__ __launch_bounds__(256) void k_route_grad(const T* logits, int64_t ld,
 
 // ------------------------------------------------------------------------------------------------ quantisation
 
-struct Scale { float value; unsigned stored; };
+struct Scale { float value; unsigned stored; float inverse; };   // inverse: what scaled() multiplies by, 0: it divides
 
 // The scale of a block whose largest finite magnitude is `peak`.
 template <int KIND> __device__ __forceinline__ Scale scale_of(float peak) {
     Scale s;
-    if (peak == 0.f) {
-        s.value = 1.f;
-        s.stored = KIND == TUNA_SCALE_E8 ? 127u : __float_as_uint(1.f);
-        return s;
-    }
     float v = __fdiv_rn(peak, 448.f);
     v = v < 0x1p-126f ? 0x1p-126f : v;
+    v = peak == 0.f ? 1.f : v;
     if (KIND == TUNA_SCALE_E8) {
         s.stored = (__float_as_uint(v) + 0x7fffffu) >> 23;        // the exponent of the next power of two
         s.value = __uint_as_float(s.stored << 23);
+        s.inverse = __uint_as_float((254u - s.stored) << 23);     // a normal number: the largest scale is below 2^120
     } else {
         s.stored = __float_as_uint(v);
         s.value = v;
+        s.inverse = v < 0x1p-90f ? 0.f : __fdiv_rn(1.f, v);
     }
     return s;
 }
@@ -454,9 +452,13 @@ __device__ __forceinline__ float finite_abs(float v) {
     return a < __builtin_inff() ? a : 0.f;                        // NaN too
 }
 
+// v / scale, rounded once.  A power of two: a product.  Else the product with the rounded inverse and one correction by what it leaves,
+// which gives the rounded quotient (Markstein) as long as that remainder does not underflow: below 2^-90 it divides.
 template <int KIND> __device__ __forceinline__ float scaled(float v, const Scale& s) {
-    // a power of two divides exactly by its reciprocal, which is a normal number for every scale that scale_of gives
-    return KIND == TUNA_SCALE_E8 ? v * __uint_as_float((254u - s.stored) << 23) : __fdiv_rn(v, s.value);
+    if (KIND == TUNA_SCALE_E8) return v * s.inverse;
+    if (s.inverse == 0.f) return __fdiv_rn(v, s.value);
+    const float q = v * s.inverse;
+    return copysignf(__builtin_fmaf(__builtin_fmaf(-q, s.value, v), s.inverse, q), v);      // (the sums lose the sign of -0)
 }
 
 // Four values as e4m3, the first in the lowest byte.
