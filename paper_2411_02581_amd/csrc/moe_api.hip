@@ -28,6 +28,12 @@ inline int scale_size(int type) { return type == TUNA_SCALE_F32 ? 4 : 1; }
 inline bool rows_ok(const void* p, int size, int64_t ld, int64_t cols) { return p && on(p, size) && ld >= cols; }
 inline bool rows_wide(const void* p, int size, int64_t ld) { return on(p, 16) && (ld * size) % 16 == 0; }
 
+// A thread for eight neighbours, a row (y and z) at a time.
+inline bool eights_fit(int64_t rows, int64_t cols) { return ceil_div(rows, 32768) <= kMaxGridY && ceil_div(cols, 2048) <= kMaxRows / 256; }
+inline dim3 eights_grid(int64_t rows, int64_t cols) {
+    return dim3((unsigned)ceil_div(cols, 2048), (unsigned)(rows < 32768 ? rows : 32768), (unsigned)ceil_div(rows, 32768));
+}
+
 inline int launched() {
     const hipError_t e = hipGetLastError();
     if (e == hipSuccess) return TUNA_OK;
@@ -162,20 +168,20 @@ int tuna_fp8_quantize(const void* x, int type, int64_t ldx, int64_t rows, int64_
     if (copies < 1 || copies > TUNA_MOE_MAX_K || (!slots && (copies != 1 || out_rows < rows)) || (slots && !on(slots, 4))) return TUNA_ERR_ARG;
     if (rows == 0 || cols == 0) return TUNA_OK;
     const int64_t width = act == TUNA_ACT_SWIGLU ? 2 * cols : cols, nb = ceil_div(cols, kBlock);
-    if (cols > kMaxRows || rows > kMaxRows || out_rows > kMaxRows || rows * nb > kMaxRows * 16) return TUNA_ERR_TOO_LARGE;
+    if (cols > kMaxRows || rows > kMaxRows || out_rows > kMaxRows || rows * nb > kMaxRows) return TUNA_ERR_TOO_LARGE;
     if (!rows_ok(x, size_of(type), ldx, width)) return TUNA_ERR_ARG;
     if (out_rows > 0 && (!rows_ok(q, 1, ldq, cols) || !rows_ok(scales, scale_size(scale_type), ld_scales, nb))) return TUNA_ERR_ARG;
     if (out_rows == 0) return TUNA_OK;
     const int rc = tuna_host::ensure_device();
     if (rc != TUNA_OK) return rc;
     const bool wide = rows_wide(x, size_of(type), ldx) && on(q, 8) && ldq % 8 == 0 && (act == TUNA_ACT_NONE || (cols * size_of(type)) % 16 == 0);
-    const dim3 grid((unsigned)ceil_div(rows * nb, 16));
+    const dim3 grid((unsigned)ceil_div(rows * nb, 32));
     with_type(type, [&](auto* t) {
         using T = Pointee<decltype(t)>;
         with_bool(scale_type == TUNA_SCALE_E8, [&](auto kind) {
             with_bool(act == TUNA_ACT_SWIGLU, [&](auto a) {
                 with_bool(wide, [&](auto wd) {
-                    LAUNCH((k_quantise<T, kind.value, a.value, wd.value != 0>), grid, 256, (const T*)x, ldx, rows, cols, slots, copies, out_rows, (uint8_t*)q, ldq,
+                    LAUNCH((k_quantise<T, kind.value, a.value, wd.value != 0>), grid, 256, (const T*)x, ldx, (unsigned)(rows * nb), cols, slots, copies, out_rows, (uint8_t*)q, ldq,
                            scales, ld_scales);
                 });
             });
@@ -214,7 +220,7 @@ int tuna_moe_swiglu_grad(const void* x, int type, int64_t ldx, const void* dh, i
                          void* dx, int64_t ld_dx, void* stream) {
     if (rows < 0 || cols < 0 || !is_float(type)) return TUNA_ERR_ARG;
     if (rows == 0 || cols == 0) return TUNA_OK;
-    if (rows > kMaxRows || cols > kMaxRows || rows * ceil_div(cols, 8) > kMaxRows * 256) return TUNA_ERR_TOO_LARGE;
+    if (rows > kMaxRows || cols > kMaxRows || !eights_fit(rows, cols)) return TUNA_ERR_TOO_LARGE;
     const int sz = size_of(type);
     if (!rows_ok(x, sz, ldx, 2 * cols) || !rows_ok(dh, sz, ld_dh, cols) || !rows_ok(dx, sz, ld_dx, 2 * cols)) return TUNA_ERR_ARG;
     const int rc = tuna_host::ensure_device();
@@ -223,7 +229,7 @@ int tuna_moe_swiglu_grad(const void* x, int type, int64_t ldx, const void* dh, i
     with_type(type, [&](auto* t) {
         using T = Pointee<decltype(t)>;
         with_bool(wide, [&](auto wd) {
-            LAUNCH((k_swiglu_grad<T, wd.value != 0>), dim3((unsigned)ceil_div(rows * ceil_div(cols, 8), 256)), 256, (const T*)x, ldx, (const T*)dh, ld_dh, rows,
+            LAUNCH((k_swiglu_grad<T, wd.value != 0>), eights_grid(rows, cols), 256, (const T*)x, ldx, (const T*)dh, ld_dh, rows,
                    cols, (T*)dx, ld_dx);
         });
     });
@@ -354,7 +360,7 @@ int tuna_moe_combine(const void* y, int y_type, int64_t ldy, int64_t y_rows, con
                      int64_t n_tokens, int k, int64_t cols, void* out, int out_type, int64_t ld_out, void* stream) {
     if (n_tokens < 0 || y_rows < 0 || cols < 0 || k < 1 || k > TUNA_MOE_MAX_K || !is_float(y_type) || !is_float(out_type)) return TUNA_ERR_ARG;
     if (n_tokens == 0 || cols == 0) return TUNA_OK;
-    if (n_tokens > kMaxRows / k || y_rows > kMaxRows || cols > kMaxRows || n_tokens * ceil_div(cols, 8) > kMaxRows * 256) return TUNA_ERR_TOO_LARGE;
+    if (n_tokens > kMaxRows / k || y_rows > kMaxRows || cols > kMaxRows || !eights_fit(n_tokens, cols)) return TUNA_ERR_TOO_LARGE;
     if ((y_rows > 0 && !rows_ok(y, size_of(y_type), ldy, cols)) || !slots || !weights || !on(slots, 4) || !on(weights, 4) ||
         !rows_ok(out, size_of(out_type), ld_out, cols))
         return TUNA_ERR_ARG;
@@ -366,7 +372,7 @@ int tuna_moe_combine(const void* y, int y_type, int64_t ldy, int64_t y_rows, con
         with_type(out_type, [&](auto* b) {
             using O = Pointee<decltype(b)>;
             with_bool(wide, [&](auto wd) {
-                LAUNCH((k_combine<Y, O, wd.value != 0>), dim3((unsigned)ceil_div(n_tokens * ceil_div(cols, 8), 256)), 256, (const Y*)y, ldy, y_rows, slots,
+                LAUNCH((k_combine<Y, O, wd.value != 0>), eights_grid(n_tokens, cols), 256, (const Y*)y, ldy, y_rows, slots,
                        weights, n_tokens, k, cols, (O*)out, ld_out);
             });
         });

@@ -498,49 +498,53 @@ __device__ __forceinline__ float silu_gate(float g) {
     return __builtin_fmaf(__builtin_fmaf(-d, r, 1.f), r, r);
 }
 
-// Sixteen lanes per block of 128 values, eight each.
+// Sixteen lanes per block of 128 values, eight each; two blocks in turn, whose loads are under way together.
 template <class T, int KIND, int ACT, bool WIDE>
-__global__ __launch_bounds__(256) void k_quantise(const T* x, int64_t ldx, int64_t rows, int64_t cols, const int32_t* slots, int copies, int64_t out_rows,
+__global__ __launch_bounds__(256) void k_quantise(const T* x, int64_t ldx, unsigned total, int64_t cols, const int32_t* slots, int copies, int64_t out_rows,
                                                   uint8_t* q, int64_t ldq, void* scales, int64_t ld_scales) {
-    const int64_t nb = blocks_of(cols);
-    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
-    if (at >= rows * nb) return;
-    const int64_t r = at / nb, b = at - r * nb;
-    const int64_t c = b * kBlock + (threadIdx.x & 15) * 8, left = cols - c;
-    float v[8];
-    const T* p = x + r * ldx + c;
-    load8<WIDE>(p, left, v);
-    if (ACT == TUNA_ACT_SWIGLU) {
-        float up[8];
-        load8<WIDE>(p + cols, left, up);
+    const unsigned nb = (unsigned)blocks_of(cols), at0 = blockIdx.x * 32 + (threadIdx.x >> 4);
+    float v[2][8], up[2][8];
+    unsigned row[2], block[2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = v[i] * silu_gate(v[i]) * up[i];
-        if (left < 8) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) if (i >= left) v[i] = 0.f;
-        }
+    for (int u = 0; u < 2; ++u) {
+        const unsigned at = at0 + u * 16 < total ? at0 + u * 16 : total - 1;
+        row[u] = at / nb;
+        block[u] = at - row[u] * nb;
+        const int64_t c = (int64_t)block[u] * kBlock + (threadIdx.x & 15) * 8;
+        const T* p = x + row[u] * ldx + c;
+        load8<WIDE>(p, cols - c, v[u]);
+        if (ACT == TUNA_ACT_SWIGLU) load8<WIDE>(p + cols, cols - c, up[u]);
     }
-    float peak = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) peak = fmaxf(peak, finite_abs(v[i]));
-    const Scale s = scale_of<KIND>(max16(peak));
-    const v2u o = quantise8<KIND>(v, s);
-    for (int j = 0; j < copies; ++j) {
-        int64_t to = r;
-        if (slots) {
-            to = slots[r * copies + j];
-            if (to < 0 || to >= out_rows) continue;
-        }
-        uint8_t* d = q + to * ldq + c;
-        if (WIDE && left >= 8) {
-            *(v2u*)d = o;
-        } else {
+    for (int u = 0; u < 2; ++u) {
+        if (at0 + u * 16 >= total) break;                         // (sixteen lanes together)
+        const int64_t r = row[u], b = block[u], c = b * kBlock + (threadIdx.x & 15) * 8, left = cols - c;
+        if (ACT == TUNA_ACT_SWIGLU) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) if (i < left) d[i] = (uint8_t)(o[i >> 2] >> (8 * (i & 3)));
+            for (int i = 0; i < 8; ++i) v[u][i] = i < left ? v[u][i] * silu_gate(v[u][i]) * up[u][i] : 0.f;
         }
-        if ((threadIdx.x & 15) == 0) {
-            if (KIND == TUNA_SCALE_E8) ((uint8_t*)scales)[to * ld_scales + b] = (uint8_t)s.stored;
-            else ((unsigned*)scales)[to * ld_scales + b] = s.stored;
+        float peak = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) peak = fmaxf(peak, finite_abs(v[u][i]));
+        const Scale s = scale_of<KIND>(max16(peak));
+        const v2u o = quantise8<KIND>(v[u], s);
+        for (int j = 0; j < copies; ++j) {
+            int64_t to = r;
+            if (slots) {
+                to = slots[r * copies + j];
+                if (to < 0 || to >= out_rows) continue;
+            }
+            uint8_t* d = q + to * ldq + c;
+            if (WIDE && left >= 8) {
+                *(v2u*)d = o;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) if (i < left) d[i] = (uint8_t)(o[i >> 2] >> (8 * (i & 3)));
+            }
+            if ((threadIdx.x & 15) == 0) {
+                if (KIND == TUNA_SCALE_E8) ((uint8_t*)scales)[to * ld_scales + b] = (uint8_t)s.stored;
+                else ((unsigned*)scales)[to * ld_scales + b] = s.stored;
+            }
         }
     }
 }
@@ -604,6 +608,7 @@ template <class T, int KIND, bool WIDE>
 __global__ __launch_bounds__(256) void k_quantise_columns(const T* x, int64_t ldx, int64_t rows, int64_t cols, const int32_t* group_rows, int groups,
                                                           uint8_t* q, int64_t ldq, void* scales, int64_t ld_scales) {
     __shared__ float peaks[16][kBlock];
+    __shared__ Scale column[kBlock];
     __shared__ __align__(16) uint8_t tile[kBlock][kBlock + 16];
     const Place pl = find_tile(group_rows, groups, rows, kBlock, blockIdx.x);
     if (pl.group < 0) return;
@@ -624,19 +629,25 @@ __global__ __launch_bounds__(256) void k_quantise_columns(const T* x, int64_t ld
         peaks[ry][cx * 8 + j] = p;
     }
     __syncthreads();
+    if (threadIdx.x < kBlock) {                                   // a thread per column: its largest, its scale
+        float p = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p = fmaxf(p, peaks[i][threadIdx.x]);
+        const Scale s = scale_of<KIND>(p);
+        column[threadIdx.x] = s;
+        const int64_t to = (int64_t)blockIdx.y * kBlock + threadIdx.x;
+        if (to < cols) {
+            if (KIND == TUNA_SCALE_E8) ((uint8_t*)scales)[to * ld_scales + pl.block] = (uint8_t)s.stored;
+            else ((unsigned*)scales)[to * ld_scales + pl.block] = s.stored;
+        }
+    }
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        float p = 0.f;
-        for (int i = 0; i < 16; ++i) p = fmaxf(p, peaks[i][cx * 8 + j]);
-        const Scale s = scale_of<KIND>(p);
         float col[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) col[i] = v[i][j];
-        *(v2u*)&tile[cx * 8 + j][ry * 8] = quantise8<KIND>(col, s);
-        if (ry == 0 && c + j < cols) {
-            if (KIND == TUNA_SCALE_E8) ((uint8_t*)scales)[(c + j) * ld_scales + pl.block] = (uint8_t)s.stored;
-            else ((unsigned*)scales)[(c + j) * ld_scales + pl.block] = s.stored;
-        }
+        *(v2u*)&tile[cx * 8 + j][ry * 8] = quantise8<KIND>(col, column[cx * 8 + j]);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < kBlock * 8; i += 256) {
@@ -652,9 +663,8 @@ __global__ __launch_bounds__(256) void k_quantise_columns(const T* x, int64_t ld
 
 template <class T, bool WIDE>
 __global__ __launch_bounds__(256) void k_swiglu_grad(const T* x, int64_t ldx, const T* dh, int64_t ld_dh, int64_t rows, int64_t cols, T* dx, int64_t ld_dx) {
-    const int64_t per = (cols + 7) / 8, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= rows * per) return;
-    const int64_t r = at / per, c = (at - r * per) * 8, left = cols - c;
+    const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, left = cols - c, r = blockIdx.y + (int64_t)blockIdx.z * 32768;
+    if (left <= 0 || r >= rows) return;
     float g[8], u[8], d[8];
     load8<WIDE>(x + r * ldx + c, left, g);
     load8<WIDE>(x + r * ldx + cols + c, left, u);
@@ -1112,9 +1122,8 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_product_thin(Product P) {
 template <class Y, class O, bool WIDE>
 __global__ __launch_bounds__(256) void k_combine(const Y* y, int64_t ldy, int64_t y_rows, const int32_t* slots, const float* weights, int64_t n_tokens, int k,
                                                  int64_t cols, O* out, int64_t ld_out) {
-    const int64_t per = (cols + 7) / 8, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= n_tokens * per) return;
-    const int64_t t = at / per, c = (at - t * per) * 8, left = cols - c;
+    const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, left = cols - c, t = blockIdx.y + (int64_t)blockIdx.z * 32768;
+    if (left <= 0 || t >= n_tokens) return;
     float s[8] = {};
     for (int j = 0; j < k; ++j) {
         const int64_t r = slots[t * k + j];
