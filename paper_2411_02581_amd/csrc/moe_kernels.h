@@ -875,8 +875,8 @@ __device__ __forceinline__ int count_tiles(const int32_t* group_rows, int groups
 }
 
 // The large form: a tile of BM x BN, WM x WN waves, blocks of 128 in turn through two halves of the LDS: while one is multiplied the next
-// one is on its way.  A row's sixteens lie in the LDS at their place xor (row mod 8), so that neighbouring rows' reads meet no bank twice;
-// the lanes load them in that order.
+// one is on its way.  A row's sixteens lie in the LDS at their place xor (row / 2 mod 8), and a lane reads numbers part and part + 4: the
+// sixteen lanes that the LDS serves together then meet every bank once; the lanes load them in that order.
 template <int KIND, bool COLS, class OUT, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(Product P, int m_tiles, int n_tiles) {
     constexpr int W = WM * WN, MT = BM / (16 * WM), NT = BN / (16 * WN), LA = BM / 8 / W, LB = BN / 8 / W;
@@ -921,17 +921,18 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(Product P, int m_ti
     const uint8_t* a = P.a + i0 * P.lda;
     const uint8_t* b = P.b + (COLS ? 0 : group * P.b_group) + j0 * P.ldb;
     const int rows_a = (int)(i_end - i0), rows_b = (int)(P.n - j0 < BN ? P.n - j0 : BN);
-    const int sixteen = ((lane & 7) ^ (lane >> 3)) * 16;
+    const int sixteen = ((lane & 7) ^ (lane >> 4)) * 16;          // of the rows of even loads; of odd ones it is 64 further or nearer
+    static_assert(LA % 2 == 0 && LB % 2 == 0, "");
     unsigned at_a[LA], at_b[LB];
 #pragma unroll
     for (int j = 0; j < LA; ++j) {
         const int r = (w * LA + j) * 8 + (lane >> 3);
-        at_a[j] = (unsigned)((r < rows_a ? r : rows_a - 1) * P.lda) + sixteen;
+        at_a[j] = (unsigned)((r < rows_a ? r : rows_a - 1) * P.lda) + (sixteen ^ (j & 1) * 64);
     }
 #pragma unroll
     for (int j = 0; j < LB; ++j) {
         const int r = (w * LB + j) * 8 + (lane >> 3);
-        at_b[j] = (unsigned)((r < rows_b ? r : rows_b - 1) * P.ldb) + sixteen;
+        at_b[j] = (unsigned)((r < rows_b ? r : rows_b - 1) * P.ldb) + (sixteen ^ (j & 1) * 64);
     }
     const uint8_t* at_s = nullptr;                                // this lane's row of scales
     constexpr int SS = KIND == TUNA_SCALE_E8 ? 1 : 4;
@@ -954,16 +955,15 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(Product P, int m_ti
             for (int j = 0; j < LB; ++j) to_lds<16>(gb + at_b[j], lb + j * 1024);
         } else {                                                  // the row ends inside the block: zeros behind it
             const v4u zero = {0u, 0u, 0u, 0u};
-            if (sixteen < left) {
 #pragma unroll
-                for (int j = 0; j < LA; ++j) to_lds<16>(ga + at_a[j], la + j * 1024);
+            for (int j = 0; j < LA; ++j) {
+                if ((sixteen ^ (j & 1) * 64) < left) to_lds<16>(ga + at_a[j], la + j * 1024);
+                else *(v4u*)(la + j * 1024 + lane * 16) = zero;
+            }
 #pragma unroll
-                for (int j = 0; j < LB; ++j) to_lds<16>(gb + at_b[j], lb + j * 1024);
-            } else {
-#pragma unroll
-                for (int j = 0; j < LA; ++j) *(v4u*)(la + j * 1024 + lane * 16) = zero;
-#pragma unroll
-                for (int j = 0; j < LB; ++j) *(v4u*)(lb + j * 1024 + lane * 16) = zero;
+            for (int j = 0; j < LB; ++j) {
+                if ((sixteen ^ (j & 1) * 64) < left) to_lds<16>(gb + at_b[j], lb + j * 1024);
+                else *(v4u*)(lb + j * 1024 + lane * 16) = zero;
             }
         }
         if (w < (BM + BN) / 64) to_lds<SS>(at_s + kb * SS, &scale[half][w * 64]);
@@ -974,7 +974,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(Product P, int m_ti
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
     if (kb0 < kb1) issue(kb0, 0);
-    const int r = lane & 15, c0 = (((lane >> 4) * 2) ^ (r & 7)) * 16, c1 = (((lane >> 4) * 2 + 1) ^ (r & 7)) * 16;
+    const int r = lane & 15, c0 = ((lane >> 4) ^ (r >> 1)) * 16, c1 = c0 ^ 64;
     int half = 0;
     for (int64_t kb = kb0; kb < kb1; ++kb, half ^= 1) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
