@@ -254,7 +254,7 @@ template <int BM, int BN, int WM, int WN, int KIND, bool COLS, class OUT> void l
 // Tiles of the large form: offsets inside a tile are 32 bits, tiles are counted in 31.
 bool product_large(const Product& P, bool cols) {
     const int64_t nt = ceil_div(P.n, 256), mt = ceil_div(P.m, 128) + (cols ? 0 : P.groups - 1);
-    return product_wide(P, cols) && P.lda < (1 << 22) && P.ldb < (1 << 22) && mt * nt + 8 <= kMaxRows / (cols ? P.groups : 1) && P.n > 64;
+    return product_wide(P, cols) && P.lda < (1 << 22) && P.ldb < (1 << 22) && P.ld_as < (1 << 20) && P.ld_bs < (1 << 20) && mt * nt + 8 <= kMaxRows / (cols ? P.groups : 1) && P.n > 64;
 }
 
 // Few rows a group: each workgroup reads 16 rows of the weights.

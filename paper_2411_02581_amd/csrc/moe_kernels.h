@@ -986,45 +986,47 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(Product P, int m_ti
             const v4u x = *(const v4u*)(t + c0), y = *(const v4u*)(t + c1);
             return v8i{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
         };
-        v8i fb[NT];
+        // the next 16 rows of a are read while these are multiplied
+        v8i fb[NT], fa[2];
+        unsigned ka[2], kbs[NT];
+        v4f kbv[NT];
+        float one = 1.f;
 #pragma unroll
         for (int j = 0; j < NT; ++j) fb[j] = fragment(tb + j * 16 * kBlock);
+        fa[0] = fragment(ta);
+        ka[0] = sa[r];
         if (CORE8 && KIND == TUNA_SCALE_E8) {
-            unsigned kbs[NT];
 #pragma unroll
             for (int j = 0; j < NT; ++j) kbs[j] = sb[j * 16 + r];
+        } else if (COLS) {                                        // by columns every row of b has a scale of its own, else these rows share one
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const v8i fa = fragment(ta + i * 16 * kBlock);
-                const unsigned ka = sa[i * 16 + r];
+            for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = mma<KIND>(fb[j], fa, acc[i][j], kbs[j], ka);
-            }
+                for (int q = 0; q < 4; ++q) kbv[j][q] = scale_float<KIND>(sb[j * 16 + (lane >> 4) * 4 + q]);
         } else {
-            // by columns every row of b has a scale of its own, else these rows share one
-            v4f kbs[NT];
-            float one = 1.f;
-            if (COLS) {
+            one = scale_float<KIND>(sb[0]);
+        }
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) kbs[j][q] = scale_float<KIND>(sb[j * 16 + (lane >> 4) * 4 + q]);
-            } else {
-                one = scale_float<KIND>(sb[0]);
+        for (int i = 0; i < MT; ++i) {
+            if (i + 1 < MT) {
+                fa[(i + 1) & 1] = fragment(ta + (i + 1) * 16 * kBlock);
+                ka[(i + 1) & 1] = sa[(i + 1) * 16 + r];
             }
+            if (CORE8 && KIND == TUNA_SCALE_E8) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const v8i fa = fragment(ta + i * 16 * kBlock);
-                const float ka = scale_float<KIND>(sa[i * 16 + r]) * one;
+                for (int j = 0; j < NT; ++j) acc[i][j] = mma<KIND>(fb[j], fa[i & 1], acc[i][j], kbs[j], ka[i & 1]);
+            } else {
+                const float k = scale_float<KIND>(ka[i & 1]) * one;
                 const v4f zero = {0.f, 0.f, 0.f, 0.f};
                 v4f p[NT];
 #pragma unroll
-                for (int j = 0; j < NT; ++j) p[j] = CORE8 ? mma<TUNA_SCALE_F32>(fb[j], fa, zero, 0, 0) : mma_wide(fb[j], fa, zero);
+                for (int j = 0; j < NT; ++j) p[j] = CORE8 ? mma<TUNA_SCALE_F32>(fb[j], fa[i & 1], zero, 0, 0) : mma_wide(fb[j], fa[i & 1], zero);
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[i][j][q] += COLS ? p[j][q] * kbs[j][q] * ka : p[j][q] * ka;
+                    for (int q = 0; q < 4; ++q) acc[i][j][q] += COLS ? p[j][q] * kbv[j][q] * k : p[j][q] * k;
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     OUT* out = (OUT*)P.out + (COLS ? group * P.out_group : 0);
