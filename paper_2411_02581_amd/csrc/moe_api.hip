@@ -253,7 +253,7 @@ template <int BM, int BN, int WM, int WN, int KIND, bool COLS, class OUT> void l
 
 // Tiles of the large form: offsets inside a tile are 32 bits, tiles are counted in 31.
 bool product_large(const Product& P, bool cols) {
-    const int64_t nt = ceil_div(P.n, 256), mt = ceil_div(P.m, 128) + (cols ? 0 : P.groups - 1);
+    const int64_t nt = ceil_div(P.n, 128), mt = ceil_div(P.m, 128) + (cols ? 0 : P.groups - 1);
     return product_wide(P, cols) && P.lda < (1 << 22) && P.ldb < (1 << 22) && P.ld_as < (1 << 20) && P.ld_bs < (1 << 20) && mt * nt + 8 <= kMaxRows / (cols ? P.groups : 1) && P.n > 64;
 }
 
@@ -287,7 +287,7 @@ int launch_product(const Product& P, int kind, bool cols, int out_type, void* st
                 with_bool(cols, [&](auto cl) {
                     if constexpr (sizeof(O) == 2)
                         if (P.m / P.groups >= 256) return launch_tiles<256, 256, 2, 4, sk.value, cl.value != 0, O>(P, stream);
-                    launch_tiles<128, 256, 2, 4, sk.value, cl.value != 0, O>(P, stream);
+                    launch_tiles<128, 128, 2, 2, sk.value, cl.value != 0, O>(P, stream);
                 });
             });
         });
