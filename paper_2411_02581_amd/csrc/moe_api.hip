@@ -257,9 +257,18 @@ bool product_large(const Product& P, bool cols) {
     return product_wide(P, cols) && P.lda < (1 << 22) && P.ldb < (1 << 22) && P.ld_as < (1 << 20) && P.ld_bs < (1 << 20) && mt * nt + 8 <= kMaxRows / (cols ? P.groups : 1) && P.n > 64;
 }
 
-// Few rows a group: each workgroup reads 16 rows of the weights.
+// Whether tiles of 256 x 256 fill the device: with fewer than a tile for each compute unit, or groups that are mostly shorter than one, tiles of
+// 128 x 128 are faster.  Of 4096 x 4096 weights, a power of two as the scale, 256 x 256 / 128 x 128: 1024 rows 55 / 29 us, 2048 rows 58 / 37,
+// 4096 rows 63 / 72; 64 groups, 3584 x 4096: 8192 rows 282 / 305, 16384 rows 375 / 427.
+bool product_fills(const Product& P, bool cols) {
+    const int64_t tiles = ceil_div(P.m, 256) * ceil_div(P.n, 256) * (cols ? P.groups : 1);
+    return tiles >= 256 && (cols || P.m / P.groups >= 128);
+}
+
+// Few rows: each workgroup reads 16 rows of the weights.  4096 x 4096, this form / tiles of 128 x 128: 8 rows 9 / 27 us, 64 rows 16 / 28; 32 groups:
+// 64 rows 98 / 111, 256 rows 142 / 129, 2048 rows 568 / 139, for every 16 rows read a group's weights again.
 bool product_thin(const Product& P, bool cols) {
-    return !cols && product_wide(P, cols) && P.m <= (int64_t)P.groups * 64 && ceil_div(P.m, 16) + P.groups <= kMaxGridY && ceil_div(P.n, 16) <= kMaxRows / 512;
+    return !cols && product_wide(P, cols) && P.m <= (P.groups == 1 ? 64 : 2 * (int64_t)P.groups) && ceil_div(P.m, 16) + P.groups <= kMaxGridY && ceil_div(P.n, 16) <= kMaxRows / 512;
 }
 
 int launch_product(const Product& P, int kind, bool cols, int out_type, void* stream) {
@@ -271,8 +280,7 @@ int launch_product(const Product& P, int kind, bool cols, int out_type, void* st
                     const dim3 grid((unsigned)ceil_div(P.n, 16), (unsigned)(ceil_div(P.m, 16 * mt.value) + P.groups - 1));
                     LAUNCH((k_product_thin<sk.value, O, mt.value>), grid, kThinWaves * 64, P);
                 };
-                // more rows than a group has on average, for groups are uneven
-                const int64_t each = P.groups == 1 ? P.m : ceil_div(P.m * 3, P.groups * 2);
+                const int64_t each = P.groups == 1 ? P.m : 16;
                 if (each <= 16) rows(Int<1>{});
                 else if (each <= 32) rows(Int<2>{});
                 else rows(Int<4>{});
@@ -286,7 +294,7 @@ int launch_product(const Product& P, int kind, bool cols, int out_type, void* st
             with_bool(kind == TUNA_SCALE_E8, [&](auto sk) {
                 with_bool(cols, [&](auto cl) {
                     if constexpr (sizeof(O) == 2)
-                        if (P.m / P.groups >= 256) return launch_tiles<256, 256, 2, 4, sk.value, cl.value != 0, O>(P, stream);
+                        if (product_fills(P, cols)) return launch_tiles<256, 256, 2, 4, sk.value, cl.value != 0, O>(P, stream);
                     launch_tiles<128, 128, 2, 2, sk.value, cl.value != 0, O>(P, stream);
                 });
             });
