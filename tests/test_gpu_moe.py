@@ -431,6 +431,97 @@ def test_products_are_each_others_gradients(kind):
     assert torch.equal(y.cpu().double(), x @ w.t())
 
 
+@pytest.mark.parametrize("bounds,n,k", [([0, 4000], 4100, 272), ([0, 1500, 1500, 4097], 4100, 400), ([0, 130, 1100, 1100, 2200], 8200, 128)])
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+def test_matmul_of_many_tiles(bounds, n, k, kind):
+    """Enough tiles of 256 x 256 for every compute unit."""
+    product(bounds[-1], n, k, bounds, kind, "bf16")
+
+
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+def test_grad_w_of_many_tiles(kind):
+    bounds, n, k = [0, 200, 200, 329, 340], 2100, 2060
+    m, groups = bounds[-1], 4
+    nb = plain.blocks(m) + groups - 1
+    dy, x = torch.randn(m, n, generator=gen(1)), torch.randn(m, k, generator=gen(2))
+    (q, s, used), (p, t, _) = (plain.quantise_columns(v, bounds, kind, nb * 128) for v in (dy, x))
+    dw = torch.full((groups, n, k), 9.0, dtype=torch.bfloat16, device=DEV)
+    ok(tuna.tuna_fp8_matmul_grad_w(q.to(DEV), nb * 128, s.to(DEV), nb, p.to(DEV), nb * 128, t.to(DEV), nb, KIND[kind],
+                                   torch.tensor(bounds, dtype=torch.int32, device=DEV), groups, dw, tuna.TUNA_BF16, k, n * k, m, n, k))
+    torch.cuda.synchronize()
+    at = 0
+    for g in range(groups):
+        c = plain.blocks(bounds[g + 1] - bounds[g])
+        part = slice(at * 128, (at + c) * 128)
+        a, b = (plain.wide(v[:, part], w[:, at:at + c], kind) if c else torch.zeros(v.shape[0], 0).double() for v, w in ((q, s), (p, t)))
+        check_product(dw[g], a, b, "bf16", max(c, 1) * 128)
+        at += c
+
+
+@pytest.mark.parametrize("m,n,k", [(50, 100, 208), (3, 4112, 1168), (64, 40, 16), (33, 130, 3200)])
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_matmul_of_few_rows(m, n, k, kind, dtype):
+    product(m, n, k, [0, m], kind, dtype)
+
+
+def test_matmul_of_many_groups_of_few_rows():
+    bounds = [0]
+    for g in range(300):
+        bounds.append(bounds[-1] + (20 if g == 7 else g % 3))
+    product(bounds[-1], 48, 272, bounds, "e8", "bf16")
+    product(bounds[-1], 48, 272, bounds, "f32", "f32")
+
+
+# ------------------------------------------------------------------------------------------------ offsets beyond 32 bits
+
+
+def test_rows_beyond_32_bits():
+    """Records and rows whose offsets pass 2^32 bytes and 2^31 elements."""
+    cols, rows = 4096, 1100000
+    x = torch.randn(6, cols, generator=gen(1)).bfloat16()
+    rec = torch.zeros(rows, cols, dtype=torch.uint8, device=DEV)
+    s = torch.zeros(rows, 32, dtype=torch.uint8, device=DEV)
+    slots = torch.tensor([0, 5, 524287, 524288, 1048577, rows - 1], dtype=torch.int32)
+    ok(tuna.tuna_fp8_quantize(x.to(DEV), tuna.TUNA_BF16, cols, 6, cols, 0, slots.to(DEV), 1, rows, rec, cols, s, 32, tuna.TUNA_SCALE_E8))
+    want, ws = plain.quantise(x, "e8")
+    assert torch.equal(rec[slots.long().to(DEV)].cpu(), want) and torch.equal(s[slots.long().to(DEV)].cpu(), ws)
+    assert int((s != 0).any(1).sum()) == 6
+    y = rec.view(torch.bfloat16).view(rows // 2, cols)           # 2^31 elements and more
+    y[-1], y[0] = x[0].to(DEV), x[1].to(DEV)
+    out = torch.zeros(1, cols, device=DEV)
+    at, w = torch.tensor([[rows // 2 - 1, 0]], dtype=torch.int32, device=DEV), torch.tensor([[0.5, 2.0]], device=DEV)
+    ok(tuna.tuna_moe_combine(y, tuna.TUNA_BF16, cols, rows // 2, at, w, 1, 2, cols, out, tuna.TUNA_F32, cols))
+    assert torch.equal(out.cpu()[0], 0.5 * x[0].float() + 2 * x[1].float())
+
+
+def test_weights_beyond_32_bits():
+    experts, inner, hidden = 64, 4096, 8192
+    w1 = torch.zeros(experts, 2 * inner, hidden, dtype=torch.uint8, device=DEV)        # 4 GiB
+    w2 = torch.zeros(experts, hidden, inner, dtype=torch.uint8, device=DEV)
+    small = codes(2 * inner, hidden, 1), codes(hidden, inner, 2)
+    w1[-1], w2[-1] = small[0].to(DEV), small[1].to(DEV)
+    s1 = torch.full((experts, 64, 64), 117, dtype=torch.uint8, device=DEV)
+    s2 = torch.full((experts, 64, 32), 117, dtype=torch.uint8, device=DEV)
+    x = torch.randn(2, hidden, generator=gen(3)).bfloat16()
+    m, n, k = 150, 2 * inner, hidden                             # the last group of a product
+    q, qs = codes(m, k, 4), some_scales((m, 64), "e8", 5)
+    rows = torch.tensor([0] * experts + [m], dtype=torch.int32, device=DEV)
+    y = torch.zeros(m, n, device=DEV)
+    ok(tuna.tuna_fp8_matmul(q.to(DEV), k, qs.to(DEV), 64, w1, k, n * k, s1, 64, 64 * 64, tuna.TUNA_SCALE_E8, rows, experts, y, tuna.TUNA_F32, n, m, n, k))
+    check_product(y, plain.wide(q, qs, "e8"), plain.from_e4m3(small[0]) * 2.0 ** -10, "f32", k)
+    logits = torch.zeros(2, experts)
+    logits[:, -1] = 5.0
+    rc, size = tuna.tuna_moe_few_workspace(2, hidden, inner, experts, 1)
+    ws, out = torch.zeros(size, dtype=torch.uint8, device=DEV), torch.zeros(2, hidden, device=DEV)
+    ok(tuna.tuna_moe_few(x.to(DEV), hidden, 2, hidden, logits.to(DEV), tuna.TUNA_F32, experts, experts, 1, 1, w1, s1, w2, s2, inner, tuna.TUNA_F8,
+                         tuna.TUNA_SCALE_E8, out, tuna.TUNA_F32, hidden, ws, size))
+    a = plain.swiglu(x.double() @ (plain.from_e4m3(small[0]) * 2.0 ** -10).t())
+    b = plain.from_e4m3(small[1]) * 2.0 ** -10
+    room = 2.0 ** -13 * (a.abs() @ b.abs().t())
+    assert bool(((out.cpu().double() - a @ b.t()).abs() <= room).all())
+
+
 # ------------------------------------------------------------------------------------------------ the sum over the experts
 
 
@@ -600,6 +691,41 @@ def test_on_a_stream_of_its_own_and_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(eager, kept):
             assert torch.equal(a, b)
+
+
+def test_the_layer_in_a_graph_and_beside_other_work():
+    """Two streams with workspaces of their own, and replays of a graph, against the eager call."""
+    t, h, f, e, k = 20, 512, 256, 8, 2
+    w1, w2 = (torch.randn(e, r, c, generator=gen(i)).mul(0.05).bfloat16().to(DEV) for i, (r, c) in enumerate(((2 * f, h), (h, f))))
+    x, logits = torch.randn(t, h, generator=gen(2)).bfloat16().to(DEV), torch.randn(t, e, generator=gen(3)).to(DEV)
+    rc, size = tuna.tuna_moe_few_workspace(t, h, f, e, k)
+    new = lambda: (torch.zeros(t, h, device=DEV), torch.zeros(size, dtype=torch.uint8, device=DEV))  # noqa: E731
+
+    def step(out, ws):
+        ok(tuna.tuna_moe_few(x, h, t, h, logits, 0, e, e, k, 1, w1, None, w2, None, f, tuna.TUNA_BF16, 0, out, tuna.TUNA_F32, h, ws, size))
+
+    eager, kept, sides = new(), new(), [(torch.cuda.Stream(), new()) for _ in range(2)]
+    step(*eager)
+    for s, buf in sides:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        for s, buf in sides:
+            with torch.cuda.stream(s):
+                step(*buf)
+    torch.cuda.synchronize()
+    for _, buf in sides:
+        assert torch.equal(buf[0], eager[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=sides[0][0]):
+        step(*kept)
+    for n in range(3):
+        x.copy_(torch.randn(t, h, generator=gen(10 + n)).bfloat16())
+        logits.copy_(torch.randn(t, e, generator=gen(20 + n)))
+        step(*eager)
+        kept[0].fill_(0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(kept[0], eager[0])
 
 
 # ------------------------------------------------------------------------------------------------ the operators together
