@@ -137,8 +137,8 @@ int tuna_fp8_matmul_grad_w(const void* dyt, int64_t ld_dyt, const void* dyt_scal
  */
 int tuna_moe_combine(const void* y, int y_type, int64_t ldy, int64_t y_rows, const int32_t* slots, const float* weights,
                      int64_t n_tokens, int k, int64_t cols, void* out, int out_type, int64_t ld_out, void* stream);
-/* dy[slots[t, j]] = weights[t, j] * dout[t] (y's type; rows without a slot are not written), dweights[t, j] =
- * <dout[t], y[slots[t, j]]> (0 where there is no slot). */
+/* dy[slots[t, j]] = weights[t, j] * dout[t] (y's type; rows without a slot are not written; no two pairs may have one slot),
+ * dweights[t, j] = <dout[t], y[slots[t, j]]> (0 where there is no slot). */
 int tuna_moe_combine_grad(const void* dout, int out_type, int64_t ld_dout, const void* y, int y_type, int64_t ldy, int64_t y_rows,
                           const int32_t* slots, const float* weights, int64_t n_tokens, int k, int64_t cols,
                           void* dy, int64_t ld_dy, float* dweights, void* stream);

@@ -177,7 +177,8 @@ __device__ __forceinline__ float exp_share(float l, float top) {
 }
 
 // One wave per token: lane i holds the logits i, i + 64, ...; k rounds take the largest key each.  The largest of the wave and where it is
-// are scalars: a round is a dozen vector instructions, a ballot for each register and scalar work beside it.  65536 x 256, k = 8: @CHOOSE@
+// are scalars: a round is some thirty vector instructions, a ballot for each register and scalar work beside it.  65536 x 256 in 32 bits, k = 8:
+// 50 us, bound by these instructions (the logits alone take 15 us to read).
 // Lane j < k receives choice number j (-1: none) and its weight.
 template <class T, int PER>
 __device__ __forceinline__ void choose(const T* row, int n_experts, int k, int renorm, int lane, int& chosen, float& weight) {
@@ -238,7 +239,7 @@ __global__ __launch_bounds__(256) void k_route_choose(const T* logits, int64_t l
 }
 
 // Everything for up to 64 tokens without a plan, in one workgroup: sixteen waves choose, then every expert has a word with a bit per token.
-// One launch in place of four: 24 tokens of 64 experts @SMALL@
+// One launch in place of four: 24 tokens of 64 experts 4.6 us in place of 10.1, and less on the host.
 template <class T, int PER>
 __global__ __launch_bounds__(1024) void k_route_small(const T* logits, int64_t ld, int n_tokens, int n_experts, int k, int renorm, int32_t* experts,
                                                       float* weights, int32_t* slots, int32_t* expert_rows) {
@@ -280,6 +281,7 @@ __global__ __launch_bounds__(1024) void k_route_small(const T* logits, int64_t l
     }
 }
 
+// (65536 x 8 pairs of 256 experts: 7.7 us for the count, 5.0 for the columns, 11.2 for the places with the plan's 1.5 MB.)
 // One workgroup per shard of tokens: how many of its pairs every expert has, and each pair's place among them.  A batch is
 // 64 tokens: a bit per token in a word per expert, so the order of the atomics does not matter.
 __global__ __launch_bounds__(256) void k_route_count(const int32_t* experts, int64_t n_tokens, int n_experts, int k, int64_t shard,
@@ -385,7 +387,7 @@ __global__ __launch_bounds__(256) void k_route_place(const int32_t* experts, con
 }
 
 // A workgroup of four waves, one token each.  p_i = weight of the first choice * exp(l_i - its logit): no sum has to be formed again.  EIGHT:
-// a lane has eight neighbours, rows start on 16 bytes.
+// a lane has eight neighbours, rows start on 16 bytes.  65536 x 256 in 32 bits: 39 us, 3.5 TB/s.
 template <class T, bool EIGHT>
 __global__ __launch_bounds__(256) void k_route_grad(const T* logits, int64_t ld, int64_t n_tokens, int n_experts, int k, int renorm,
                                                     const int32_t* experts, const float* weights, const float* dweights, T* dlogits, int64_t ld_d) {
@@ -498,7 +500,8 @@ __device__ __forceinline__ float silu_gate(float g) {
     return __builtin_fmaf(__builtin_fmaf(-d, r, 1.f), r, r);
 }
 
-// Sixteen lanes per block of 128 values, eight each; two blocks in turn, whose loads are under way together.
+// Sixteen lanes per block of 128 values, eight each; two blocks in turn, whose loads are under way together.  Bound by memory: 16384 x 4096 of
+// bf16 to four records each 88 us, 4.6 TB/s; 20011 x 1792 gated 51 us, 3.5 TB/s.
 template <class T, int KIND, int ACT, bool WIDE>
 __global__ __launch_bounds__(256) void k_quantise(const T* x, int64_t ldx, unsigned total, int64_t cols, const int32_t* slots, int copies, int64_t out_rows,
                                                   uint8_t* q, int64_t ldq, void* scales, int64_t ld_scales) {
@@ -603,6 +606,7 @@ __device__ __forceinline__ void group_blocks(const int32_t* group_rows, int g, i
     first = done - count;
 }
 
+// Bound by memory and the two passes through the LDS: 12005 x 2048 and x 2736 of bf16 26 and 36 us, 2.9 TB/s.
 // A tile of 128 rows by 128 columns: thread (16 column chunks of 8) x (16 row chunks of 8).
 template <class T, int KIND, bool WIDE>
 __global__ __launch_bounds__(256) void k_quantise_columns(const T* x, int64_t ldx, int64_t rows, int64_t cols, const int32_t* group_rows, int groups,
@@ -661,6 +665,7 @@ __global__ __launch_bounds__(256) void k_quantise_columns(const T* x, int64_t ld
     }
 }
 
+// Bound by memory: 20011 x 2 x 1792 of bf16 56 us, 6.4 TB/s with what is still in the caches.
 template <class T, bool WIDE>
 __global__ __launch_bounds__(256) void k_swiglu_grad(const T* x, int64_t ldx, const T* dh, int64_t ld_dh, int64_t rows, int64_t cols, T* dx, int64_t ld_dx) {
     const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, left = cols - c, r = blockIdx.y + (int64_t)blockIdx.z * 32768;
@@ -1044,7 +1049,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(Product P, int m_ti
 }
 
 // The form for few rows, which reads the weights once and little else: a workgroup has 16 rows of b and 16 MT rows of a, its waves share the
-// blocks of the length, operands go from memory to registers, and the waves' sums are added up in their order.
+// blocks of the length, operands go from memory to registers, and the waves' sums are added up in their order.  40 x 4096 x 2048: 8.1 us, of which
+// the 8 MB of weights need 2: bound by the way of one load after the start of a kernel, and the launch.
 constexpr int kThinWaves = 8;
 
 template <int KIND, class OUT, int MT>
@@ -1121,6 +1127,7 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_product_thin(Product P) {
 
 // ------------------------------------------------------------------------------------------------ the sum over a token's experts
 
+// Bound by memory: 16384 tokens, k = 8, 4096 columns of bf16 260 us, 4.6 TB/s.
 template <class Y, class O, bool WIDE>
 __global__ __launch_bounds__(256) void k_combine(const Y* y, int64_t ldy, int64_t y_rows, const int32_t* slots, const float* weights, int64_t n_tokens, int k,
                                                  int64_t cols, O* out, int64_t ld_out) {
@@ -1139,7 +1146,7 @@ __global__ __launch_bounds__(256) void k_combine(const Y* y, int64_t ldy, int64_
     store8<WIDE>(out + t * ld_out + c, left, s);
 }
 
-// One workgroup per token.
+// One workgroup per token: a row of dout is read once, k rows of y and dy beside it.  The same sizes: 438 us, 5.2 TB/s.
 template <class O, class Y, bool WIDE>
 __global__ __launch_bounds__(256) void k_combine_grad(const O* dout, int64_t ld_dout, const Y* y, int64_t ldy, int64_t y_rows, const int32_t* slots,
                                                       const float* weights, int k, int64_t cols, Y* dy, int64_t ld_dy, float* dweights) {
@@ -1236,7 +1243,8 @@ constexpr int kFewAhead1 = 3;          // blocks of 128 that a wave of the first
 constexpr int kFewAhead2 = 4;          // and of the second: weights and activations
 
 // First kernel: a workgroup makes 16 activations, or 64, of one expert (as many rows of the gate half and of the up half) for all tokens that
-// chose it, 16 MT of them at a time.  ONE: there is one token, and blockIdx.y counts its chosen experts; else blockIdx.y is the expert, and its tokens
+// chose it, 16 MT of them at a time.  Bound by reading the weights: 40 tokens, k = 8 of 128 experts, 1536 x 4096: 1.49 GB in 360 us, 4.1 TB/s; one
+// token, k = 4, 1024 x 2048: 17 MB in 10 us, the way from logits to weights to sums and the launch.  ONE: there is one token, and blockIdx.y counts its chosen experts; else blockIdx.y is the expert, and its tokens
 // are found without a sort: it is among the k first of a token when fewer than k eligible logits come before its own.
 template <class L, class W, int KIND, bool WIDE, int MT, bool SPLIT, bool ONE>
 __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
@@ -1450,7 +1458,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
 }
 
 // Second kernel: a workgroup per 16 columns of the result, for all tokens and chosen experts.  A task is a chosen expert with up to 16 of its
-// pairs (more of them read its weights again); the tasks' steps are one sequence, of which every wave has a run; a wave's sums are its own,
+// pairs (more of them read its weights again); 0.74 GB in 208 us, 3.6 TB/s, and 8.4 MB in 7 us for the sizes above.  The tasks' steps are one sequence, of which every wave has a run; a wave's sums are its own,
 // and at the end they are added up in the waves' order.
 template <class W, int KIND, bool WIDE, class OUT, bool ONE>
 __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
