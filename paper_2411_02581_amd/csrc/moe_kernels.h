@@ -984,7 +984,6 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(Product P, int m_ti
     for (int64_t kb = kb0; kb < kb1; ++kb, half ^= 1) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        if (kb + 1 < kb1) issue(kb + 1, half ^ 1);
         const uint8_t *ta = tile[half] + (wm * MT * 16 + r) * kBlock, *tb = tile[half] + (BM + wn * NT * 16 + r) * kBlock;
         const unsigned *sa = scale[half] + wm * MT * 16, *sb = scale[half] + BM + wn * NT * 16;
         auto fragment = [&](const uint8_t* t) {
@@ -1011,6 +1010,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(Product P, int m_ti
         } else {
             one = scale_float<KIND>(sb[0]);
         }
+        if (kb + 1 < kb1) issue(kb + 1, half ^ 1);
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             if (i + 1 < MT) {
