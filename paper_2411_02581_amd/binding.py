@@ -459,8 +459,9 @@ def _rows(a: Any, type_code: Optional[int] = None) -> Optional[int]:
 
 def tuna_moe_route(logits, type: int, ld: int, n_tokens: int, n_experts: int, k: int, flags: int, experts, weights, slots, expert_rows,
                    row_bytes: int, sendcounts, sdispls, recvcounts, rdispls, workspace, workspace_bytes: int, stream=None) -> int:
-    return load().tuna_moe_route(_rows(logits, type), type, ld, n_tokens, n_experts, k, flags, _ptr(experts), _ptr(weights), _ptr(slots),
-                                 _ptr(expert_rows), row_bytes, _ptr(sendcounts), _ptr(sdispls), _ptr(recvcounts), _ptr(rdispls),
+    import torch
+    return load().tuna_moe_route(_rows(logits, type), type, ld, n_tokens, n_experts, k, flags, _ptr(experts, torch.int32), _ptr(weights, torch.float32), _ptr(slots, torch.int32),
+                                 _ptr(expert_rows, torch.int32), row_bytes, _ptr(sendcounts, torch.int32), _ptr(sdispls, torch.int64), _ptr(recvcounts, torch.int32), _ptr(rdispls, torch.int64),
                                  _ptr(workspace), workspace_bytes, _stream(stream))
 
 
@@ -473,19 +474,22 @@ def tuna_moe_route_workspace(n_tokens: int, n_experts: int, k: int, with_plan: b
 
 def tuna_moe_route_grad(logits, type: int, ld: int, n_tokens: int, n_experts: int, k: int, flags: int, experts, weights, dweights,
                         dlogits, ld_dlogits: int, stream=None) -> int:
-    return load().tuna_moe_route_grad(_rows(logits, type), type, ld, n_tokens, n_experts, k, flags, _ptr(experts), _ptr(weights),
-                                      _ptr(dweights), _rows(dlogits, type), ld_dlogits, _stream(stream))
+    import torch
+    return load().tuna_moe_route_grad(_rows(logits, type), type, ld, n_tokens, n_experts, k, flags, _ptr(experts, torch.int32), _ptr(weights, torch.float32),
+                                      _ptr(dweights, torch.float32), _rows(dlogits, type), ld_dlogits, _stream(stream))
 
 
 def tuna_fp8_quantize(x, type: int, ldx: int, rows: int, cols: int, act: int, slots, copies: int, out_rows: int, q, ldq: int,
                       scales, ld_scales: int, scale_type: int, stream=None) -> int:
-    return load().tuna_fp8_quantize(_rows(x, type), type, ldx, rows, cols, act, _ptr(slots), copies, out_rows, _rows(q), ldq,
+    import torch
+    return load().tuna_fp8_quantize(_rows(x, type), type, ldx, rows, cols, act, _ptr(slots, torch.int32), copies, out_rows, _rows(q), ldq,
                                     _rows(scales), ld_scales, scale_type, _stream(stream))
 
 
 def tuna_fp8_quantize_columns(x, type: int, ldx: int, rows: int, cols: int, group_rows, groups: int, q, ldq: int, scales,
                               ld_scales: int, scale_type: int, stream=None) -> int:
-    return load().tuna_fp8_quantize_columns(_rows(x, type), type, ldx, rows, cols, _ptr(group_rows), groups, _rows(q), ldq,
+    import torch
+    return load().tuna_fp8_quantize_columns(_rows(x, type), type, ldx, rows, cols, _ptr(group_rows, torch.int32), groups, _rows(q), ldq,
                                             _rows(scales), ld_scales, scale_type, _stream(stream))
 
 
@@ -495,27 +499,31 @@ def tuna_moe_swiglu_grad(x, type: int, ldx: int, dh, ld_dh: int, rows: int, cols
 
 def tuna_fp8_matmul(x, ldx: int, xs, ld_xs: int, w, ldw: int, w_group: int, ws, ld_ws: int, ws_group: int, scale_type: int,
                     group_rows, groups: int, y, y_type: int, ldy: int, m: int, n: int, k: int, stream=None) -> int:
+    import torch
     return load().tuna_fp8_matmul(_rows(x, TUNA_F8), ldx, _rows(xs), ld_xs, _rows(w, TUNA_F8), ldw, w_group, _rows(ws), ld_ws, ws_group,
-                                  scale_type, _ptr(group_rows), groups, _rows(y, y_type), y_type, ldy, m, n, k, _stream(stream))
+                                  scale_type, _ptr(group_rows, torch.int32), groups, _rows(y, y_type), y_type, ldy, m, n, k, _stream(stream))
 
 
 def tuna_fp8_matmul_grad_w(dyt, ld_dyt: int, dyt_scales, ld_dyt_scales: int, xt, ld_xt: int, xt_scales, ld_xt_scales: int, scale_type: int,
                            group_rows, groups: int, dw, dw_type: int, ld_dw: int, dw_group: int, m: int, n: int, k: int, stream=None) -> int:
+    import torch
     return load().tuna_fp8_matmul_grad_w(_rows(dyt, TUNA_F8), ld_dyt, _rows(dyt_scales), ld_dyt_scales, _rows(xt, TUNA_F8), ld_xt,
-                                         _rows(xt_scales), ld_xt_scales, scale_type, _ptr(group_rows), groups, _rows(dw, dw_type),
+                                         _rows(xt_scales), ld_xt_scales, scale_type, _ptr(group_rows, torch.int32), groups, _rows(dw, dw_type),
                                          dw_type, ld_dw, dw_group, m, n, k, _stream(stream))
 
 
 def tuna_moe_combine(y, y_type: int, ldy: int, y_rows: int, slots, weights, n_tokens: int, k: int, cols: int, out, out_type: int,
                      ld_out: int, stream=None) -> int:
-    return load().tuna_moe_combine(_rows(y, y_type), y_type, ldy, y_rows, _ptr(slots), _ptr(weights), n_tokens, k, cols,
+    import torch
+    return load().tuna_moe_combine(_rows(y, y_type), y_type, ldy, y_rows, _ptr(slots, torch.int32), _ptr(weights, torch.float32), n_tokens, k, cols,
                                    _rows(out, out_type), out_type, ld_out, _stream(stream))
 
 
 def tuna_moe_combine_grad(dout, out_type: int, ld_dout: int, y, y_type: int, ldy: int, y_rows: int, slots, weights, n_tokens: int, k: int,
                           cols: int, dy, ld_dy: int, dweights, stream=None) -> int:
-    return load().tuna_moe_combine_grad(_rows(dout, out_type), out_type, ld_dout, _rows(y, y_type), y_type, ldy, y_rows, _ptr(slots),
-                                        _ptr(weights), n_tokens, k, cols, _rows(dy, y_type), ld_dy, _ptr(dweights), _stream(stream))
+    import torch
+    return load().tuna_moe_combine_grad(_rows(dout, out_type), out_type, ld_dout, _rows(y, y_type), y_type, ldy, y_rows, _ptr(slots, torch.int32),
+                                        _ptr(weights, torch.float32), n_tokens, k, cols, _rows(dy, y_type), ld_dy, _ptr(dweights, torch.float32), _stream(stream))
 
 
 def tuna_moe_few(x, ldx: int, n_tokens: int, hidden: int, logits, logits_type: int, ld_logits: int, n_experts: int, k: int, flags: int,

@@ -153,10 +153,14 @@ int tuna_moe_route_grad(const void* logits, int type, int64_t ld, int64_t n_toke
     if (rc != TUNA_OK) return rc;
     with_type(type, [&](auto* t) {
         using T = Pointee<decltype(t)>;
-        with_bool(rows_wide(logits, sizeof(T), ld) && rows_wide(dlogits, sizeof(T), ld_dlogits), [&](auto wd) {
-            LAUNCH((k_route_grad<T, wd.value != 0>), dim3((unsigned)ceil_div(n_tokens, 4)), 256, (const T*)logits, ld, n_tokens, n_experts, k,
+        auto go = [&](auto n) {
+            LAUNCH((k_route_grad<T, n.value>), dim3((unsigned)ceil_div(n_tokens, 4)), 256, (const T*)logits, ld, n_tokens, n_experts, k,
                    flags & TUNA_ROUTE_RENORM ? 1 : 0, experts, weights, dweights, (T*)dlogits, ld_dlogits);
-        });
+        };
+        const bool wide = rows_wide(logits, sizeof(T), ld) && rows_wide(dlogits, sizeof(T), ld_dlogits);
+        if (wide && n_experts <= 256 && n_experts % 4 == 0) go(Int<4>{});
+        else if (wide && n_experts % 8 == 0) go(Int<8>{});
+        else go(Int<1>{});
     });
     return launched();
 }

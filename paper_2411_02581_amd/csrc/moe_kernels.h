@@ -386,26 +386,54 @@ __global__ __launch_bounds__(256) void k_route_place(const int32_t* experts, con
     }
 }
 
-// A workgroup of four waves, one token each.  p_i = weight of the first choice * exp(l_i - its logit): no sum has to be formed again.  EIGHT:
-// a lane has eight neighbours, rows start on 16 bytes.  65536 x 256 in 32 bits: 39 us, 3.5 TB/s.
-template <class T, bool EIGHT>
+// N neighbours of a row in one load or store, N = 4 or 8; rows start on 16 bytes and N divides what is left of them.
+template <int N> __device__ __forceinline__ void load_n(const float* p, float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        const v4f a = *(const v4f*)(p + i);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[i + q] = a[q];
+    }
+}
+template <int N> __device__ __forceinline__ void load_n(const unsigned short* p, float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        const v2u a = *(const v2u*)(p + i);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[i + q] = bf16_bits((unsigned short)(a[q >> 1] >> 16 * (q & 1)));
+    }
+}
+template <int N> __device__ __forceinline__ void store_n(float* p, const float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) *(v4f*)(p + i) = v4f{v[i], v[i + 1], v[i + 2], v[i + 3]};
+}
+template <int N> __device__ __forceinline__ void store_n(unsigned short* p, const float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+        *(v2u*)(p + i) = v2u{(unsigned)to_bf16(v[i]) | (unsigned)to_bf16(v[i + 1]) << 16, (unsigned)to_bf16(v[i + 2]) | (unsigned)to_bf16(v[i + 3]) << 16};
+}
+
+// A workgroup of four waves, one token each.  p_i = weight of the first choice * exp(l_i - its logit): no sum has to be formed again.  N > 1:
+// a lane has N neighbours (four up to 256 experts, so that all lanes have some, else eight).  65536 x 256 in 32 bits: 26 us, 5.2 TB/s.
+template <class T, int N>
 __global__ __launch_bounds__(256) void k_route_grad(const T* logits, int64_t ld, int64_t n_tokens, int n_experts, int k, int renorm,
                                                     const int32_t* experts, const float* weights, const float* dweights, T* dlogits, int64_t ld_d) {
-    __shared__ __align__(16) float g[4][TUNA_MOE_MAX_EXPERTS + 8];
+    __shared__ __align__(16) float g[4][TUNA_MOE_MAX_EXPERTS];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t t = (int64_t)blockIdx.x * 4 + w;
     if (t >= n_tokens) return;
     const T* row = logits + t * ld;
-    float l[8];
-    if (EIGHT && !renorm && lane * 8 < n_experts) load8<true>(row + lane * 8, n_experts - lane * 8, l);
-    if (EIGHT) {
-        for (int e = lane * 4; e < n_experts; e += 256) *(v4f*)&g[w][e] = v4f{0.f, 0.f, 0.f, 0.f};
-    } else {
-        for (int e = lane; e < n_experts; e += 64) g[w][e] = 0.f;
-    }
-    wave_lds_done();
     const int e = lane < k ? experts[t * k + lane] : -1;
     const float wt = lane < k ? weights[t * k + lane] : 0.f, d = lane < k ? dweights[t * k + lane] : 0.f;
+    constexpr int M = N > 1 ? N : 4;
+    float l[M] = {};
+    if (N > 1 && !renorm && lane * M < n_experts) load_n<M>(row + lane * M, l);
+    if (N > 1) {
+        for (int i = lane * 4; i < n_experts; i += 256) *(v4f*)&g[w][i] = v4f{0.f, 0.f, 0.f, 0.f};
+    } else {
+        for (int i = lane; i < n_experts; i += 64) g[w][i] = 0.f;
+    }
+    wave_lds_done();
     const bool there = e >= 0 && e < n_experts;
     const float sum = wave_total(there ? wt * d : 0.f);
     if (there) g[w][e] = renorm ? wt * (d - sum) : d;
@@ -414,13 +442,13 @@ __global__ __launch_bounds__(256) void k_route_grad(const T* logits, int64_t ld,
     const float top = e0 < 0 ? 0.f : load1(row + e0);
     wave_lds_done();
     auto slope = [&](float logit, float v) { return renorm ? v : e0 < 0 ? 0.f : w0 * exp_share(logit, top) * (v - sum); };
-    if (EIGHT) {
-        for (int at = lane * 8; at < n_experts; at += 512) {
-            if (at >= 512 && !renorm) load8<true>(row + at, n_experts - at, l);
-            float o[8];
+    if (N > 1) {
+        for (int at = lane * M; at < n_experts; at += 64 * M) {
+            if (at >= 64 * M && !renorm) load_n<M>(row + at, l);
+            float o[M];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = at + i < n_experts ? slope(l[i], g[w][at + i]) : 0.f;
-            store8<true>(dlogits + t * ld_d + at, n_experts - at, o);
+            for (int i = 0; i < M; ++i) o[i] = slope(l[i], g[w][at + i]);
+            store_n<M>(dlogits + t * ld_d + at, o);
         }
     } else {
         for (int i = lane; i < n_experts; i += 64) store1(dlogits + t * ld_d + i, slope(renorm ? 0.f : load1(row + i), g[w][i]));
