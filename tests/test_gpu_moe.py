@@ -165,8 +165,8 @@ def wild(rows, cols, seed):
     x = torch.randn(rows, cols, generator=gen(seed)) * torch.exp(4 * torch.randn(rows, 1, generator=gen(seed + 1)))
     f = x.view(-1)
     n = f.numel()
-    for v in (math.inf, -math.inf, math.nan, 0.0, -0.0, 1e-42, 3e38, -1e-30):
-        f[int(torch.randint(0, n, (1,), generator=gen(seed + int(abs(hash(str(v))) % 97))))] = v
+    for i, v in enumerate((math.inf, -math.inf, math.nan, 0.0, -0.0, 1e-42, 3e38, -1e-30)):
+        f[int(torch.randint(0, n, (1,), generator=gen(seed + 7 * i + 2)))] = v
     if rows > 2:
         x[1, :130] = 0
         x[2] = 1e-40
