@@ -910,6 +910,10 @@ __device__ __forceinline__ int count_tiles(const int32_t* group_rows, int groups
 // The large form: a tile of BM x BN, WM x WN waves, blocks of 128 in turn through two halves of the LDS: while one is multiplied the next
 // one is on its way.  A row's sixteens lie in the LDS at their place xor (row / 2 mod 8), and a lane reads numbers part and part + 4: the
 // sixteen lanes that the LDS serves together then meet every bank once; the lanes load them in that order.
+// No conflicts are counted.  256 x 256, 16384 x 8192 x 8192: 919 to 959 us by machine, 2.3 to 2.4 PFLOP/s, the matrix cores at work 51 % of the
+// time: between two blocks all waves wait for the barrier and then for the same LDS.  64 groups of 256 rows, 3584 x 4096: 378 to 396 us, of which
+// the weights alone take 235 to read.  128 x 128 by columns to 32 bits, 12005 x 2736 x 2048: 191 us, 0.7 PFLOP/s, bound by the widening and
+// scaling.  Four waves of 128 x 128 in place of eight of 128 x 64 took 995 us for the first.
 template <int KIND, bool COLS, class OUT, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(Product P, int m_tiles, int n_tiles) {
     constexpr int W = WM * WN, MT = BM / (16 * WM), NT = BN / (16 * WN), LA = BM / 8 / W, LB = BN / 8 / W;
