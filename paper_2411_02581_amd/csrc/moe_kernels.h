@@ -521,11 +521,20 @@ __device__ __forceinline__ float max16(float v) {                 // over 16 nei
     return v;
 }
 
-// 1 / (1 + exp(-g)); the division is one approximate reciprocal and a step of Newton's, exact to a unit of the last place.
-__device__ __forceinline__ float silu_gate(float g) {
-    const float d = 1.f + exp_32(-g > 87.f ? 87.f : -g);
+// The sigmoid of g and silu(g) = g sigmoid(g).  1 / (1 + exp(-g)) is one approximate reciprocal and a step of Newton's, exact to a unit of the last
+// place.  Below -87, where exp(-g) would leave the range, the sigmoid is exp(g) (the 1 is far below its last place), taken as exp(g + 44) exp(-44):
+// the sum is exact, and the product with exp(-44) comes last, so that it alone goes below the normal numbers, down to 0.  A sigmoid that
+// stopped at some small value would leave a large negative gate something of itself.
+struct Gate { float sigmoid, silu; };
+__device__ __forceinline__ Gate gate_of(float g) {
+    const bool low = g < -87.f;
+    const float e = exp_32(low ? g + 44.f : -g), d = 1.f + e;
     const float r = __builtin_amdgcn_rcpf(d);
-    return __builtin_fmaf(__builtin_fmaf(-d, r, 1.f), r, r);
+    Gate t;
+    t.sigmoid = low ? e : __builtin_fmaf(__builtin_fmaf(-d, r, 1.f), r, r);
+    t.silu = g * t.sigmoid;
+    if (low) { t.sigmoid *= 7.78113224e-20f; t.silu *= 7.78113224e-20f; }
+    return t;
 }
 
 // Sixteen lanes per block of 128 values, eight each; two blocks in turn, whose loads are under way together.  Bound by memory: 16384 x 4096 of
@@ -552,7 +561,7 @@ __global__ __launch_bounds__(256) void k_quantise(const T* x, int64_t ldx, unsig
         const int64_t r = row[u], b = block[u], c = b * kBlock + (threadIdx.x & 15) * 8, left = cols - c;
         if (ACT == TUNA_ACT_SWIGLU) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[u][i] = i < left ? v[u][i] * silu_gate(v[u][i]) * up[u][i] : 0.f;
+            for (int i = 0; i < 8; ++i) v[u][i] = i < left ? gate_of(v[u][i]).silu * up[u][i] : 0.f;
         }
         float peak = 0.f;
 #pragma unroll
@@ -704,7 +713,8 @@ __global__ __launch_bounds__(256) void k_swiglu_grad(const T* x, int64_t ldx, co
     load8<WIDE>(dh + r * ld_dh + c, left, d);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float s = silu_gate(g[i]), act = g[i] * s;
+        const Gate t = gate_of(g[i]);
+        const float s = t.sigmoid, act = t.silu;
         const float dg = d[i] * u[i] * s * (1.f + g[i] * (1.f - s));
         u[i] = d[i] * act;
         g[i] = dg;
@@ -1461,7 +1471,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
         auto keep = [&](int i, int64_t f, float x, float y) {     // activation f of token number i of the list
             if (i >= n || f >= F.inner) return;
             const int t = list[i];
-            const float v = x * silu_gate(x) * y;
+            const float v = gate_of(x).silu * y;
             const unsigned short hi = to_bf16(v);
             const int64_t to = (int64_t)(t * F.k + rank_of[t]) * F.ld_h + f;
             F.hi[to] = hi;

@@ -1,0 +1,72 @@
+"""The operators of include/tuna_moe.h on the GPU at the ends of their ranges, against their definitions in 64 bits (moe_plain.py)."""
+import pytest
+import torch
+
+import moe_plain as plain
+import paper_2411_02581_amd as tuna
+from test_gpu_moe import CODE, DEV, EPS, KIND, STORED, TYPES, gen, ok, rounding
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ gates far below zero
+
+GATES = [-80.0, -86.5, -87.0, -87.25, -87.5, -88.0, -88.75, -90.0, -95.0, -100.0, -103.5, -104.0, -110.0, -1e4, -1e30, -1e36, -3e38]
+
+
+def far_gates(dtype, cols):
+    """A row for each gate, so that no other one sets its blocks' scales; the last row's are the type's lowest value."""
+    gate = torch.tensor(GATES + [torch.finfo(TYPES[dtype]).min], dtype=torch.float32)[:, None].expand(-1, cols)
+    up = torch.randn(gate.shape[0], cols, generator=gen(1)) * 4
+    return torch.cat([gate, up], 1).to(TYPES[dtype])
+
+
+@pytest.mark.parametrize("cols", [128, 203])
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gates_far_below_zero(cols, kind, dtype):
+    x = far_gates(dtype, cols)
+    rows = x.shape[0]
+    dh = torch.randn(rows, cols, generator=gen(2)).to(TYPES[dtype])
+    q = torch.zeros(rows, cols, dtype=torch.uint8, device=DEV)
+    s = torch.zeros(rows, plain.blocks(cols), dtype=STORED[kind], device=DEV)
+    g = torch.zeros(rows, 2 * cols, dtype=TYPES[dtype], device=DEV)
+    ok(tuna.tuna_fp8_quantize(x.to(DEV), CODE[dtype], 2 * cols, rows, cols, tuna.TUNA_ACT_SWIGLU, None, 1, rows, q, cols, s, s.shape[1], KIND[kind]))
+    ok(tuna.tuna_moe_swiglu_grad(x.to(DEV), CODE[dtype], 2 * cols, dh.to(DEV), cols, rows, cols, g, 2 * cols))
+    torch.cuda.synchronize()
+    gate, up = x.double().chunk(2, -1)
+    # the sigmoid is a 32-bit value that may be below the smallest normal one: half a step of 2^-149, nothing where it is far below that; the
+    # products with the gate and with up may end there too
+    low = 2.0 ** -149 * ((gate > -110) * gate.abs() + 2) * (1 + up.abs())
+    h = plain.swiglu(x)
+    v = plain.wide(q.cpu(), s.cpu(), kind)
+    sc = plain.scale_values(s.cpu(), kind).repeat_interleave(128, -1)[:, :cols]
+    # half a step of e4m3: 1/16 of the value, or half the smallest step
+    assert bool(((v - h).abs() <= torch.maximum(h.abs() / 16, sc * 2.0 ** -10) * (1 + 64 * EPS) + low).all())
+    peak = torch.nn.functional.pad(h.abs(), (0, -cols % 128)).unflatten(-1, (-1, 128)).amax(-1)
+    assert bool((sc[:, ::128] <= torch.where(peak < 2.0 ** -140, 1.0, (peak / 224).clamp_min(2.0 ** -126) * (1 + 64 * EPS))).all())
+    exact = plain.swiglu_grad(x, dh)
+    d = dh.double().abs()
+    # every factor within a few half ulps of itself, for 1 + gate (1 - sigmoid) does not cancel down here
+    room = 32 * EPS * exact.abs() + torch.cat([low * (1 + d), 2.0 ** -149 * ((gate > -110) * gate.abs() + 2) * (1 + d)], -1)
+    step = 2.0 ** -133 if dtype == "bf16" else 2.0 ** -149       # the output's smallest
+    assert bool(((g.cpu().double() - exact).abs() <= room + rounding(dtype) * exact.abs() + step).all())
+
+
+@pytest.mark.parametrize("tokens", [1, 3])
+def test_few_with_gates_far_below_zero(tokens):
+    """The gate is -1e36 and below in every column, so nothing is left of the layer."""
+    h, f, e, k = 128, 32, 4, 2
+    x = torch.zeros(tokens, h, dtype=torch.bfloat16)
+    x[:, 0], x[:, 1] = -1e30, 1.0
+    w1, w2 = torch.zeros(e, 2 * f, h, dtype=torch.bfloat16), torch.ones(e, h, f, dtype=torch.bfloat16)
+    w1[:, :f, 0] = torch.logspace(6, 8, f).bfloat16()
+    w1[:, f:, 1] = 1.0
+    logits = torch.randn(tokens, e, generator=gen(3))
+    rc, size = tuna.tuna_moe_few_workspace(tokens, h, f, e, k)
+    ok(rc)
+    out, ws = torch.full((tokens, h), 9.0, device=DEV), torch.zeros(size, dtype=torch.uint8, device=DEV)
+    ok(tuna.tuna_moe_few(x.to(DEV), h, tokens, h, logits.to(DEV), tuna.TUNA_F32, e, e, k, 1, w1.to(DEV), None, w2.to(DEV), None, f, tuna.TUNA_BF16, 0, out,
+                         tuna.TUNA_F32, h, ws, size))
+    exact, _ = plain.few(x, logits, k, True, w1.double(), w2.double())
+    assert bool((exact == 0).all()) and bool((out.cpu() == 0).all())
