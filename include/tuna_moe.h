@@ -20,8 +20,8 @@
  *   - `ld...` is the distance between rows in elements of the array (scales: in scales); it is at least the row's length.
  *   - The arguments are checked on the host; TUNA_ERR_ARG, TUNA_ERR_TOO_LARGE or TUNA_ERR_WORKSPACE_TOO_SMALL comes
  *     back before anything is enqueued.  Indices that live on the device (slots, expert numbers, group_rows) are held
- *     inside their arrays by the kernels: a slot or an expert outside its range counts as -1 (absent), group bounds are
- *     clamped to [0, m] and to ascending order.
+ *     inside their arrays by the kernels: a slot or an expert outside its range counts as -1 (absent), a group bound
+ *     counts as the largest of all bounds up to it, inside [0, m], so that groups never overlap.
  *   - Values: TUNA_F32, TUNA_BF16, TUNA_F8 (e4m3, largest 448, no infinity).  Pointers are aligned to their elements;
  *     operands whose rows start on 16 bytes (and have such a distance) run wider loads.
  *   - Sums, softmax statistics and products are accumulated in 32 bits and rounded once, to the type of the output.  The

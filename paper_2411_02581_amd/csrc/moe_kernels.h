@@ -127,7 +127,7 @@ __device__ __forceinline__ int wave_scan(int v, int lane) {       // inclusive
 template <int CTRL> __device__ __forceinline__ unsigned dpp(unsigned old, unsigned v) {
     return (unsigned)__builtin_amdgcn_update_dpp((int)old, (int)v, CTRL, 0xf, 0xf, false);
 }
-__device__ __forceinline__ unsigned wave_max(unsigned v) {
+__device__ __forceinline__ unsigned wave_max_scan(unsigned v) {   // inclusive, in vector registers
     auto more = [&](unsigned o) { v = o > v ? o : v; };
     more(dpp<0x111>(v, v));
     more(dpp<0x112>(v, v));
@@ -135,8 +135,9 @@ __device__ __forceinline__ unsigned wave_max(unsigned v) {
     more(dpp<0x118>(v, v));
     more(dpp<0x142>(v, v));
     more(dpp<0x143>(v, v));
-    return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+    return v;
 }
+__device__ __forceinline__ unsigned wave_max(unsigned v) { return (unsigned)__builtin_amdgcn_readlane((int)wave_max_scan(v), 63); }
 __device__ __forceinline__ float wave_total(float v) {
     auto more = [&](unsigned o) { v += __uint_as_float(o); };
     more(dpp<0x111>(0u, __float_as_uint(v)));
@@ -592,10 +593,19 @@ __global__ __launch_bounds__(256) void k_quantise(const T* x, int64_t ldx, unsig
 // Where a block of 128 rows of the columns' form lies: block `want` of all groups' blocks.
 struct Place { int group; int64_t first, end, block; };           // rows first .. end - 1; block: its number among all
 
-__device__ __forceinline__ void group_bounds(const int32_t* group_rows, int g, int64_t m, int64_t& a, int64_t& b) {
-    a = group_rows[g]; b = group_rows[g + 1];
-    a = a < 0 ? 0 : a > m ? m : a;
-    b = b < a ? a : b > m ? m : b;
+// The groups g0 .. g0 + 63 of `groups`, one a lane: rows a .. b - 1 of [0, m).  A bound counts as the largest of all up to it, so that groups never
+// overlap, and their blocks of n rows are at most ceil(m / n) + groups - 1 whatever the bounds are: what the host has checked room for.  low: the
+// largest bound before g0's groups, then before the next 64's.
+__device__ __forceinline__ int bound_at(const int32_t* group_rows, int i, int64_t m) {
+    const int v = group_rows[i];
+    return v < 0 ? 0 : v > m ? (int)m : v;
+}
+__device__ __forceinline__ void group_bounds(const int32_t* group_rows, int groups, int g0, int64_t m, int& low, int& a, int& b) {
+    const int lane = threadIdx.x & 63, g = g0 + lane;
+    const int top = (int)wave_max_scan(g < groups ? (unsigned)bound_at(group_rows, g + 1, m) : 0u), before = __shfl_up(top, 1);
+    b = top > low ? top : low;
+    a = lane > 0 && before > low ? before : low;
+    low = __builtin_amdgcn_readlane(b, 63);
 }
 
 // The group and the part of it that tile number `want` is, tiles of `size` rows counted group after group; group -1: there is none.
@@ -606,17 +616,18 @@ __device__ __forceinline__ Place find_tile(const int32_t* group_rows, int groups
         return p;
     }
     int64_t done = 0;
+    int low = bound_at(group_rows, 0, m);
     for (int g0 = 0; g0 < groups; g0 += 64) {
-        int64_t a = 0, b = 0;
-        if (g0 + lane < groups) group_bounds(group_rows, g0 + lane, m, a, b);
-        const int n = (int)((b - a + size - 1) / size);
+        int a, b;
+        group_bounds(group_rows, groups, g0, m, low, a, b);
+        const int n = (int)(((int64_t)b - a + size - 1) / size);
         const int inc = wave_scan(n, lane);
         const unsigned long long hit = __ballot(done + inc > want);
         if (hit) {
             const int l = __ffsll((long long)hit) - 1;
             const int64_t before = done + __shfl(inc, l) - __shfl(n, l);
-            const int64_t first = ((int64_t)__shfl((int)a, l)) + (want - before) * size;
-            const int64_t end = (int64_t)__shfl((int)b, l);
+            const int64_t first = (int64_t)__shfl(a, l) + (want - before) * size;
+            const int64_t end = (int64_t)__shfl(b, l);
             Place p = {g0 + l, first, first + size < end ? first + size : end, want};
             return p;
         }
@@ -627,14 +638,15 @@ __device__ __forceinline__ Place find_tile(const int32_t* group_rows, int groups
 }
 
 // The first block of 128 rows of a group in the columns' form, and how many it has.
-__device__ __forceinline__ void group_blocks(const int32_t* group_rows, int g, int64_t m, int64_t& first, int64_t& count) {
+__device__ __forceinline__ void group_blocks(const int32_t* group_rows, int groups, int g, int64_t m, int64_t& first, int64_t& count) {
     const int lane = threadIdx.x & 63;
     if (!group_rows) { first = 0; count = blocks_of(m); return; }
     int64_t done = 0;
+    int low = bound_at(group_rows, 0, m);
     for (int g0 = 0; g0 <= g; g0 += 64) {
-        int64_t a = 0, b = 0;
-        if (g0 + lane <= g) group_bounds(group_rows, g0 + lane, m, a, b);
-        const int n = (int)blocks_of(b - a);
+        int a, b;
+        group_bounds(group_rows, groups, g0, m, low, a, b);
+        const int n = (int)blocks_of((int64_t)b - a);
         const int inc = wave_scan(n, lane);
         const int l = g - g0 < 63 ? g - g0 : 63;
         count = __shfl(n, l);
@@ -823,7 +835,7 @@ __global__ __launch_bounds__(256) void k_product64(Product P) {
         i0 = (int64_t)blockIdx.x * 64;
         i_end = i0 + 64 < P.m ? i0 + 64 : P.m;
         int64_t count;
-        group_blocks(P.group_rows, group, P.k, kb0, count);
+        group_blocks(P.group_rows, P.groups, group, P.k, kb0, count);
         kb1 = kb0 + count;
         length = kb1 * kBlock;
     } else {
@@ -906,11 +918,11 @@ __device__ __forceinline__ int xcd_run(unsigned id, unsigned total) {
 // How many tiles of `size` rows the groups have.
 __device__ __forceinline__ int count_tiles(const int32_t* group_rows, int groups, int64_t m, int size) {
     if (!group_rows) return (int)((m + size - 1) / size);
-    int n = 0;
-    for (int g = threadIdx.x & 63; g < groups; g += 64) {
-        int64_t a, b;
-        group_bounds(group_rows, g, m, a, b);
-        n += (int)((b - a + size - 1) / size);
+    int n = 0, low = bound_at(group_rows, 0, m);
+    for (int g0 = 0; g0 < groups; g0 += 64) {
+        int a, b;
+        group_bounds(group_rows, groups, g0, m, low, a, b);
+        n += (int)(((int64_t)b - a + size - 1) / size);
     }
 #pragma unroll
     for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
@@ -952,7 +964,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(Product P, int m_ti
         i0 = (int64_t)ti * BM;
         i_end = i0 + BM < P.m ? i0 + BM : P.m;
         int64_t count;
-        group_blocks(P.group_rows, group, P.k, kb0, count);
+        group_blocks(P.group_rows, P.groups, group, P.k, kb0, count);
         kb1 = kb0 + count;
     } else {
         const Place pl = find_tile(P.group_rows, P.groups, P.m, BM, ti);

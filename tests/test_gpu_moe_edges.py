@@ -4,7 +4,7 @@ import torch
 
 import moe_plain as plain
 import paper_2411_02581_amd as tuna
-from test_gpu_moe import CODE, DEV, EPS, KIND, STORED, TYPES, gen, ok, rounding
+from test_gpu_moe import CODE, DEV, EPS, KIND, STORED, TYPES, check_product, codes, gen, ok, rounding, some_scales
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +70,84 @@ def test_few_with_gates_far_below_zero(tokens):
                          tuna.TUNA_F32, h, ws, size))
     exact, _ = plain.few(x, logits, k, True, w1.double(), w2.double())
     assert bool((exact == 0).all()) and bool((out.cpu() == 0).all())
+
+
+# ------------------------------------------------------------------------------------------------ group bounds in any order
+
+
+def ascending(bounds, m):
+    """What bounds in any order stand for: each the largest of all up to it, inside [0, m]."""
+    out, low = [], 0
+    for b in bounds:
+        low = max(low, min(max(b, 0), m))
+        out.append(low)
+    return out
+
+
+def mixed(groups, m, seed):
+    """Bounds that rise and fall, some of them outside [0, m]."""
+    rise = torch.linspace(-20, m + 20, groups + 1)
+    return (rise + torch.randn(groups + 1, generator=gen(seed)) * m / 8).int().tolist()
+
+
+FALLING = [([0, 1280, 0, 1280, 0, 1280, 0, 1280, 0], 1280), ([0, 300, 100, 500, -7, 650, 2000000000, 40], 700), ([50, 20, 400], 600), ([-5, 1000, 10, 2000000000], 40),
+           ([700, 0, 300], 700), ([0, 129] * 33 + [0, 128, 257, 300], 400), (mixed(70, 900, 1), 900), (mixed(130, 1500, 2), 1500)]
+
+
+@pytest.mark.parametrize("bounds,m", FALLING)
+@pytest.mark.parametrize("kind,cols", [("f32", 130), ("e8", 256)])
+def test_columns_of_groups_in_any_order(bounds, m, kind, cols):
+    groups, up = len(bounds) - 1, ascending(bounds, m)
+    nb = plain.blocks(m) + groups - 1
+    x = torch.randn(m, cols, generator=gen(4)).bfloat16()
+    want, ws, used = plain.quantise_columns(x, up, kind, nb * 128)
+    assert used <= nb
+    q = torch.full((cols + 1, nb * 128), 0xA5, dtype=torch.uint8, device=DEV)
+    s = torch.full((cols + 1, nb), 7, dtype=STORED[kind], device=DEV)
+    ok(tuna.tuna_fp8_quantize_columns(x.to(DEV), tuna.TUNA_BF16, cols, m, cols, torch.tensor(bounds, dtype=torch.int32, device=DEV), groups, q, nb * 128, s, nb,
+                                      KIND[kind]))
+    torch.cuda.synchronize()
+    assert torch.equal(s[:cols, :used].cpu(), ws[:, :used]) and torch.equal(q[:cols, :used * 128].cpu(), want[:, :used * 128])
+    assert bool((q[:, used * 128:] == 0xA5).all()) and bool((q[cols] == 0xA5).all())
+    assert bool((s[:, used:] == 7).all()) and bool((s[cols] == 7).all())
+
+
+# the simple form, tiles of 128 x 128, few rows a group, tiles of 256 x 256
+@pytest.mark.parametrize("bounds,m,n,k", [(b, m, 40, 100) for b, m in FALLING] + [(b, m, 144, 272) for b, m in FALLING] +
+                         [(mixed(70, 100, 3), 100, 48, 272), (mixed(8, 2560, 5), 2560, 8200, 128)])
+@pytest.mark.parametrize("kind,dtype", [("f32", "f32"), ("e8", "bf16")])
+def test_matmul_of_groups_in_any_order(bounds, m, n, k, kind, dtype):
+    groups, up, nk, nn = len(bounds) - 1, ascending(bounds, m), plain.blocks(k), plain.blocks(n)
+    x, xs = codes(m, k, 1), some_scales((m, nk), kind, 2)
+    w, ws = codes(groups * n, k, 3), some_scales((groups * nn, nk), kind, 4)
+    y = torch.full((m + 1, n), 9.0, dtype=TYPES[dtype], device=DEV)
+    ok(tuna.tuna_fp8_matmul(x.to(DEV), k, xs.to(DEV), nk, w.to(DEV), k, n * k, ws.to(DEV), nk, nn * nk, KIND[kind],
+                            torch.tensor(bounds, dtype=torch.int32, device=DEV), groups, y, CODE[dtype], n, m, n, k))
+    torch.cuda.synchronize()
+    a, b = plain.wide(x, xs, kind), plain.wide(w.view(groups, n, k), ws.view(groups, nn, nk), kind, 128)
+    for g in range(groups):
+        check_product(y[up[g]:up[g + 1]], a[up[g]:up[g + 1]], b[g], dtype, k)
+    assert bool((y[:up[0]] == 9.0).all()) and bool((y[up[-1]:] == 9.0).all())
+
+
+@pytest.mark.parametrize("bounds,m", FALLING)
+@pytest.mark.parametrize("n,k", [(70, 33), (130, 144)])
+@pytest.mark.parametrize("kind,dtype", [("f32", "f32"), ("e8", "bf16")])
+def test_grad_w_of_groups_in_any_order(bounds, m, n, k, kind, dtype):
+    groups, up = len(bounds) - 1, ascending(bounds, m)
+    nb = plain.blocks(m) + groups - 1
+    (q, s, used), (p, t, _) = (plain.quantise_columns(torch.randn(m, c, generator=gen(c)), up, kind, nb * 128) for c in (n, k))
+    for v in (q, p):
+        v[:, used * 128:] = 0x7F                                 # what lies behind the groups' blocks is not read
+    dw = torch.full((groups, n, k + 2), 9.0, dtype=TYPES[dtype], device=DEV)
+    ok(tuna.tuna_fp8_matmul_grad_w(q.to(DEV), nb * 128, s.to(DEV), nb, p.to(DEV), nb * 128, t.to(DEV), nb, KIND[kind],
+                                   torch.tensor(bounds, dtype=torch.int32, device=DEV), groups, dw, CODE[dtype], k + 2, n * (k + 2), m, n, k))
+    torch.cuda.synchronize()
+    at = 0
+    for g in range(groups):
+        c = plain.blocks(up[g + 1] - up[g])
+        part = slice(at * 128, (at + c) * 128)
+        a, b = (plain.wide(v[:, part], z[:, at:at + c], kind) if c else torch.zeros(v.shape[0], 0).double() for v, z in ((q, s), (p, t)))
+        check_product(dw[g, :, :k], a, b, dtype, max(c, 1) * 128)
+        at += c
+    assert bool((dw[:, :, k:] == 9.0).all())
