@@ -22,6 +22,9 @@
  *     back before anything is enqueued.  Indices that live on the device (slots, expert numbers, group_rows) are held
  *     inside their arrays by the kernels: a slot or an expert outside its range counts as -1 (absent), a group bound
  *     counts as the largest of all bounds up to it, inside [0, m], so that groups never overlap.
+ *   - Rows, columns and (token, expert) pairs number at most 2^31 - 1 each.  With b = 2^24 - 1, what a launch has threads for:
+ *     the router and its gradient take 4 b tokens, the sum's gradient b tokens, tuna_fp8_quantize 32 b blocks of 128 values and
+ *     its form by columns b blocks of rows; products of rows off 16 bytes 64 b rows.  More is TUNA_ERR_TOO_LARGE.
  *   - Values: TUNA_F32, TUNA_BF16, TUNA_F8 (e4m3, largest 448, no infinity).  Pointers are aligned to their elements;
  *     operands whose rows start on 16 bytes (and have such a distance) run wider loads.
  *   - Sums, softmax statistics and products are accumulated in 32 bits and rounded once, to the type of the output.  The

@@ -28,6 +28,9 @@ inline int scale_size(int type) { return type == TUNA_SCALE_F32 ? 4 : 1; }
 inline bool rows_ok(const void* p, int size, int64_t ld, int64_t cols) { return p && on(p, size) && ld >= cols; }
 inline bool rows_wide(const void* p, int size, int64_t ld) { return on(p, 16) && (ld * size) % 16 == 0; }
 
+// A grid dimension has at most 2^32 - 1 threads.
+inline bool grid_fits(int64_t blocks, int threads) { return blocks <= 0xffffffffll / threads; }
+
 // A thread for eight neighbours, a row (y and z) at a time.
 inline bool eights_fit(int64_t rows, int64_t cols) { return ceil_div(rows, 32768) <= kMaxGridY && ceil_div(cols, 2048) <= kMaxRows / 256; }
 inline dim3 eights_grid(int64_t rows, int64_t cols) {
@@ -74,6 +77,9 @@ RouteSizes route_sizes(int64_t n, int experts, int k, bool plan) {
     return r;
 }
 
+// What a call takes: pairs are counted in 31 bits, and a wave has a token.
+bool route_fits(int64_t n, int k) { return n <= kMaxRows / k && grid_fits(ceil_div(n, 4), 256); }
+
 bool route_args(int64_t n, int experts, int k) {
     return n >= 0 && experts >= 1 && experts <= TUNA_MOE_MAX_EXPERTS && k >= 1 && k <= TUNA_MOE_MAX_K && k <= experts;
 }
@@ -84,7 +90,7 @@ extern "C" {
 
 int tuna_moe_route_workspace(int64_t n_tokens, int n_experts, int k, int with_plan, size_t* bytes) {
     if (!bytes || !route_args(n_tokens, n_experts, k)) return TUNA_ERR_ARG;
-    if (n_tokens > kMaxRows / k) return TUNA_ERR_TOO_LARGE;
+    if (!route_fits(n_tokens, k)) return TUNA_ERR_TOO_LARGE;
     *bytes = route_sizes(n_tokens, n_experts, k, with_plan != 0).bytes;
     return TUNA_OK;
 }
@@ -101,7 +107,7 @@ int tuna_moe_route(const void* logits, int type, int64_t ld, int64_t n_tokens, i
     if (plan && (!sendcounts || !sdispls || !recvcounts || !rdispls || row_bytes < 1 || !on(sendcounts, 4) || !on(sdispls, 8) || !on(recvcounts, 4) ||
                  !on(rdispls, 8)))
         return TUNA_ERR_ARG;
-    if (n_tokens > kMaxRows / k) return TUNA_ERR_TOO_LARGE;
+    if (!route_fits(n_tokens, k)) return TUNA_ERR_TOO_LARGE;
     const RouteSizes r = route_sizes(n_tokens, n_experts, k, plan);
     // a token has an expert once, so a block of the all-to-all is at most a shard long
     if (plan && row_bytes > kMaxRows / r.shard) return TUNA_ERR_TOO_LARGE;
@@ -132,9 +138,13 @@ int tuna_moe_route(const void* logits, int type, int64_t ld, int64_t n_tokens, i
                             experts, weights);
             });
         });
-    if (small) return launched();
+    // every kernel reads what those before it have written: none is launched behind one that was not
+    int e = launched();
+    if (small || e != TUNA_OK) return e;
     LAUNCH(k_route_count, dim3(r.shards), 256, experts, n_tokens, n_experts, k, r.shard, counts, places);
+    if ((e = launched()) != TUNA_OK) return e;
     LAUNCH(k_route_columns, dim3(n_experts), 256, counts, r.shards, n_experts, before, totals);
+    if ((e = launched()) != TUNA_OK) return e;
     LAUNCH(k_route_place, dim3(r.shards), 256, experts, counts, before, totals, n_tokens, n_experts, k, r.shard, r.shards, places, slots, expert_rows,
            row_bytes, sendcounts, sdispls, recvcounts, rdispls);
     return launched();
@@ -144,7 +154,7 @@ int tuna_moe_route_grad(const void* logits, int type, int64_t ld, int64_t n_toke
                         const int32_t* experts, const float* weights, const float* dweights,
                         void* dlogits, int64_t ld_dlogits, void* stream) {
     if (!route_args(n_tokens, n_experts, k) || !is_float(type) || (flags & ~TUNA_ROUTE_RENORM)) return TUNA_ERR_ARG;
-    if (n_tokens > kMaxRows / k) return TUNA_ERR_TOO_LARGE;
+    if (!route_fits(n_tokens, k)) return TUNA_ERR_TOO_LARGE;
     if (n_tokens == 0) return TUNA_OK;
     if (!rows_ok(logits, size_of(type), ld, n_experts) || !rows_ok(dlogits, size_of(type), ld_dlogits, n_experts) || !experts || !weights || !dweights ||
         !on(experts, 4) || !on(weights, 4) || !on(dweights, 4))
@@ -172,7 +182,7 @@ int tuna_fp8_quantize(const void* x, int type, int64_t ldx, int64_t rows, int64_
     if (copies < 1 || copies > TUNA_MOE_MAX_K || (!slots && (copies != 1 || out_rows < rows)) || (slots && !on(slots, 4))) return TUNA_ERR_ARG;
     if (rows == 0 || cols == 0) return TUNA_OK;
     const int64_t width = act == TUNA_ACT_SWIGLU ? 2 * cols : cols, nb = ceil_div(cols, kBlock);
-    if (cols > kMaxRows || rows > kMaxRows || out_rows > kMaxRows || rows * nb > kMaxRows) return TUNA_ERR_TOO_LARGE;
+    if (cols > kMaxRows || rows > kMaxRows || out_rows > kMaxRows || rows * nb > kMaxRows || !grid_fits(ceil_div(rows * nb, 32), 256)) return TUNA_ERR_TOO_LARGE;
     if (!rows_ok(x, size_of(type), ldx, width)) return TUNA_ERR_ARG;
     if (out_rows > 0 && (!rows_ok(q, 1, ldq, cols) || !rows_ok(scales, scale_size(scale_type), ld_scales, nb))) return TUNA_ERR_ARG;
     if (out_rows == 0) return TUNA_OK;
@@ -205,7 +215,7 @@ int tuna_fp8_quantize_columns(const void* x, int type, int64_t ldx, int64_t rows
     const int64_t nb = ceil_div(rows, kBlock) + groups - 1;
     if (!rows_ok(x, size_of(type), ldx, cols) || !rows_ok(q, 1, ldq, nb * kBlock) || !rows_ok(scales, scale_size(scale_type), ld_scales, nb)) return TUNA_ERR_ARG;
     const int64_t across = ceil_div(cols, kBlock);
-    if (across > kMaxGridY) return TUNA_ERR_TOO_LARGE;
+    if (across > kMaxGridY || !grid_fits(nb, 256)) return TUNA_ERR_TOO_LARGE;
     const int rc = tuna_host::ensure_device();
     if (rc != TUNA_OK) return rc;
     with_type(type, [&](auto* t) {
@@ -255,10 +265,10 @@ template <int BM, int BN, int WM, int WN, int KIND, bool COLS, class OUT> void l
     LAUNCH((k_product<KIND, COLS, OUT, BM, BN, WM, WN>), dim3((unsigned)grid), WM * WN * 64, P, (int)mt, (int)nt);
 }
 
-// Tiles of the large form: offsets inside a tile are 32 bits, tiles are counted in 31.
+// Tiles of the large form: offsets inside a tile are 32 bits, tiles of 128 x 128 have 256 threads.
 bool product_large(const Product& P, bool cols) {
     const int64_t nt = ceil_div(P.n, 128), mt = ceil_div(P.m, 128) + (cols ? 0 : P.groups - 1);
-    return product_wide(P, cols) && P.lda < (1 << 22) && P.ldb < (1 << 22) && P.ld_as < (1 << 20) && P.ld_bs < (1 << 20) && mt * nt + 8 <= kMaxRows / (cols ? P.groups : 1) && P.n > 64;
+    return product_wide(P, cols) && P.lda < (1 << 22) && P.ldb < (1 << 22) && P.ld_as < (1 << 20) && P.ld_bs < (1 << 20) && grid_fits((mt * nt + 8) * (cols ? P.groups : 1), 256) && P.n > 64;
 }
 
 // Whether tiles of 256 x 256 fill the device: with fewer than a tile for each compute unit, or groups that are mostly shorter than one, tiles of
@@ -266,7 +276,8 @@ bool product_large(const Product& P, bool cols) {
 // 4096 rows 63 / 72; 64 groups, 3584 x 4096: 8192 rows 282 / 305, 16384 rows 375 / 427.
 bool product_fills(const Product& P, bool cols) {
     const int64_t tiles = ceil_div(P.m, 256) * ceil_div(P.n, 256) * (cols ? P.groups : 1);
-    return tiles >= 256 && (cols || P.m / P.groups >= 128);
+    const int64_t most = cols ? (tiles / P.groups + 8) * P.groups : (ceil_div(P.m, 256) + P.groups - 1) * ceil_div(P.n, 256) + 8;
+    return tiles >= 256 && (cols || P.m / P.groups >= 128) && grid_fits(most, 512);
 }
 
 // Few rows: each workgroup reads 16 rows of the weights.  4096 x 4096, this form / tiles of 128 x 128: 8 rows 9 / 27 us, 64 rows 16 / 28; 32 groups:
@@ -306,6 +317,7 @@ int launch_product(const Product& P, int kind, bool cols, int out_type, void* st
         return launched();
     }
     const int64_t nt = ceil_div(P.n, 64), mt = cols ? ceil_div(P.m, 64) : ceil_div(P.m, 64) + P.groups - 1;
+    if (!grid_fits(mt, 256)) return TUNA_ERR_TOO_LARGE;
     const dim3 grid((unsigned)mt, (unsigned)nt, cols ? P.groups : 1);
     with_type(out_type, [&](auto* o) {
         using O = Pointee<decltype(o)>;
@@ -397,7 +409,7 @@ int tuna_moe_combine_grad(const void* dout, int out_type, int64_t ld_dout, const
                           void* dy, int64_t ld_dy, float* dweights, void* stream) {
     if (n_tokens < 0 || y_rows < 0 || cols < 0 || k < 1 || k > TUNA_MOE_MAX_K || !is_float(y_type) || !is_float(out_type)) return TUNA_ERR_ARG;
     if (n_tokens == 0) return TUNA_OK;
-    if (n_tokens > kMaxRows / k || y_rows > kMaxRows || cols > kMaxRows) return TUNA_ERR_TOO_LARGE;
+    if (n_tokens > kMaxRows / k || !grid_fits(n_tokens, 256) || y_rows > kMaxRows || cols > kMaxRows) return TUNA_ERR_TOO_LARGE;
     if (!slots || !weights || !dweights || !on(slots, 4) || !on(weights, 4) || !on(dweights, 4)) return TUNA_ERR_ARG;
     if (cols > 0 && !rows_ok(dout, size_of(out_type), ld_dout, cols)) return TUNA_ERR_ARG;
     if (cols > 0 && y_rows > 0 && (!rows_ok(y, size_of(y_type), ldy, cols) || !rows_ok(dy, size_of(y_type), ld_dy, cols))) return TUNA_ERR_ARG;
@@ -463,6 +475,7 @@ int tuna_moe_few(const void* x, int64_t ldx, int64_t n_tokens, int64_t hidden, c
     const bool one = n_tokens == 1, split = one || (int64_t)pairs * ceil_div(inner, 64) < 1024;
     const dim3 g1((unsigned)ceil_div(inner, split ? 16 : 16 * kFewFirst), (unsigned)(one ? k : n_experts)), g2((unsigned)ceil_div(hidden, 16));
     const size_t sums = (size_t)kFewSecond * n_tokens * 16 * 4;
+    int e = TUNA_OK;
     with_bool(wide, [&](auto wd) {
         auto both = [&](auto* wp, auto kind) {
             using W = Pointee<decltype(wp)>;
@@ -473,6 +486,7 @@ int tuna_moe_few(const void* x, int64_t ldx, int64_t n_tokens, int64_t hidden, c
                 else if (pairs <= (size_t)n_experts * 8) LAUNCH((k_few_first<L, W, kind.value, wd.value != 0, 1, false, false>), g1, 256, F);
                 else LAUNCH((k_few_first<L, W, kind.value, wd.value != 0, 2, false, false>), g1, 256, F);
             });
+            if ((e = launched()) != TUNA_OK) return;              // the second kernel reads what the first has written
             with_type(out_type, [&](auto* o) {
                 using O = Pointee<decltype(o)>;
                 if (one) hipLaunchKernelGGL((k_few_second<W, kind.value, wd.value != 0, O, true>), g2, dim3(kFewSecond * 64), sums, (hipStream_t)stream, F);
@@ -483,7 +497,7 @@ int tuna_moe_few(const void* x, int64_t ldx, int64_t n_tokens, int64_t hidden, c
         else if (scale_type == TUNA_SCALE_E8) both((uint8_t*)nullptr, Int<TUNA_SCALE_E8>{});
         else both((uint8_t*)nullptr, Int<TUNA_SCALE_F32>{});
     });
-    return launched();
+    return e != TUNA_OK ? e : launched();
 }
 
 }  // extern "C"
