@@ -78,7 +78,7 @@ int tuna_moe_route(const void* logits, int type, int64_t ld, int64_t n_tokens, i
                    int32_t* experts, float* weights, int32_t* slots, int32_t* expert_rows,
                    int64_t row_bytes, int32_t* sendcounts, int64_t* sdispls, int32_t* recvcounts, int64_t* rdispls,
                    void* workspace, size_t workspace_bytes, void* stream);
-/* HOST only: the workspace of tuna_moe_route, with (1) or without (0) a plan. */
+/* HOST only: the workspace of tuna_moe_route, with (1) or without (0) a plan; what is enough for n_tokens is enough for fewer. */
 int tuna_moe_route_workspace(int64_t n_tokens, int n_experts, int k, int with_plan, size_t* bytes);
 /* The gradient of the weights with respect to the logits (the choice itself has none): dlogits has the logits' type and
  * is written whole, 0 for experts that are not eligible.  `weights` and `experts` as tuna_moe_route left them. */

@@ -68,9 +68,12 @@ RouteSizes route_sizes(int64_t n, int experts, int k, bool plan) {
         r.shard = ceil_div(ceil_div(n > 0 ? n : 1, TUNA_MOE_MAX_EXPERTS), 64) * 64;
         r.shards = (int)(n > 0 ? ceil_div(n, r.shard) : 1);
     }
+    // room for as many shards as any batch of up to this size has, so that its workspace is enough for them: 65536 tokens are 1024 shards, 65537 are 513
+    const int64_t batches = n > 0 ? ceil_div(n, 64) : 1;
+    const int64_t most = plan ? r.shards : batches < TUNA_MOE_MAX_EXPERTS ? batches : TUNA_MOE_MAX_EXPERTS;
     size_t at = 0;
-    r.counts = at; at += align16((size_t)r.shards * experts * 4);
-    r.before = at; at += align16((size_t)r.shards * experts * 4);
+    r.counts = at; at += align16((size_t)most * experts * 4);
+    r.before = at; at += align16((size_t)most * experts * 4);
     r.totals = at; at += align16((size_t)experts * 4);
     r.places = at; at += align16((size_t)n * k * 4);
     r.bytes = at;
