@@ -442,9 +442,25 @@ def tuna_version() -> int:
 # ---------------------------------------------------------------------------------------------------- tuna_moe.h
 
 
-def _rows(a: Any, type_code: Optional[int] = None) -> Optional[int]:
-    """Device address of an array of rows: a tensor whose last axis is dense (the distance of its rows is an argument of
-    the call), or a plain integer address."""
+_value_types: dict = {}      # torch's types for the codes of values and of scales; filled by the first tensor that is looked at
+_scale_types: dict = {}
+
+
+def _fits(a: Any, types: dict, code: int) -> Any:
+    """`a`, whose type has to be one of those that the code stands for.  A code that stands for none is left to the library."""
+    if not _value_types:
+        import torch
+        # 8-bit values and exponents travel as bytes too: the rows of a record are a tensor of bytes
+        _scale_types.update({TUNA_SCALE_F32: (torch.float32,), TUNA_SCALE_E8: (torch.uint8, torch.float8_e8m0fnu)})
+        _value_types.update({TUNA_F32: (torch.float32,), TUNA_BF16: (torch.bfloat16,), TUNA_F8: (torch.float8_e4m3fn, torch.uint8)})
+    if code in types and a.dtype not in types[code]:
+        raise TypeError("tensor dtype %s, expected %s" % (a.dtype, " or ".join(str(t) for t in types[code])))
+    return a
+
+
+def _rows(a: Any, code: int, types: dict = _value_types) -> Optional[int]:
+    """Device address of an array of rows: a tensor of the type that the code names whose last axis is dense (the distance of its
+    rows is an argument of the call), or a plain integer address."""
     if a is None or isinstance(a, int):
         return a
     if not a.is_cuda:
@@ -452,9 +468,16 @@ def _rows(a: Any, type_code: Optional[int] = None) -> Optional[int]:
     steps = a.stride()
     if steps and steps[-1] != 1 and a.shape[-1] > 1:
         raise TypeError("a tensor with a dense last axis expected")
-    if type_code is not None and a.element_size() != (4, 2, 1)[type_code]:
-        raise TypeError("tensor dtype %s does not fit the type named" % a.dtype)
-    return a.data_ptr()
+    return _fits(a, types, code).data_ptr()
+
+
+def _scales(a: Any, scale_type: int) -> Optional[int]:
+    return _rows(a, scale_type, _scale_types)
+
+
+def _dense(a: Any, code: int, types: dict = _value_types) -> Optional[int]:
+    """Device address of a contiguous tensor of the type that the code names, or a plain integer address."""
+    return _ptr(a if a is None or isinstance(a, int) else _fits(a, types, code))
 
 
 def tuna_moe_route(logits, type: int, ld: int, n_tokens: int, n_experts: int, k: int, flags: int, experts, weights, slots, expert_rows,
@@ -482,15 +505,15 @@ def tuna_moe_route_grad(logits, type: int, ld: int, n_tokens: int, n_experts: in
 def tuna_fp8_quantize(x, type: int, ldx: int, rows: int, cols: int, act: int, slots, copies: int, out_rows: int, q, ldq: int,
                       scales, ld_scales: int, scale_type: int, stream=None) -> int:
     import torch
-    return load().tuna_fp8_quantize(_rows(x, type), type, ldx, rows, cols, act, _ptr(slots, torch.int32), copies, out_rows, _rows(q), ldq,
-                                    _rows(scales), ld_scales, scale_type, _stream(stream))
+    return load().tuna_fp8_quantize(_rows(x, type), type, ldx, rows, cols, act, _ptr(slots, torch.int32), copies, out_rows, _rows(q, TUNA_F8), ldq,
+                                    _scales(scales, scale_type), ld_scales, scale_type, _stream(stream))
 
 
 def tuna_fp8_quantize_columns(x, type: int, ldx: int, rows: int, cols: int, group_rows, groups: int, q, ldq: int, scales,
                               ld_scales: int, scale_type: int, stream=None) -> int:
     import torch
-    return load().tuna_fp8_quantize_columns(_rows(x, type), type, ldx, rows, cols, _ptr(group_rows, torch.int32), groups, _rows(q), ldq,
-                                            _rows(scales), ld_scales, scale_type, _stream(stream))
+    return load().tuna_fp8_quantize_columns(_rows(x, type), type, ldx, rows, cols, _ptr(group_rows, torch.int32), groups, _rows(q, TUNA_F8), ldq,
+                                            _scales(scales, scale_type), ld_scales, scale_type, _stream(stream))
 
 
 def tuna_moe_swiglu_grad(x, type: int, ldx: int, dh, ld_dh: int, rows: int, cols: int, dx, ld_dx: int, stream=None) -> int:
@@ -500,15 +523,15 @@ def tuna_moe_swiglu_grad(x, type: int, ldx: int, dh, ld_dh: int, rows: int, cols
 def tuna_fp8_matmul(x, ldx: int, xs, ld_xs: int, w, ldw: int, w_group: int, ws, ld_ws: int, ws_group: int, scale_type: int,
                     group_rows, groups: int, y, y_type: int, ldy: int, m: int, n: int, k: int, stream=None) -> int:
     import torch
-    return load().tuna_fp8_matmul(_rows(x, TUNA_F8), ldx, _rows(xs), ld_xs, _rows(w, TUNA_F8), ldw, w_group, _rows(ws), ld_ws, ws_group,
+    return load().tuna_fp8_matmul(_rows(x, TUNA_F8), ldx, _scales(xs, scale_type), ld_xs, _rows(w, TUNA_F8), ldw, w_group, _scales(ws, scale_type), ld_ws, ws_group,
                                   scale_type, _ptr(group_rows, torch.int32), groups, _rows(y, y_type), y_type, ldy, m, n, k, _stream(stream))
 
 
 def tuna_fp8_matmul_grad_w(dyt, ld_dyt: int, dyt_scales, ld_dyt_scales: int, xt, ld_xt: int, xt_scales, ld_xt_scales: int, scale_type: int,
                            group_rows, groups: int, dw, dw_type: int, ld_dw: int, dw_group: int, m: int, n: int, k: int, stream=None) -> int:
     import torch
-    return load().tuna_fp8_matmul_grad_w(_rows(dyt, TUNA_F8), ld_dyt, _rows(dyt_scales), ld_dyt_scales, _rows(xt, TUNA_F8), ld_xt,
-                                         _rows(xt_scales), ld_xt_scales, scale_type, _ptr(group_rows, torch.int32), groups, _rows(dw, dw_type),
+    return load().tuna_fp8_matmul_grad_w(_rows(dyt, TUNA_F8), ld_dyt, _scales(dyt_scales, scale_type), ld_dyt_scales, _rows(xt, TUNA_F8), ld_xt,
+                                         _scales(xt_scales, scale_type), ld_xt_scales, scale_type, _ptr(group_rows, torch.int32), groups, _rows(dw, dw_type),
                                          dw_type, ld_dw, dw_group, m, n, k, _stream(stream))
 
 
@@ -530,8 +553,9 @@ def tuna_moe_few(x, ldx: int, n_tokens: int, hidden: int, logits, logits_type: i
                  w1, s1, w2, s2, inner: int, weight_type: int, scale_type: int, out, out_type: int, ld_out: int,
                  workspace, workspace_bytes: int, stream=None) -> int:
     return load().tuna_moe_few(_rows(x, TUNA_BF16), ldx, n_tokens, hidden, _rows(logits, logits_type), logits_type, ld_logits, n_experts, k,
-                               flags, _ptr(w1), _ptr(s1), _ptr(w2), _ptr(s2), inner, weight_type, scale_type, _rows(out, out_type),
-                               out_type, ld_out, _ptr(workspace), workspace_bytes, _stream(stream))
+                               flags, _dense(w1, weight_type), _dense(s1, scale_type, _scale_types), _dense(w2, weight_type),
+                               _dense(s2, scale_type, _scale_types), inner, weight_type, scale_type, _rows(out, out_type), out_type, ld_out,
+                               _ptr(workspace), workspace_bytes, _stream(stream))
 
 
 def tuna_moe_few_workspace(n_tokens: int, hidden: int, inner: int, n_experts: int, k: int):
