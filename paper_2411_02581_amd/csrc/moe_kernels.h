@@ -1484,10 +1484,12 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
             if (i >= n || f >= F.inner) return;
             const int t = list[i];
             const float v = gate_of(x).silu * y;
-            const unsigned short hi = to_bf16(v);
+            const bool finite = fabsf(v) < __builtin_inff();
+            unsigned short hi = to_bf16(v);
+            if (finite && (hi & 0x7fff) == 0x7f80) --hi;          // above bf16's largest value: that one, and the rest in the second part
             const int64_t to = (int64_t)(t * F.k + rank_of[t]) * F.ld_h + f;
             F.hi[to] = hi;
-            F.lo[to] = fabsf(v) < __builtin_inff() ? to_bf16(v - bf16_bits(hi)) : (unsigned short)0;
+            F.lo[to] = finite ? to_bf16(v - bf16_bits(hi)) : (unsigned short)0;
         };
 #pragma unroll
         for (int s = 0; s < MT; ++s) {

@@ -151,3 +151,56 @@ def test_grad_w_of_groups_in_any_order(bounds, m, n, k, kind, dtype):
         check_product(dw[g, :, :k], a, b, dtype, max(c, 1) * 128)
         at += c
     assert bool((dw[:, :, k:] == 9.0).all())
+
+
+# ------------------------------------------------------------------------------------------------ activations between the two kernels of the layer for few tokens
+
+
+def few_plain(x, w1, w2, e, k=1, logits=None, out_type="f32"):
+    """The layer with bf16 weights; every token's experts by `logits` (the first one)."""
+    t, h, f = x.shape[0], x.shape[1], w2.shape[2]
+    logits = torch.zeros(t, e) if logits is None else logits
+    rc, size = tuna.tuna_moe_few_workspace(t, h, f, e, k)
+    ok(rc)
+    out, ws = torch.full((t, h), 9.0, dtype=TYPES[out_type], device=DEV), torch.zeros(size, dtype=torch.uint8, device=DEV)
+    ok(tuna.tuna_moe_few(x.to(DEV), h, t, h, logits.to(DEV), tuna.TUNA_F32, e, e, k, 1, w1.to(DEV), None, w2.to(DEV), None, f, tuna.TUNA_BF16, 0, out,
+                         CODE[out_type], h, ws, size))
+    torch.cuda.synchronize()
+    return out.cpu()
+
+
+@pytest.mark.parametrize("tokens", [1, 5])
+def test_few_with_activations_beyond_bf16(tokens):
+    """Finite activations above bf16's largest value: a first part that is rounded to nearest would be infinite."""
+    h, f, e = 128, 16, 2
+    x = torch.zeros(tokens, h, dtype=torch.bfloat16)
+    w1, w2 = torch.zeros(e, 2 * f, h, dtype=torch.bfloat16), torch.zeros(e, h, f, dtype=torch.bfloat16)
+    x[:, 0], x[:, 1], x[:, 2] = torch.finfo(torch.bfloat16).max, 1.5 * 2.0 ** 119, 1.0
+    w1[:, :f, :2] = 1.0                                          # gate: 2^128 - 2^118, which is nearer to 2^128 than to bf16's largest
+    w1[:, f:, 2] = 1.0                                           # up: one, or minus one
+    w1[:, f + 1::2, 2] = -1.0
+    w2[:] = (torch.eye(f).repeat(h // f, 1) * 2.0 ** -100).bfloat16()
+    got = few_plain(x, w1, w2, e).double()
+    exact, _ = plain.few(x, torch.zeros(tokens, e), 1, True, w1.double(), w2.double())
+    assert bool((plain.swiglu(w1[0].double() @ x[0].double()).abs() > float(torch.finfo(torch.bfloat16).max) + 2.0 ** 119).any())
+    assert bool((plain.swiglu(w1[0].double() @ x[0].double()).abs() < float(torch.finfo(torch.float32).max)).all())
+    # two sums of two terms, a product, then 2^-16 of the activation at most
+    assert bool(((got - exact).abs() <= 2.0 ** -15 * exact.abs()).all())
+
+
+@pytest.mark.parametrize("tokens,f", [(1, 48), (5, 48), (30, 2304)])
+def test_few_keeps_sixteen_bits_of_an_activation(tokens, f):
+    """The second product passes single activations through: two parts of eight bits each, 2^-16 of the activation, and what its own sum needs."""
+    h, e = 256, 2
+    x = torch.randn(tokens, h, generator=gen(1)).bfloat16()
+    w1 = (torch.randn(e, 2 * f, h, generator=gen(2)) * 0.1).bfloat16()
+    w2 = torch.zeros(e, h, f, dtype=torch.bfloat16)
+    at = torch.randint(0, f, (h,), generator=gen(3))
+    w2[:, torch.arange(h), at] = 1.0
+    got = few_plain(x, w1, w2, e).double()
+    exact, _ = plain.few(x, torch.zeros(tokens, e), 1, True, w1.double(), w2.double())
+    gate, up = (x.double() @ w1[0].double().t()).chunk(2, -1)
+    size_g, size_u = (x.double().abs() @ w1[0].double().abs().t()).chunk(2, -1)
+    # a product's sum of 256 terms: 128 half ulps of the magnitudes (blocks of 128 in 32 bits); silu has a slope of at most 1.1
+    room = 2.0 ** -16 * exact.abs() + (130 * EPS * (1.1 * size_g * up.abs() + size_u * gate.abs()))[:, at] + 8 * EPS * exact.abs()
+    assert bool(((got - exact).abs() <= room).all())
