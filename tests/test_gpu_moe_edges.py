@@ -204,3 +204,31 @@ def test_few_keeps_sixteen_bits_of_an_activation(tokens, f):
     # a product's sum of 256 terms: 128 half ulps of the magnitudes (blocks of 128 in 32 bits); silu has a slope of at most 1.1
     room = 2.0 ** -16 * exact.abs() + (130 * EPS * (1.1 * size_g * up.abs() + size_u * gate.abs()))[:, at] + 8 * EPS * exact.abs()
     assert bool(((got - exact).abs() <= room).all())
+
+
+# ------------------------------------------------------------------------------------------------ products that cancel
+
+
+@pytest.mark.parametrize("m,n,k", [(20, 48, 256), (130, 144, 384), (70, 33, 200)])
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_matmul_of_large_terms_that_cancel(m, n, k, kind, dtype):
+    """In every eight neighbours two products of 2^17 cancel beside six of about one.  In 32 bits the sum is exact (whole numbers below 2^24); in bf16 it is
+    held to the magnitudes, which is all that is said of it: the small terms of such a sum are lost."""
+    x = torch.randint(-1, 2, (m, k), generator=gen(1)).double()
+    w = torch.randint(-1, 2, (n, k), generator=gen(2)).double()
+    x[:, 0:k - 4:8], w[:, 0:k - 4:8] = 384.0, 352.0
+    x[:, 3:k - 4:8], w[:, 3:k - 4:8] = -384.0, 352.0
+    one = (lambda *s: torch.ones(*s, device=DEV)) if kind == "f32" else (lambda *s: torch.full(s, 127, dtype=torch.uint8, device=DEV))
+    nk = plain.blocks(k)
+    y = torch.full((m, n), 9.0, dtype=TYPES[dtype], device=DEV)
+    ok(tuna.tuna_fp8_matmul(plain.to_e4m3(x).to(DEV), k, one(m, nk), nk, plain.to_e4m3(w).to(DEV), k, 0, one(plain.blocks(n), nk), nk, 0, KIND[kind], None, 1, y,
+                            CODE[dtype], n, m, n, k))
+    torch.cuda.synchronize()
+    exact = x @ w.t()
+    assert float(exact.abs().max()) < 2 ** 8
+    if dtype == "f32":
+        assert torch.equal(y.cpu().double(), exact)
+    check_product(y, x, w, dtype, k)
+    # what the header says: 2^-10 of the magnitudes, and the output's rounding
+    assert bool(((y.cpu().double() - exact).abs() <= 2.0 ** -10 * (x.abs() @ w.abs().t()) + rounding(dtype) * exact.abs()).all())
