@@ -446,16 +446,15 @@ _value_types: dict = {}      # torch's types for the codes of values and of scal
 _scale_types: dict = {}
 
 
-def _fits(a: Any, types: dict, code: int) -> Any:
-    """`a`, whose type has to be one of those that the code stands for.  A code that stands for none is left to the library."""
+def _misfit(a: Any, code: int, types: dict) -> None:
+    """A tensor whose type is not among those of the code: there is no such code, and the library says so, or an error."""
     if not _value_types:
         import torch
         # 8-bit values and exponents travel as bytes too: the rows of a record are a tensor of bytes
         _scale_types.update({TUNA_SCALE_F32: (torch.float32,), TUNA_SCALE_E8: (torch.uint8, torch.float8_e8m0fnu)})
         _value_types.update({TUNA_F32: (torch.float32,), TUNA_BF16: (torch.bfloat16,), TUNA_F8: (torch.float8_e4m3fn, torch.uint8)})
-    if code in types and a.dtype not in types[code]:
+    if a.dtype not in types.get(code, (a.dtype,)):
         raise TypeError("tensor dtype %s, expected %s" % (a.dtype, " or ".join(str(t) for t in types[code])))
-    return a
 
 
 def _rows(a: Any, code: int, types: dict = _value_types) -> Optional[int]:
@@ -465,10 +464,11 @@ def _rows(a: Any, code: int, types: dict = _value_types) -> Optional[int]:
         return a
     if not a.is_cuda:
         raise TypeError("device tensor expected")
-    steps = a.stride()
-    if steps and steps[-1] != 1 and a.shape[-1] > 1:
+    if not a.is_contiguous() and a.stride()[-1] != 1 and a.shape[-1] > 1:
         raise TypeError("a tensor with a dense last axis expected")
-    return _fits(a, types, code).data_ptr()
+    if a.dtype not in types.get(code, ()):
+        _misfit(a, code, types)
+    return a.data_ptr()
 
 
 def _scales(a: Any, scale_type: int) -> Optional[int]:
@@ -477,7 +477,9 @@ def _scales(a: Any, scale_type: int) -> Optional[int]:
 
 def _dense(a: Any, code: int, types: dict = _value_types) -> Optional[int]:
     """Device address of a contiguous tensor of the type that the code names, or a plain integer address."""
-    return _ptr(a if a is None or isinstance(a, int) else _fits(a, types, code))
+    if a is not None and not isinstance(a, int) and a.dtype not in types.get(code, ()):
+        _misfit(a, code, types)
+    return _ptr(a)
 
 
 def tuna_moe_route(logits, type: int, ld: int, n_tokens: int, n_experts: int, k: int, flags: int, experts, weights, slots, expert_rows,

@@ -83,3 +83,17 @@ def test_index_and_weight_arrays():
             else:
                 with pytest.raises(TypeError):
                     tuna.tuna_moe_route_grad(*a, stream=0)
+
+
+def test_the_last_axis_is_dense_and_the_rows_may_lie_apart():
+    def with_steps(shape, steps):
+        v = Tensor(BF16)
+        v.shape, v.stride, v.is_contiguous = shape, lambda: steps, lambda: False
+        return v
+
+    call = lambda v: tuna.tuna_moe_swiglu_grad(v, 1, 300, A, 128, 0, 128, A, 256, stream=0)  # noqa: E731
+    assert call(with_steps((4, 256), (300, 1))) == tuna.TUNA_OK
+    assert call(with_steps((4, 1), (300, 7))) == tuna.TUNA_OK
+    assert call(with_steps((2, 4, 256), (9000, 300, 1))) == tuna.TUNA_OK
+    with pytest.raises(TypeError):
+        call(with_steps((4, 256), (1, 4)))
