@@ -41,7 +41,7 @@ class ExpertParallel:
 
     def __init__(self, w1, w2, k, max_tokens, experts_per_node=0):
         self.experts, self.hidden, self.inner = w2.shape
-        self.k, self.per_node, dev = k, experts_per_node, w1.device
+        self.k, self.per_node, self.max_tokens, dev = k, experts_per_node, max_tokens, w1.device
         (self.w1, self.s1), (self.w2, self.s2) = quantise_weights(w1), quantise_weights(w2)
         e, h, f, pairs = self.experts, self.hidden, self.inner, max_tokens * k
         self.record = -(-(h + _blocks(h)) // 16) * 16            # values, then scales; rows on 16 bytes
@@ -57,7 +57,16 @@ class ExpertParallel:
         self.mid, self.q, self.qs = new(pairs, 2 * f, dtype=torch.bfloat16), new(pairs, f), new(pairs, _blocks(f))
         self.y, self.back = new(pairs, h, dtype=torch.bfloat16), new(pairs, h, dtype=torch.bfloat16)
 
+    def _check(self, x, logits, most):
+        """The buffers have room for `most` tokens, and the calls name the distances of dense rows."""
+        t = x.shape[0]
+        if t > most or x.shape != (t, self.hidden) or logits.shape != (t, self.experts):
+            raise ValueError("up to %d tokens of %d columns and as many rows of %d logits expected" % (most, self.hidden, self.experts))
+        if x.dtype != torch.bfloat16 or logits.dtype != torch.float32 or not x.is_contiguous() or not logits.is_contiguous():
+            raise ValueError("contiguous bf16 tokens and 32-bit logits expected")
+
     def __call__(self, x, logits):
+        self._check(x, logits, self.max_tokens)
         t, e, h, f, k = x.shape[0], self.experts, self.hidden, self.inner, self.k
         experts, slots = (torch.empty(t, k, dtype=torch.int32, device=x.device) for _ in range(2))
         weights, out, pairs = torch.empty(t, k, device=x.device), torch.empty_like(x), t * k
@@ -81,6 +90,7 @@ class ExpertParallel:
         return out
 
     def step(self, x, logits):
+        self._check(x, logits, min(self.max_tokens, tuna.TUNA_MOE_FEW_TOKENS))
         t, e, h = x.shape[0], self.experts, self.hidden
         out = torch.empty_like(x)
         _ok(tuna.tuna_moe_few(x, h, t, h, logits, tuna.TUNA_F32, e, e, self.k, tuna.TUNA_ROUTE_RENORM, self.w1, self.s1, self.w2, self.s2, self.inner,
