@@ -232,3 +232,21 @@ def test_matmul_of_large_terms_that_cancel(m, n, k, kind, dtype):
     check_product(y, x, w, dtype, k)
     # what the header says: 2^-10 of the magnitudes, and the output's rounding
     assert bool(((y.cpu().double() - exact).abs() <= 2.0 ** -10 * (x.abs() @ w.abs().t()) + rounding(dtype) * exact.abs()).all())
+
+
+# ------------------------------------------------------------------------------------------------ not a number, in every form of the product
+
+
+# few rows, the simple form, tiles of 128 x 128 and of 256 x 256
+@pytest.mark.parametrize("m,n,k", [(20, 144, 256), (70, 130, 200), (70, 130, 256), (300, 272, 272), (4100, 4100, 128)])
+@pytest.mark.parametrize("kind", ["f32", "e8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_not_a_number_stays_in_its_row_and_column(m, n, k, kind, dtype):
+    x, w = codes(m, k, 3), codes(n, k, 4)
+    x[5, 17], w[9, k - 3], x[m - 1, k - 1] = 0x7F, 0xFF, 0x7F
+    nk = plain.blocks(k)
+    one = (lambda *s: torch.ones(*s, device=DEV)) if kind == "f32" else (lambda *s: torch.full(s, 127, dtype=torch.uint8, device=DEV))
+    y = torch.zeros(m, n, dtype=TYPES[dtype], device=DEV)
+    ok(tuna.tuna_fp8_matmul(x.to(DEV), k, one(m, nk), nk, w.to(DEV), k, 0, one(plain.blocks(n), nk), nk, 0, KIND[kind], None, 1, y, CODE[dtype], n, m, n, k))
+    nan = y.cpu().isnan()
+    assert bool(nan[5].all()) and bool(nan[m - 1].all()) and bool(nan[:, 9].all()) and int(nan.sum()) == m + 2 * n - 2
