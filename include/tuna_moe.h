@@ -23,14 +23,18 @@
  *     inside their arrays by the kernels: a slot or an expert outside its range counts as -1 (absent), a group bound
  *     counts as the largest of all bounds up to it, inside [0, m], so that groups never overlap.
  *   - Rows, columns and (token, expert) pairs number at most 2^31 - 1 each.  With b = 2^24 - 1, what a launch has threads for:
- *     the router and its gradient take 4 b tokens, the sum's gradient b tokens, tuna_fp8_quantize 32 b blocks of 128 values and
- *     its form by columns b blocks of rows; products of rows off 16 bytes 64 b rows.  More is TUNA_ERR_TOO_LARGE.
+ *     the router and its gradient take 4 b tokens, the sum's gradient b tokens, tuna_fp8_quantize 32 b blocks of 128 values,
+ *     its form by columns b blocks of rows and 128 * 65535 columns; products of rows off 16 bytes 64 b rows; y has up to
+ *     64 * 65535 columns (dw: its k); the sum and the gate's gradient take 2^31 - 2^15 rows.  More is TUNA_ERR_TOO_LARGE.
  *   - Values: TUNA_F32, TUNA_BF16, TUNA_F8 (e4m3, largest 448, no infinity).  Pointers are aligned to their elements;
  *     operands whose rows start on 16 bytes (and have such a distance) run wider loads.
- *   - Sums, softmax statistics and products are accumulated in 32 bits and rounded once, to the type of the output.  The
- *     products of tuna_fp8_matmul(_grad_w) with an output of TUNA_BF16 run on the 8-bit matrix cores, which add eight
- *     neighbouring products at a time, each cut at 2^-13 of the largest one's power of two (some 1.5e-5 of the result, far
- *     below its rounding); with an output of TUNA_F32 products are exact and sums are in 32 bits, at half the rate.
+ *   - Sums, softmax statistics and products are accumulated in 32 bits and rounded once, to the type of the output, but for two
+ *     places.  (1) The products of tuna_fp8_matmul(_grad_w) with an output of TUNA_BF16 run on the 8-bit matrix cores, which
+ *     add eight neighbouring products at a time, each cut at 2^-13 of the largest one's power of two: off by at most 2^-10 of
+ *     the sum of the products' MAGNITUDES.  Where little cancels that is some 1.5e-5 of the result, below its rounding; where
+ *     large products cancel, the small ones beside them are lost and the result shows it.  With an output of TUNA_F32
+ *     products are exact and sums are in 32 bits, at half the rate: for those who need that.  (2) tuna_moe_few keeps its
+ *     activations between its two kernels as two bf16 parts, 2^-16 of each, for either type of the output.
  *   - Results do not depend on what runs beside the call: there are no floating-point atomics.
  */
 #ifndef TUNA_MOE_H
@@ -149,7 +153,8 @@ int tuna_moe_combine_grad(const void* dout, int out_type, int64_t ld_dout, const
 /*
  * The whole layer for at most TUNA_MOE_FEW_TOKENS tokens, in two kernels, for serving:
  *     out[t] = sum over the chosen experts e: weight(t, e) * w2[e] (silu(gate) * up),   [gate | up] = w1[e] x[t]
- * with the choice and the weights of tuna_moe_route.  Every chosen expert's weights are read once.
+ * with the choice and the weights of tuna_moe_route.  A chosen expert's weights are read once for up to 16 of its tokens, w1 for up
+ * to 32 where the experts have more than 8 pairs on average, and again for as many more.
  *   x  [n_tokens, hidden] TUNA_BF16;  logits [n_tokens, n_experts] TUNA_F32 or TUNA_BF16
  *   w1 [n_experts, 2 inner, hidden], w2 [n_experts, hidden, inner], dense: TUNA_F8 with s1 [n_experts, ceil(2 inner / 128),
  *      ceil(hidden / 128)], s2 [n_experts, ceil(hidden / 128), ceil(inner / 128)], or TUNA_BF16 (s1 = s2 = NULL)

@@ -129,7 +129,9 @@ int tuna_moe_route(const void* logits, int type, int64_t ld, int64_t n_tokens, i
         else if (n_experts <= 512) f(Int<8>{});
         else f(Int<16>{});
     };
-    // up to 64 tokens one workgroup is as fast as the device: what counts is that there is one launch
+    // Up to 64 tokens without a plan: one workgroup, one launch in place of four.  A call, this way / the other: 1 token of 64 experts, k = 4, 8 / 15 us,
+    // 64 tokens 8 / 16; 64 tokens of 256 experts, k = 8, 16 / 17.  Of 1024 experts, k = 16, one workgroup is enough for some 20 tokens: 16 tokens 18 / 22,
+    // 32 tokens 32 / 22, 64 tokens 61 / 24.
     const bool small = !plan && n_tokens > 0 && n_tokens <= 64;
     if (n_tokens > 0)
         with_type(type, [&](auto* t) {
@@ -171,6 +173,8 @@ int tuna_moe_route_grad(const void* logits, int type, int64_t ld, int64_t n_toke
                    flags & TUNA_ROUTE_RENORM ? 1 : 0, experts, weights, dweights, (T*)dlogits, ld_dlogits);
         };
         const bool wide = rows_wide(logits, sizeof(T), ld) && rows_wide(dlogits, sizeof(T), ld_dlogits);
+        // Four logits a lane / eight, 65536 tokens, k = 8: in 32 bits 256 experts 28 / 36 us, 384 46 / 41, 512 50 / 50, 768 74 / 79, 1024 101 / 104; in
+        // bf16 24 / 33, 36 / 34, 40 / 37, 57 / 60, 71 / 62.  Renormalised four are faster throughout: 1024 experts 63 / 72 and 40 / 44.
         if (wide && n_experts <= 256 && n_experts % 4 == 0) go(Int<4>{});
         else if (wide && n_experts % 8 == 0) go(Int<8>{});
         else go(Int<1>{});
@@ -268,7 +272,8 @@ template <int BM, int BN, int WM, int WN, int KIND, bool COLS, class OUT> void l
     LAUNCH((k_product<KIND, COLS, OUT, BM, BN, WM, WN>), dim3((unsigned)grid), WM * WN * 64, P, (int)mt, (int)nt);
 }
 
-// Tiles of the large form: offsets inside a tile are 32 bits, tiles of 128 x 128 have 256 threads.
+// Tiles of the large form: offsets inside a tile are 32 bits, tiles of 128 x 128 have 256 threads.  Up to 64 columns go to the simple form, which is the
+// slower one here too: 2048 rows of 4096, 64 columns 49 us, in tiles of 128 x 128 23.
 bool product_large(const Product& P, bool cols) {
     const int64_t nt = ceil_div(P.n, 128), mt = ceil_div(P.m, 128) + (cols ? 0 : P.groups - 1);
     return product_wide(P, cols) && P.lda < (1 << 22) && P.ldb < (1 << 22) && P.ld_as < (1 << 20) && P.ld_bs < (1 << 20) && grid_fits((mt * nt + 8) * (cols ? P.groups : 1), 256) && P.n > 64;
@@ -311,6 +316,7 @@ int launch_product(const Product& P, int kind, bool cols, int out_type, void* st
             using O = Pointee<decltype(o)>;
             with_bool(kind == TUNA_SCALE_E8, [&](auto sk) {
                 with_bool(cols, [&](auto cl) {
+                    // with 32-bit outputs the widening has no room in the registers of the larger tile: 4096^3 152 us in 128 x 128, 194 in 256 x 256
                     if constexpr (sizeof(O) == 2)
                         if (product_fills(P, cols)) return launch_tiles<256, 256, 2, 4, sk.value, cl.value != 0, O>(P, stream);
                     launch_tiles<128, 128, 2, 2, sk.value, cl.value != 0, O>(P, stream);
@@ -473,9 +479,15 @@ int tuna_moe_few(const void* x, int64_t ldx, int64_t n_tokens, int64_t hidden, c
     F.lo = (unsigned short*)at;
     const bool wide = rows_wide(x, 2, ldx) && on(w1, 16) && on(w2, 16) && (hidden * wsz) % 16 == 0 && (inner * wsz) % 16 == 0 &&
                       hidden <= ((int64_t)1 << 31) / inner / wsz;        // a lane's offset in an expert's half is 32 bits
-    // one token: its k experts' rows alone; else all experts', most of which may have nothing to do.  Few pairs: the waves of a workgroup share
-    // 16 columns, so that there are workgroups enough for the device; many: each wave has 16, and fewer workgroups look for their tokens
+    // One token: its k experts' rows alone; else all experts', most of which may have nothing to do.  Few pairs: the waves of a workgroup share
+    // 16 columns, so that there are workgroups enough for the device; many: each wave has 16, and fewer workgroups look for their tokens.
+    // Calls, shared / each 16: 8-bit weights, k = 4 of 64 experts, 1024 x 2048: 3 tokens 45 / 52 us, 4 54 / 56, 8 97 / 80, 12 120 / 95, 16 135 / 100;
+    // bf16: 4 tokens 76 / 88, 8 123 / 126, 16 169 / 155.  k = 8 of 128, 1536 x 4096: 2 tokens 130 / 114, 5 245 / 216, 24 640 / 530, 40 755 / 580.
+    // k = 2 of 8, 1536 x 4096: 16 tokens 59 / 72.  What counts is how many experts have a token times their columns: the limit here is the pairs'.
     const bool one = n_tokens == 1, split = one || (int64_t)pairs * ceil_div(inner, 64) < 1024;
+    // Up to 8 pairs an expert 16 tokens at a time, else 32 (fewer waves have room).  16 / 32, 8-bit weights, 64 tokens, 1024 x 2048: k = 2 of 8 experts
+    // 82 / 69 us, k = 2 of 16 65 / 65, k = 4 of 16 104 / 91, k = 4 of 32 109 / 109, k = 4 of 64 184 / 177; 16 tokens, k = 4 of 64, 101 / 126;
+    // k = 8 of 128, 1536 x 4096: 24 tokens 530 / 597, 40 tokens 584 / 667, 64 tokens 644 / 718.
     const dim3 g1((unsigned)ceil_div(inner, split ? 16 : 16 * kFewFirst), (unsigned)(one ? k : n_experts)), g2((unsigned)ceil_div(hidden, 16));
     const size_t sums = (size_t)kFewSecond * n_tokens * 16 * 4;
     int e = TUNA_OK;
