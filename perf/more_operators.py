@@ -288,7 +288,7 @@ def plain_balance(s, c):
     counts = torch.bincount(pairs.view(-1), minlength=n * e + 1)[:n * e].view(n, e)
     there = (p.sum(-1) > 0).long()
     tokens = torch.bincount(sequence, weights=there.double(), minlength=n).long()
-    total = torch.zeros(n, e, dtype=torch.float64, device=DEVICE).index_add_(0, sequence, p.double())
+    total = (sequence == torch.arange(n, device=DEVICE)[:, None]).double() @ p.double()
     shares = total / tokens.clamp_min(1)[:, None]
     every = counts.sum(-1).clamp_min(1)
     loss = e * (counts * shares).sum(-1) / every
@@ -474,24 +474,29 @@ def exact_balance(s, c):
     return dict(out, dlogits=dl) if c["train"] else out
 
 
+def _power(e):
+    """2^e in 64 bits, made from its bits."""
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
 def _exact_again(x):
     """x rounded to e2m1 in blocks of 32 with a power of two for each, in 64 bits."""
     n = x.shape[-1]
     x = torch.nn.functional.pad(x.double(), (0, -n % BLOCK)).unflatten(-1, (-1, BLOCK))
     m, e = torch.frexp(x.abs().amax(-1, keepdim=True) / 6)
-    power = torch.ldexp(torch.ones_like(m), torch.where(m == 0.5, e - 1, e).clamp_min(-126))
-    x = x / torch.where(m == 0, 1.0, power)
-    step = torch.ldexp(torch.full_like(x, 0.5), (torch.frexp(x)[1] - 1).clamp_min(0))          # between neighbours, by the power of two below
-    return (torch.round(x / step) * step * torch.where(m == 0, 1.0, power)).flatten(-2)[..., :n]
+    power = _power(torch.where(m == 0, 0, torch.where(m == 0.5, e - 1, e).clamp_min(-126)))
+    x = x / power
+    step = _power((torch.frexp(x)[1] - 1).clamp_min(0) - 1)      # between neighbours, by the power of two below
+    return (torch.round(x / step) * step * power).flatten(-2)[..., :n]
 
 
 def _exact_wide(q, s, n):
     code = torch.stack([q % 16, q // 16], -1).flatten(-2)[..., :n].double()
     sign, low = 1 - 2 * torch.floor(code / 8), code % 8
     e, m = torch.floor(low / 2), low % 2
-    v = sign * torch.where(e == 0, m / 2, (1 + m / 2) * torch.exp2(e - 1))
+    v = sign * torch.where(e == 0, m / 2, (1 + m / 2) * _power(e - 1))
     at = torch.arange(n, device=q.device) // BLOCK
-    return v * torch.exp2(s.double() - 127)[..., at]
+    return v * _power(s.int() - 127)[..., at]
 
 
 def exact_pack(s, c):
