@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtuna.so")
 SOURCES = [os.path.join(CSRC, "tuna_api.hip"), os.path.join(CSRC, "moe_api.hip")]
 HEADERS = [os.path.join(CSRC, "tuna_kernels.h"), os.path.join(CSRC, "tuna_plan.h"),
-           os.path.join(CSRC, "moe_kernels.h"),
+           os.path.join(CSRC, "moe_common.h"), os.path.join(CSRC, "moe_host.h"), os.path.join(CSRC, "moe_kernels.h"),
            os.path.join(os.path.dirname(HERE), "include", "tuna.h"), os.path.join(os.path.dirname(HERE), "include", "tuna_moe.h")]
 
 

@@ -2,182 +2,12 @@
 // over a token's experts, and the whole layer for a few tokens.  Times in these comments are averages over a kernel trace; where one is given in brackets
 // it is the least of the trace.
 #pragma once
-#include <hip/hip_runtime.h>
-#include <stdint.h>
-#include "tuna_moe.h"
+#include "moe_common.h"
 
 namespace moe {
 
-typedef float v4f __attribute__((ext_vector_type(4)));
-typedef int v8i __attribute__((ext_vector_type(8)));
-typedef unsigned v4u __attribute__((ext_vector_type(4)));
-typedef unsigned v2u __attribute__((ext_vector_type(2)));
-typedef __bf16 v8b __attribute__((ext_vector_type(8)));
-typedef __bf16 v2b __attribute__((ext_vector_type(2)));
-
-constexpr int kBlock = 128;            // values that share a scale
-template <int V> struct Int { static constexpr int value = V; };
-constexpr int kLanes = 64;
-
-__device__ __forceinline__ int64_t blocks_of(int64_t n) { return (n + kBlock - 1) / kBlock; }
-
-// ------------------------------------------------------------------------------------------------ values
-
-__device__ __forceinline__ float bf16_bits(unsigned short b) { return __uint_as_float((unsigned)b << 16); }
-__device__ __forceinline__ unsigned short to_bf16(float v) {      // to nearest, ties to even; NaN stays NaN
-    const __bf16 h = (__bf16)v;
-    unsigned short b;
-    __builtin_memcpy(&b, &h, 2);
-    return b;
-}
-
-template <class T> __device__ __forceinline__ float load1(const T* p);
-template <> __device__ __forceinline__ float load1<float>(const float* p) { return *p; }
-template <> __device__ __forceinline__ float load1<unsigned short>(const unsigned short* p) { return bf16_bits(*p); }
-__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store1(unsigned short* p, float v) { *p = to_bf16(v); }
-
-// Eight neighbours, of which `left` are inside the row (the others read as 0 and are not stored).  WIDE: the address is on 16 bytes.
-template <bool WIDE> __device__ __forceinline__ void load8(const float* p, int64_t left, float (&v)[8]) {
-    if (WIDE && left >= 8) {
-        const v4f a = *(const v4f*)p, b = *(const v4f*)(p + 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.f;
-}
-template <bool WIDE> __device__ __forceinline__ void load8(const unsigned short* p, int64_t left, float (&v)[8]) {
-    if (WIDE && left >= 8) {
-        const v4u a = *(const v4u*)p;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(a[i] << 16);
-            v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? bf16_bits(p[i]) : 0.f;
-}
-template <bool WIDE> __device__ __forceinline__ void store8(float* p, int64_t left, const float (&v)[8]) {
-    if (WIDE && left >= 8) {
-        *(v4f*)p = v4f{v[0], v[1], v[2], v[3]};
-        *(v4f*)(p + 4) = v4f{v[4], v[5], v[6], v[7]};
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) if (i < left) p[i] = v[i];
-}
-template <bool WIDE> __device__ __forceinline__ void store8(unsigned short* p, int64_t left, const float (&v)[8]) {
-    if (WIDE && left >= 8) {
-        v4u a;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = (unsigned)to_bf16(v[2 * i]) | (unsigned)to_bf16(v[2 * i + 1]) << 16;
-        *(v4u*)p = a;
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) if (i < left) p[i] = to_bf16(v[i]);
-}
-
-// Eight 16-bit values of which `left` exist, as they lie; zeros behind them.
-template <bool WIDE> __device__ __forceinline__ v4u bits8(const unsigned short* p, int64_t left) {
-    v4u a = {0u, 0u, 0u, 0u};
-    if (WIDE && left >= 8) return *(const v4u*)p;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < left) a[i >> 1] |= (unsigned)p[i] << (16 * (i & 1));
-    return a;
-}
-
-// Sixteen 8-bit values of which `left` exist; zeros behind them.  WIDE: on 16 bytes, and rows of whole sixteens.
-template <bool WIDE> __device__ __forceinline__ v4u chunk16(const uint8_t* p, int64_t left) {
-    v4u a = {0u, 0u, 0u, 0u};
-    if (left <= 0) return a;
-    if (WIDE) return *(const v4u*)p;
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if (i < left) a[i >> 2] |= (unsigned)p[i] << (8 * (i & 3));
-    return a;
-}
-
-// ------------------------------------------------------------------------------------------------ moves between lanes
-
-// What a wave's lanes have written to the LDS is there for its other lanes.
-__device__ __forceinline__ void wave_lds_done() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-    return v;
-}
-__device__ __forceinline__ int wave_scan(int v, int lane) {       // inclusive
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
-    return v;
-}
-
-// The largest, and the sum, of a wave's 64 values, as scalars: shifts within rows of 16 lanes, then from row to row.
-template <int CTRL> __device__ __forceinline__ unsigned dpp(unsigned old, unsigned v) {
-    return (unsigned)__builtin_amdgcn_update_dpp((int)old, (int)v, CTRL, 0xf, 0xf, false);
-}
-__device__ __forceinline__ unsigned wave_max_scan(unsigned v) {   // inclusive, in vector registers
-    auto more = [&](unsigned o) { v = o > v ? o : v; };
-    more(dpp<0x111>(v, v));
-    more(dpp<0x112>(v, v));
-    more(dpp<0x114>(v, v));
-    more(dpp<0x118>(v, v));
-    more(dpp<0x142>(v, v));
-    more(dpp<0x143>(v, v));
-    return v;
-}
-__device__ __forceinline__ unsigned wave_max(unsigned v) { return (unsigned)__builtin_amdgcn_readlane((int)wave_max_scan(v), 63); }
-__device__ __forceinline__ float wave_total(float v) {
-    auto more = [&](unsigned o) { v += __uint_as_float(o); };
-    more(dpp<0x111>(0u, __float_as_uint(v)));
-    more(dpp<0x112>(0u, __float_as_uint(v)));
-    more(dpp<0x114>(0u, __float_as_uint(v)));
-    more(dpp<0x118>(0u, __float_as_uint(v)));
-    more((unsigned)__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
-    more((unsigned)__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x143, 0xc, 0xf, false));
-    return __uint_as_float((unsigned)__builtin_amdgcn_readlane(__float_as_int(v), 63));
-}
-
-// exp(x) for x <= 88 within two units of the last place: 2^(x log2 e), with what the product rounds away put back.
-__device__ __forceinline__ float exp_32(float x) {
-    constexpr float kLog2e = 1.44269504088896341f, kRest = 1.9259629911266175e-08f, kLn2 = 0.693147180559945309f;
-    const float t = x * kLog2e;
-    const float rest = __builtin_fmaf(x, kRest, __builtin_fmaf(x, kLog2e, -t));
-    const float e = __builtin_amdgcn_exp2f(t);
-    return t > -150.f ? __builtin_fmaf(e, rest * kLn2, e) : 0.f;
-}
-
 // ------------------------------------------------------------------------------------------------ routing
 //
-// A logit as a key whose order is the logits' (ties by index come from the index below it); 0 = not eligible.
-__device__ __forceinline__ unsigned logit_key(float v) {
-    v += 0.0f;                                                    // -0 and +0 are equal
-    const unsigned b = __float_as_uint(v);
-    if (v != v || b == 0xff800000u) return 0u;
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-
-__device__ __forceinline__ float key_logit(unsigned key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
-
-// exp(l - top) for eligible logits; where the largest is +inf, only those at +inf have a share.
-__device__ __forceinline__ float exp_share(float l, float top) {
-    if (logit_key(l) == 0u) return 0.f;
-    if (top == __builtin_inff()) return l == top ? 1.f : 0.f;
-    return exp_32(l - top);
-}
-
 // One wave per token: lane i holds the logits i, i + 64, ...; k rounds take the largest key each.  The largest of the wave and where it is
 // are scalars: a round is some thirty vector instructions, a ballot for each register and scalar work beside it.  65536 x 256 in 32 bits, k = 8:
 // 51 us, bound by these instructions (the logits alone take 15 us to read).
@@ -479,11 +309,6 @@ template <int KIND> __device__ __forceinline__ Scale scale_of(float peak) {
     return s;
 }
 
-__device__ __forceinline__ float finite_abs(float v) {
-    const float a = fabsf(v);
-    return a < __builtin_inff() ? a : 0.f;                        // NaN too
-}
-
 // v / scale, rounded once.  A power of two: a product.  Else the product with the rounded inverse and one correction by what it leaves,
 // which gives the rounded quotient (Markstein) as long as that remainder does not underflow: below 2^-90 it divides.
 template <int KIND> __device__ __forceinline__ float scaled(float v, const Scale& s) {
@@ -521,22 +346,6 @@ __device__ __forceinline__ float max16(float v) {                 // over 16 nei
 #pragma unroll
     for (int d = 8; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
     return v;
-}
-
-// The sigmoid of g and silu(g) = g sigmoid(g).  1 / (1 + exp(-g)) is one approximate reciprocal and a step of Newton's, exact to a unit of the last
-// place.  Below -87, where exp(-g) would leave the range, the sigmoid is exp(g) (the 1 is far below its last place), taken as exp(g + 44) exp(-44):
-// the sum is exact, and the product with exp(-44) comes last, so that it alone goes below the normal numbers, down to 0.  A sigmoid that
-// stopped at some small value would leave a large negative gate something of itself.
-struct Gate { float sigmoid, silu; };
-__device__ __forceinline__ Gate gate_of(float g) {
-    const bool low = g < -87.f;
-    const float e = exp_32(low ? g + 44.f : -g), d = 1.f + e;
-    const float r = __builtin_amdgcn_rcpf(d);
-    Gate t;
-    t.sigmoid = low ? e : __builtin_fmaf(__builtin_fmaf(-d, r, 1.f), r, r);
-    t.silu = g * t.sigmoid;
-    if (low) { t.sigmoid *= 7.78113224e-20f; t.silu *= 7.78113224e-20f; }
-    return t;
 }
 
 // Sixteen lanes per block of 128 values, eight each; two blocks in turn, whose loads are under way together.  Bound by memory: 16384 x 4096 of
@@ -589,71 +398,6 @@ __global__ __launch_bounds__(256) void k_quantise(const T* x, int64_t ldx, unsig
             }
         }
     }
-}
-
-// Where a block of 128 rows of the columns' form lies: block `want` of all groups' blocks.
-struct Place { int group; int64_t first, end, block; };           // rows first .. end - 1; block: its number among all
-
-// The groups g0 .. g0 + 63 of `groups`, one a lane: rows a .. b - 1 of [0, m).  A bound counts as the largest of all up to it, so that groups never
-// overlap, and their blocks of n rows are at most ceil(m / n) + groups - 1 whatever the bounds are: what the host has checked room for.  low: the
-// largest bound before g0's groups, then before the next 64's.
-__device__ __forceinline__ int bound_at(const int32_t* group_rows, int i, int64_t m) {
-    const int v = group_rows[i];
-    return v < 0 ? 0 : v > m ? (int)m : v;
-}
-__device__ __forceinline__ void group_bounds(const int32_t* group_rows, int groups, int g0, int64_t m, int& low, int& a, int& b) {
-    const int lane = threadIdx.x & 63, g = g0 + lane;
-    const int top = (int)wave_max_scan(g < groups ? (unsigned)bound_at(group_rows, g + 1, m) : 0u), before = __shfl_up(top, 1);
-    b = top > low ? top : low;
-    a = lane > 0 && before > low ? before : low;
-    low = __builtin_amdgcn_readlane(b, 63);
-}
-
-// The group and the part of it that tile number `want` is, tiles of `size` rows counted group after group; group -1: there is none.
-__device__ __forceinline__ Place find_tile(const int32_t* group_rows, int groups, int64_t m, int size, int64_t want) {
-    const int lane = threadIdx.x & 63;
-    if (!group_rows) {
-        Place p = {want * size < m ? 0 : -1, want * size, want * size + size < m ? want * size + size : m, want};
-        return p;
-    }
-    int64_t done = 0;
-    int low = bound_at(group_rows, 0, m);
-    for (int g0 = 0; g0 < groups; g0 += 64) {
-        int a, b;
-        group_bounds(group_rows, groups, g0, m, low, a, b);
-        const int n = (int)(((int64_t)b - a + size - 1) / size);
-        const int inc = wave_scan(n, lane);
-        const unsigned long long hit = __ballot(done + inc > want);
-        if (hit) {
-            const int l = __ffsll((long long)hit) - 1;
-            const int64_t before = done + __shfl(inc, l) - __shfl(n, l);
-            const int64_t first = (int64_t)__shfl(a, l) + (want - before) * size;
-            const int64_t end = (int64_t)__shfl(b, l);
-            Place p = {g0 + l, first, first + size < end ? first + size : end, want};
-            return p;
-        }
-        done += __shfl(inc, 63);
-    }
-    Place p = {-1, 0, 0, 0};
-    return p;
-}
-
-// The first block of 128 rows of a group in the columns' form, and how many it has.
-__device__ __forceinline__ void group_blocks(const int32_t* group_rows, int groups, int g, int64_t m, int64_t& first, int64_t& count) {
-    const int lane = threadIdx.x & 63;
-    if (!group_rows) { first = 0; count = blocks_of(m); return; }
-    int64_t done = 0;
-    int low = bound_at(group_rows, 0, m);
-    for (int g0 = 0; g0 <= g; g0 += 64) {
-        int a, b;
-        group_bounds(group_rows, groups, g0, m, low, a, b);
-        const int n = (int)blocks_of((int64_t)b - a);
-        const int inc = wave_scan(n, lane);
-        const int l = g - g0 < 63 ? g - g0 : 63;
-        count = __shfl(n, l);
-        done += __shfl(inc, l);
-    }
-    first = done - count;
 }
 
 // Bound by memory and the two passes through the LDS: 12005 x 2048 and x 2736 of bf16 26 and 36 us, 2.9 TB/s.
@@ -736,34 +480,6 @@ __global__ __launch_bounds__(256) void k_swiglu_grad(const T* x, int64_t ldx, co
     store8<WIDE>(dx + r * ld_dx + cols + c, left, u);
 }
 
-// Units lo .. hi - 1: each is fetched AHEAD - 1 units before it is used.  In the loop no load hangs on a condition, so that a wait for one unit's
-// leaves the later ones' under way.  MANY: the loop runs to the end, where it fetches the last unit again; else the end is a loop of its own,
-// which costs registers and spares short runs those loads (one token: both kernels 23.1 us with them, 18.2 without).
-template <int AHEAD, bool MANY, class S, class FETCH, class USE> __device__ __forceinline__ void pipeline(S (&st)[AHEAD], int lo, int hi, FETCH fetch, USE use) {
-    if (MANY && lo >= hi) return;
-#pragma unroll
-    for (int d = 0; d < AHEAD - 1; ++d) if (MANY || lo + d < hi) fetch(st[d], lo + d < hi ? lo + d : hi - 1);
-    int v = lo;
-    for (; MANY ? v < hi : v + 2 * AHEAD - 2 < hi; v += AHEAD) {
-#pragma unroll
-        for (int d = 0; d < AHEAD; ++d) {
-            const int next = v + d + AHEAD - 1;
-            fetch(st[(d + AHEAD - 1) % AHEAD], !MANY || next < hi ? next : hi - 1);
-            __builtin_amdgcn_sched_barrier(0);
-            if (!MANY || v + d < hi) use(st[d], v + d);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    }
-    if (!MANY)
-        for (; v < hi; v += AHEAD) {
-#pragma unroll
-            for (int d = 0; d < AHEAD; ++d) {
-                if (v + d + AHEAD - 1 < hi) fetch(st[(d + AHEAD - 1) % AHEAD], v + d + AHEAD - 1);
-                if (v + d < hi) use(st[d], v + d);
-            }
-        }
-}
-
 // ------------------------------------------------------------------------------------------------ products in 8 bits
 
 // Operands of a product out[i, j] = sum over k of a[i, k] * b[j, k].  Rows a are the activations (or dy transposed), rows b the weights
@@ -805,17 +521,6 @@ __device__ __forceinline__ v4f mma_wide(v8i b, v8i a, v4f c) {
 template <int KIND> __device__ __forceinline__ v4f mma(v8i b, v8i a, v4f c, unsigned sb, unsigned sa) {
     if (KIND == TUNA_SCALE_E8) return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 0, 0, 0, (int)sb, 0, (int)sa);
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 0, 0, 0, 127, 0, 127);
-}
-
-// Up to four neighbours of a row of the result, in one store where all exist and lie on their size.
-template <class OUT> __device__ __forceinline__ void store_four(OUT* o, const v4f& v, int n) {
-    if (n == 4 && ((uintptr_t)o & (4 * sizeof(OUT) - 1)) == 0) {
-        if constexpr (sizeof(OUT) == 2) *(v2u*)o = v2u{(unsigned)to_bf16(v[0]) | (unsigned)to_bf16(v[1]) << 16, (unsigned)to_bf16(v[2]) | (unsigned)to_bf16(v[3]) << 16};
-        else *(v4f*)o = v;
-        return;
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) if (q < n) store1(o + q, v[q]);
 }
 
 // Which matrix cores: the 8-bit ones add eight neighbouring products at a time, each cut at 2^-13 of the largest one's power of two: at most 2^-10 of
@@ -899,36 +604,6 @@ __global__ __launch_bounds__(256) void k_product64(Product P) {
             const int64_t j = j0 + s * 16 + (lane >> 4) * 4 + i;
             if (j < P.n) store1(out + j, acc[s][i]);
         }
-}
-
-// Sixteen bytes a lane (or a scale a lane, as a word) from memory straight into the LDS, lane after lane behind `to`.
-template <int BYTES> __device__ __forceinline__ void to_lds(const void* from, void* to) {
-    const auto* g = (const __attribute__((address_space(1))) void*)from;
-    auto* l = (__attribute__((address_space(3))) void*)to;
-    if constexpr (BYTES == 16) __builtin_amdgcn_global_load_lds(g, l, 16, 0, 0);
-    else if constexpr (BYTES == 4) __builtin_amdgcn_global_load_lds(g, l, 4, 0, 0);
-    else __builtin_amdgcn_global_load_lds(g, l, 1, 0, 0);
-}
-
-// Workgroups go to the eight XCDs in turn: each XCD gets a run of neighbouring tiles, whose operands meet in its L2.  The tile of workgroup `id`
-// among `total`, or -1 (there may be more workgroups than tiles).
-__device__ __forceinline__ int xcd_run(unsigned id, unsigned total) {
-    const unsigned per = total / 8, more = total % 8, x = id % 8, at = id / 8;
-    return at < per + (x < more ? 1 : 0) ? (int)(x * per + (x < more ? x : more) + at) : -1;
-}
-
-// How many tiles of `size` rows the groups have.
-__device__ __forceinline__ int count_tiles(const int32_t* group_rows, int groups, int64_t m, int size) {
-    if (!group_rows) return (int)((m + size - 1) / size);
-    int n = 0, low = bound_at(group_rows, 0, m);
-    for (int g0 = 0; g0 < groups; g0 += 64) {
-        int a, b;
-        group_bounds(group_rows, groups, g0, m, low, a, b);
-        n += (int)(((int64_t)b - a + size - 1) / size);
-    }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
-    return n;
 }
 
 // The large form: a tile of BM x BN, WM x WN waves, blocks of 128 in turn through two halves of the LDS: while one is multiplied the next
