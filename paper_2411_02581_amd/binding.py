@@ -35,10 +35,11 @@ TUNA_T_SLOTS, TUNA_T_EXACT, TUNA_T_AUTO = 0, 1, 2
 TUNA_HOP_ENGINE, TUNA_HOP_TILED, TUNA_HOP_DIRECT, TUNA_HOP_ROWS, TUNA_HOP_LONG = 1, 2, 4, 8, 16
 
 # tuna_moe.h
-TUNA_F32, TUNA_BF16, TUNA_F8 = 0, 1, 2
+TUNA_F32, TUNA_BF16, TUNA_F8, TUNA_F4 = 0, 1, 2, 4
 TUNA_SCALE_F32, TUNA_SCALE_E8 = 0, 1
 TUNA_ACT_NONE, TUNA_ACT_SWIGLU = 0, 1
 TUNA_ROUTE_RENORM = 1
+TUNA_BALANCE_ADD = 1
 TUNA_MOE_MAX_EXPERTS, TUNA_MOE_MAX_K, TUNA_MOE_FEW_TOKENS = 1024, 16, 64
 
 EXPORTS = ("tuna_alltoallv", "tuna_alltoallv_hier", "tuna_alltoallv_noalloc", "tuna_alltoallv_ex", "tuna_alltoallv_init_ex",
@@ -48,7 +49,8 @@ EXPORTS = ("tuna_alltoallv", "tuna_alltoallv_hier", "tuna_alltoallv_noalloc", "t
            "tuna_strerror", "tuna_version")
 MOE_EXPORTS = ("tuna_moe_route", "tuna_moe_route_workspace", "tuna_moe_route_grad", "tuna_fp8_quantize", "tuna_fp8_quantize_columns",
                "tuna_moe_swiglu_grad", "tuna_fp8_matmul", "tuna_fp8_matmul_grad_w", "tuna_moe_combine", "tuna_moe_combine_grad",
-               "tuna_moe_few", "tuna_moe_few_workspace")
+               "tuna_moe_few", "tuna_moe_few_workspace", "tuna_moe_balance", "tuna_moe_balance_workspace", "tuna_moe_balance_grad",
+               "tuna_fp4_quantize", "tuna_fp4_quantize_columns", "tuna_fp4_dequantize", "tuna_fp4_matmul", "tuna_fp4_matmul_grad_w")
 
 
 class tuna_phase_stats_t(ctypes.Structure):
@@ -163,6 +165,14 @@ def load() -> ctypes.CDLL:
     lib.tuna_moe_combine_grad.argtypes = [vp, i, l, vp, i, l, l, vp, vp, l, i, l, vp, l, vp, vp]
     lib.tuna_moe_few.argtypes = [vp, l, l, l, vp, i, l, i, i, i, vp, vp, vp, vp, l, i, i, vp, i, l, vp, sz, vp]
     lib.tuna_moe_few_workspace.argtypes = [l, l, l, i, i, ctypes.POINTER(sz)]
+    lib.tuna_moe_balance.argtypes = [vp, i, l, l, i, vp, i, vp, i, vp, vp, vp, vp, vp, sz, vp]
+    lib.tuna_moe_balance_workspace.argtypes = [l, i, i, ctypes.POINTER(sz)]
+    lib.tuna_moe_balance_grad.argtypes = [vp, i, l, l, i, vp, i, vp, vp, vp, i, vp, l, vp]
+    lib.tuna_fp4_quantize.argtypes = [vp, i, l, l, l, i, vp, i, l, vp, l, vp, l, vp]
+    lib.tuna_fp4_quantize_columns.argtypes = [vp, i, l, l, l, vp, i, vp, l, vp, l, vp]
+    lib.tuna_fp4_dequantize.argtypes = [vp, l, vp, l, l, l, vp, i, l, vp]
+    lib.tuna_fp4_matmul.argtypes = [vp, l, vp, l, vp, l, l, vp, l, l, vp, i, vp, i, l, l, l, l, vp]
+    lib.tuna_fp4_matmul_grad_w.argtypes = [vp, l, vp, l, vp, l, vp, l, vp, i, vp, i, l, l, l, l, l, vp]
     lib.tuna_strerror.argtypes = [i]
     lib.tuna_strerror.restype = ctypes.c_char_p
     lib.tuna_version.argtypes = []
@@ -452,7 +462,8 @@ def _misfit(a: Any, code: int, types: dict) -> None:
         import torch
         # 8-bit values and exponents travel as bytes too: the rows of a record are a tensor of bytes
         _scale_types.update({TUNA_SCALE_F32: (torch.float32,), TUNA_SCALE_E8: (torch.uint8, torch.float8_e8m0fnu)})
-        _value_types.update({TUNA_F32: (torch.float32,), TUNA_BF16: (torch.bfloat16,), TUNA_F8: (torch.float8_e4m3fn, torch.uint8)})
+        _value_types.update({TUNA_F32: (torch.float32,), TUNA_BF16: (torch.bfloat16,), TUNA_F8: (torch.float8_e4m3fn, torch.uint8),
+                             TUNA_F4: (torch.uint8, torch.float4_e2m1fn_x2)})
     if a.dtype not in types.get(code, (a.dtype,)):
         raise TypeError("tensor dtype %s, expected %s" % (a.dtype, " or ".join(str(t) for t in types[code])))
 
@@ -565,3 +576,59 @@ def tuna_moe_few_workspace(n_tokens: int, hidden: int, inner: int, n_experts: in
     out = ctypes.c_size_t(0)
     rc = load().tuna_moe_few_workspace(n_tokens, hidden, inner, n_experts, k, ctypes.byref(out))
     return rc, int(out.value)
+
+
+def tuna_moe_balance(logits, type: int, ld: int, n_tokens: int, n_experts: int, experts, k: int, group_rows, groups: int, counts, tokens, shares, loss,
+                     workspace, workspace_bytes: int, stream=None) -> int:
+    import torch
+    return load().tuna_moe_balance(_rows(logits, type), type, ld, n_tokens, n_experts, _ptr(experts, torch.int32), k, _ptr(group_rows, torch.int32), groups,
+                                   _ptr(counts, torch.int32), _ptr(tokens, torch.int32), _ptr(shares, torch.float32), _ptr(loss, torch.float32),
+                                   _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def tuna_moe_balance_workspace(n_tokens: int, n_experts: int, groups: int):
+    """Returns (code, bytes).  Host only."""
+    out = ctypes.c_size_t(0)
+    rc = load().tuna_moe_balance_workspace(n_tokens, n_experts, groups, ctypes.byref(out))
+    return rc, int(out.value)
+
+
+def tuna_moe_balance_grad(logits, type: int, ld: int, n_tokens: int, n_experts: int, group_rows, groups: int, counts, tokens, dloss, flags: int,
+                          dlogits, ld_dlogits: int, stream=None) -> int:
+    import torch
+    return load().tuna_moe_balance_grad(_rows(logits, type), type, ld, n_tokens, n_experts, _ptr(group_rows, torch.int32), groups, _ptr(counts, torch.int32),
+                                        _ptr(tokens, torch.int32), _ptr(dloss, torch.float32), flags, _rows(dlogits, type), ld_dlogits, _stream(stream))
+
+
+def tuna_fp4_quantize(x, type: int, ldx: int, rows: int, cols: int, act: int, slots, copies: int, out_rows: int, q, ldq: int,
+                      scales, ld_scales: int, stream=None) -> int:
+    import torch
+    return load().tuna_fp4_quantize(_rows(x, type), type, ldx, rows, cols, act, _ptr(slots, torch.int32), copies, out_rows, _rows(q, TUNA_F4), ldq,
+                                    _scales(scales, TUNA_SCALE_E8), ld_scales, _stream(stream))
+
+
+def tuna_fp4_quantize_columns(x, type: int, ldx: int, rows: int, cols: int, group_rows, groups: int, q, ldq: int, scales,
+                              ld_scales: int, stream=None) -> int:
+    import torch
+    return load().tuna_fp4_quantize_columns(_rows(x, type), type, ldx, rows, cols, _ptr(group_rows, torch.int32), groups, _rows(q, TUNA_F4), ldq,
+                                            _scales(scales, TUNA_SCALE_E8), ld_scales, _stream(stream))
+
+
+def tuna_fp4_dequantize(q, ldq: int, scales, ld_scales: int, rows: int, cols: int, x, type: int, ldx: int, stream=None) -> int:
+    return load().tuna_fp4_dequantize(_rows(q, TUNA_F4), ldq, _scales(scales, TUNA_SCALE_E8), ld_scales, rows, cols, _rows(x, type), type, ldx, _stream(stream))
+
+
+def tuna_fp4_matmul(x, ldx: int, xs, ld_xs: int, w, ldw: int, w_group: int, ws, ld_ws: int, ws_group: int, group_rows, groups: int,
+                    y, y_type: int, ldy: int, m: int, n: int, k: int, stream=None) -> int:
+    import torch
+    return load().tuna_fp4_matmul(_rows(x, TUNA_F4), ldx, _scales(xs, TUNA_SCALE_E8), ld_xs, _rows(w, TUNA_F4), ldw, w_group,
+                                  _scales(ws, TUNA_SCALE_E8), ld_ws, ws_group, _ptr(group_rows, torch.int32), groups, _rows(y, y_type), y_type, ldy,
+                                  m, n, k, _stream(stream))
+
+
+def tuna_fp4_matmul_grad_w(dyt, ld_dyt: int, dyt_scales, ld_dyt_scales: int, xt, ld_xt: int, xt_scales, ld_xt_scales: int,
+                           group_rows, groups: int, dw, dw_type: int, ld_dw: int, dw_group: int, m: int, n: int, k: int, stream=None) -> int:
+    import torch
+    return load().tuna_fp4_matmul_grad_w(_rows(dyt, TUNA_F4), ld_dyt, _scales(dyt_scales, TUNA_SCALE_E8), ld_dyt_scales, _rows(xt, TUNA_F4), ld_xt,
+                                         _scales(xt_scales, TUNA_SCALE_E8), ld_xt_scales, _ptr(group_rows, torch.int32), groups, _rows(dw, dw_type),
+                                         dw_type, ld_dw, dw_group, m, n, k, _stream(stream))

@@ -9,9 +9,10 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtuna.so")
-SOURCES = [os.path.join(CSRC, "tuna_api.hip"), os.path.join(CSRC, "moe_api.hip")]
+SOURCES = [os.path.join(CSRC, "tuna_api.hip"), os.path.join(CSRC, "moe_api.hip"), os.path.join(CSRC, "fp4_api.hip"), os.path.join(CSRC, "balance_api.hip")]
 HEADERS = [os.path.join(CSRC, "tuna_kernels.h"), os.path.join(CSRC, "tuna_plan.h"),
            os.path.join(CSRC, "moe_common.h"), os.path.join(CSRC, "moe_host.h"), os.path.join(CSRC, "moe_kernels.h"),
+           os.path.join(CSRC, "fp4_kernels.h"), os.path.join(CSRC, "balance_kernels.h"),
            os.path.join(os.path.dirname(HERE), "include", "tuna.h"), os.path.join(os.path.dirname(HERE), "include", "tuna_moe.h")]
 
 

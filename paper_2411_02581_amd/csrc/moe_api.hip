@@ -406,15 +406,18 @@ int tuna_moe_few(const void* x, int64_t ldx, int64_t n_tokens, int64_t hidden, c
     size_t need;
     const int rw = tuna_moe_few_workspace(n_tokens, hidden, inner, n_experts, k, &need);
     if (rw != TUNA_OK) return rw;
-    if ((flags & ~TUNA_ROUTE_RENORM) || !is_float(logits_type) || !is_float(out_type) || (weight_type != TUNA_F8 && weight_type != TUNA_BF16)) return TUNA_ERR_ARG;
+    if ((flags & ~TUNA_ROUTE_RENORM) || !is_float(logits_type) || !is_float(out_type) || (weight_type != TUNA_F8 && weight_type != TUNA_BF16 && weight_type != TUNA_F4))
+        return TUNA_ERR_ARG;
     if (n_tokens == 0 || hidden == 0) return TUNA_OK;
     const size_t pairs = (size_t)n_tokens * k;
     if (inner < 1 || !rows_ok(x, 2, ldx, hidden) || !rows_ok(logits, size_of(logits_type), ld_logits, n_experts) || !rows_ok(out, size_of(out_type), ld_out, hidden))
         return TUNA_ERR_ARG;
     const int wsz = size_of(weight_type);
     if (!w1 || !w2 || !on(w1, wsz) || !on(w2, wsz)) return TUNA_ERR_ARG;
-    if (weight_type == TUNA_F8 && (!is_scale(scale_type) || !s1 || !s2 || !on(s1, scale_size(scale_type)) || !on(s2, scale_size(scale_type)))) return TUNA_ERR_ARG;
-    if (weight_type != TUNA_F8 && (s1 || s2)) return TUNA_ERR_ARG;
+    const bool scaled = weight_type != TUNA_BF16;
+    if (weight_type == TUNA_F4 && scale_type != TUNA_SCALE_E8) return TUNA_ERR_ARG;
+    if (scaled && (!is_scale(scale_type) || !s1 || !s2 || !on(s1, scale_size(scale_type)) || !on(s2, scale_size(scale_type)))) return TUNA_ERR_ARG;
+    if (!scaled && (s1 || s2)) return TUNA_ERR_ARG;
     if (ldx > (1 << 24) || (int64_t)pairs * (inner + 8) > (1 << 30) || ceil_div(inner, 16) > kMaxRows / 256 || ceil_div(hidden, 16) > kMaxRows / 256) return TUNA_ERR_TOO_LARGE;
     if (!workspace || !on(workspace, 16)) return TUNA_ERR_ARG;
     if (workspace_bytes < need) return TUNA_ERR_WORKSPACE_TOO_SMALL;
@@ -430,8 +433,9 @@ int tuna_moe_few(const void* x, int64_t ldx, int64_t n_tokens, int64_t hidden, c
     F.share = (float*)at; at += align16(pairs * 4);
     F.hi = (unsigned short*)at; at += pairs * F.ld_h * 2;
     F.lo = (unsigned short*)at;
-    const bool wide = rows_wide(x, 2, ldx) && on(w1, 16) && on(w2, 16) && (hidden * wsz) % 16 == 0 && (inner * wsz) % 16 == 0 &&
-                      hidden <= ((int64_t)1 << 31) / inner / wsz;        // a lane's offset in an expert's half is 32 bits
+    const int64_t row1 = weight_type == TUNA_F4 ? ceil_div(hidden, 2) : hidden * wsz, row2 = weight_type == TUNA_F4 ? ceil_div(inner, 2) : inner * wsz;
+    const bool wide = rows_wide(x, 2, ldx) && on(w1, 16) && on(w2, 16) && row1 % 16 == 0 && row2 % 16 == 0 &&
+                      row1 <= ((int64_t)1 << 31) / inner && row2 <= ((int64_t)1 << 31) / hidden;       // a lane's offset in an expert's half is 32 bits
     // One token: its k experts' rows alone; else all experts', most of which may have nothing to do.  Few pairs: the waves of a workgroup share
     // 16 columns, so that there are workgroups enough for the device; many: each wave has 16, and fewer workgroups look for their tokens.
     // Calls, shared / each 16: 8-bit weights, k = 4 of 64 experts, 1024 x 2048: 3 tokens 45 / 52 us, 4 54 / 56, 8 97 / 80, 12 120 / 95, 16 135 / 100;
@@ -462,6 +466,7 @@ int tuna_moe_few(const void* x, int64_t ldx, int64_t n_tokens, int64_t hidden, c
             });
         };
         if (weight_type == TUNA_BF16) both((unsigned short*)nullptr, Int<-1>{});
+        else if (weight_type == TUNA_F4) both((Four*)nullptr, Int<TUNA_SCALE_E8>{});
         else if (scale_type == TUNA_SCALE_E8) both((uint8_t*)nullptr, Int<TUNA_SCALE_E8>{});
         else both((uint8_t*)nullptr, Int<TUNA_SCALE_F32>{});
     });

@@ -15,6 +15,7 @@ typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 typedef __bf16 v2b __attribute__((ext_vector_type(2)));
 
 constexpr int kBlock = 128;            // values that share a scale
+constexpr int kBlock4 = 32;            // and in 4 bits
 template <int V> struct Int { static constexpr int value = V; };
 constexpr int kLanes = 64;
 
@@ -99,6 +100,16 @@ template <bool WIDE> __device__ __forceinline__ v4u chunk16(const uint8_t* p, in
 #pragma unroll
     for (int i = 0; i < 16; ++i)
         if (i < left) a[i >> 2] |= (unsigned)p[i] << (8 * (i & 3));
+    return a;
+}
+
+// Thirty-two 4-bit values of which `left` exist; zeros behind them.  WIDE: on 16 bytes.
+template <bool WIDE> __device__ __forceinline__ v4u chunk32(const uint8_t* p, int64_t left) {
+    if (WIDE && left >= 32) return *(const v4u*)p;
+    v4u a = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (2 * i < left) a[i >> 2] |= (2 * i + 1 < left ? (unsigned)p[i] : (unsigned)p[i] & 15u) << (8 * (i & 3));
     return a;
 }
 
@@ -247,16 +258,16 @@ __device__ __forceinline__ Place find_tile(const int32_t* group_rows, int groups
     return p;
 }
 
-// The first block of 128 rows of a group in the columns' form, and how many it has.
-__device__ __forceinline__ void group_blocks(const int32_t* group_rows, int groups, int g, int64_t m, int64_t& first, int64_t& count) {
+// The first block of `size` rows of a group (128: in the columns' form), and how many it has.
+__device__ __forceinline__ void group_blocks(const int32_t* group_rows, int groups, int g, int64_t m, int64_t& first, int64_t& count, int size = kBlock) {
     const int lane = threadIdx.x & 63;
-    if (!group_rows) { first = 0; count = blocks_of(m); return; }
+    if (!group_rows) { first = 0; count = (m + size - 1) / size; return; }
     int64_t done = 0;
     int low = bound_at(group_rows, 0, m);
     for (int g0 = 0; g0 <= g; g0 += 64) {
         int a, b;
         group_bounds(group_rows, groups, g0, m, low, a, b);
-        const int n = (int)blocks_of((int64_t)b - a);
+        const int n = (int)(((int64_t)b - a + size - 1) / size);
         const int inc = wave_scan(n, lane);
         const int l = g - g0 < 63 ? g - g0 : 63;
         count = __shfl(n, l);

@@ -927,8 +927,38 @@ struct Few {
 // The parts of 128 neighbours of a row that one of four lanes holds, as they lie in memory, and eight of them at a time as bf16, which holds
 // every e4m3 exactly.  at(h, part): where the eight number h of lane `part` start.  Every load takes 64 bytes of a row in a piece.  whole(): all of it
 // is inside the row, so that the loads hang on no condition; the address is a wave's base and a lane's 32-bit offset in bytes.
+// row(n): the elements of a row of n values; kUnit: those of a block of 128.  A lane's scales of row r of `rows` of expert e: scales(...) says where the
+// first is, the next block's is kScales behind.  4-bit values take theirs where they are widened (INSIDE: bf16 holds the products), others in 32 bits.
+struct Four { uint8_t two; };           // two 4-bit values
 template <class W> struct Part;
-template <> struct Part<uint8_t> {
+template <class W> struct PartBase {
+    static constexpr int kUnit = kBlock, kScales = 1;
+    static constexpr bool INSIDE = false;
+    static __device__ __forceinline__ int64_t row(int64_t n) { return n; }
+    static __device__ __forceinline__ int64_t scales(int64_t e, int64_t rows, int64_t r, int64_t cols, int) { return (e * blocks_of(rows) + r / kBlock) * blocks_of(cols); }
+    static __device__ __forceinline__ int64_t last(int64_t at, int64_t, int, int64_t) { return at; }
+};
+template <> struct Part<Four> {
+    static constexpr int kUnit = kBlock / 2, kScales = kBlock / kBlock4;
+    static constexpr bool INSIDE = true;
+    v4u v;
+    static __device__ __forceinline__ int at(int h, int part) { return part * 32 + h * 8; }
+    static __device__ __forceinline__ int64_t row(int64_t n) { return (n + 1) / 2; }
+    static __device__ __forceinline__ int64_t scales(int64_t e, int64_t rows, int64_t r, int64_t cols, int part) { return (e * rows + r) * ((cols + kBlock4 - 1) / kBlock4) + part; }
+    // in the last block of a row: the row's last scale for the parts behind its end, whose values are zeros
+    static __device__ __forceinline__ int64_t last(int64_t at, int64_t b, int part, int64_t cols) {
+        const int64_t over = b * kScales + part - ((cols + kBlock4 - 1) / kBlock4 - 1);
+        return over > 0 ? at - over : at;
+    }
+    __device__ __forceinline__ void whole(const Four* base, unsigned off) { v = *(const v4u*)((const uint8_t*)base + (size_t)off); }
+    template <bool WIDE> __device__ __forceinline__ void load(const Four* p, int part, int64_t left) { v = chunk32<WIDE>((const uint8_t*)p + part * 16, left - part * 32); }
+    __device__ __forceinline__ v8b eight(int h, float k) const {
+        const v2b a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[h], k, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[h], k, 1);
+        const v2b c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[h], k, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[h], k, 3);
+        return v8b{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
+};
+template <> struct Part<uint8_t> : PartBase<uint8_t> {
     v4u v[2];
     static __device__ __forceinline__ int at(int h, int part) { return (h >> 1) * 64 + part * 16 + (h & 1) * 8; }
     __device__ __forceinline__ void whole(const uint8_t* base, unsigned off) {
@@ -939,9 +969,9 @@ template <> struct Part<uint8_t> {
 #pragma unroll
         for (int i = 0; i < 2; ++i) v[i] = chunk16<WIDE>(p + i * 64 + part * 16, left - (i * 64 + part * 16));
     }
-    __device__ __forceinline__ v8b eight(int h) const { return widen8(v[h >> 1][(h & 1) * 2], v[h >> 1][(h & 1) * 2 + 1]); }
+    __device__ __forceinline__ v8b eight(int h, float) const { return widen8(v[h >> 1][(h & 1) * 2], v[h >> 1][(h & 1) * 2 + 1]); }
 };
-template <> struct Part<unsigned short> {
+template <> struct Part<unsigned short> : PartBase<unsigned short> {
     v4u v[4];
     static __device__ __forceinline__ int at(int h, int part) { return h * 32 + part * 8; }
     __device__ __forceinline__ void whole(const unsigned short* base, unsigned off) {
@@ -952,7 +982,7 @@ template <> struct Part<unsigned short> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = bits8<WIDE>(p + at(i, part), left - at(i, part));
     }
-    __device__ __forceinline__ v8b eight(int h) const {
+    __device__ __forceinline__ v8b eight(int h, float) const {
         v8b r;
         __builtin_memcpy(&r, &v[h], 16);
         return r;
@@ -1087,10 +1117,11 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
     const int64_t f0 = SPLIT ? (int64_t)blockIdx.x * 16 : ((int64_t)blockIdx.x * kFewFirst + w) * 16;
     const int c = lane & 15, part = lane >> 4;
     const int64_t col = f0 + c < F.inner ? f0 + c : F.inner - 1;
-    const W* wg = (const W*)F.w1 + (int64_t)e * 2 * F.inner * F.hidden;
-    const W* wu = wg + F.inner * F.hidden;
-    const int64_t at_w = col * F.hidden, nb = blocks_of(F.hidden), sg = ((int64_t)e * blocks_of(2 * F.inner) + col / kBlock) * nb,
-                  su = ((int64_t)e * blocks_of(2 * F.inner) + (F.inner + col) / kBlock) * nb;
+    using Wp = Part<W>;
+    const int64_t row_w = Wp::row(F.hidden), at_w = col * row_w, nb = blocks_of(F.hidden);
+    const W* wg = (const W*)F.w1 + (int64_t)e * 2 * F.inner * row_w;
+    const W* wu = wg + F.inner * row_w;
+    const int64_t sg = Wp::scales(e, 2 * F.inner, col, F.hidden, part), su = Wp::scales(e, 2 * F.inner, F.inner + col, F.hidden, part);
     const unsigned off_w = (unsigned)(at_w * sizeof(W)) + part * 16;
     // whole blocks in a pipeline; what is behind them (all, for rows that do not start on 16 bytes) one block at a time
     const int whole = WIDE ? (int)(F.hidden / kBlock) : 0;
@@ -1123,10 +1154,13 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
         auto multiply = [&](const v8b (&a)[MT][4], const Part<W>& pg, const Part<W>& pu, float kg, float ku) {
             v4f g[MT], u[MT];
 #pragma unroll
-            for (int s = 0; s < MT; ++s) g[s] = u[s] = v4f{0.f, 0.f, 0.f, 0.f};
+            for (int s = 0; s < MT; ++s) {
+                g[s] = Wp::INSIDE ? gate[s] : v4f{0.f, 0.f, 0.f, 0.f};
+                u[s] = Wp::INSIDE ? up[s] : v4f{0.f, 0.f, 0.f, 0.f};
+            }
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-                const v8b bg = pg.eight(h), bu = pu.eight(h);
+                const v8b bg = pg.eight(h, kg), bu = pu.eight(h, ku);
 #pragma unroll
                 for (int s = 0; s < MT; ++s) {
                     g[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s][h], bg, g[s], 0, 0, 0);
@@ -1134,7 +1168,10 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
                 }
             }
 #pragma unroll
-            for (int s = 0; s < MT; ++s) { gate[s] += g[s] * kg; up[s] += u[s] * ku; }
+            for (int s = 0; s < MT; ++s) {
+                if (Wp::INSIDE) { gate[s] = g[s]; up[s] = u[s]; }
+                else { gate[s] += g[s] * kg; up[s] += u[s] * ku; }
+            }
         };
         constexpr int stride = SPLIT ? kFewFirst : 1, skip = SPLIT;
         if constexpr (WIDE) {
@@ -1143,10 +1180,10 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
             const int units = (whole - skip * w + stride - 1) / stride;
             auto fetch = [&](Ahead& t, int unit) {
                 const int64_t b = unit * stride + skip * w;
-                t.g.whole(wg + b * kBlock, off_w);
-                t.u.whole(wu + b * kBlock, off_w);
-                t.kg = scale_value<KIND>(F.s1, sg + b);
-                t.ku = scale_value<KIND>(F.s1, su + b);
+                t.g.whole(wg + b * Wp::kUnit, off_w);
+                t.u.whole(wu + b * Wp::kUnit, off_w);
+                t.kg = scale_value<KIND>(F.s1, sg + b * Wp::kScales);
+                t.ku = scale_value<KIND>(F.s1, su + b * Wp::kScales);
                 load_x(t.a, b * kBlock, Int<1>{});
             };
             pipeline<kFewAhead1, !SPLIT>(st, 0, units, fetch, [&](const Ahead& t, int) { multiply(t.a, t.g, t.u, t.kg, t.ku); });
@@ -1154,11 +1191,12 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
         for (int64_t b = whole + skip * w; b < nb; b += stride) {
             Part<W> g, u;
             const int64_t at = b * kBlock;
-            g.template load<WIDE>(wg + at + at_w, part, F.hidden - at);
-            u.template load<WIDE>(wu + at + at_w, part, F.hidden - at);
+            g.template load<WIDE>(wg + b * Wp::kUnit + at_w, part, F.hidden - at);
+            u.template load<WIDE>(wu + b * Wp::kUnit + at_w, part, F.hidden - at);
             v8b a[MT][4];
             load_x(a, at, Int<0>{});
-            multiply(a, g, u, scale_value<KIND>(F.s1, sg + b), scale_value<KIND>(F.s1, su + b));
+            multiply(a, g, u, scale_value<KIND>(F.s1, Wp::last(sg + b * Wp::kScales, b, part, F.hidden)),
+                     scale_value<KIND>(F.s1, Wp::last(su + b * Wp::kScales, b, part, F.hidden)));
         }
         auto keep = [&](int i, int64_t f, float x, float y) {     // activation f of token number i of the list
             if (i >= n || f >= F.inner) return;
@@ -1266,7 +1304,8 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
     const int64_t c0 = (int64_t)blockIdx.x * 16;
     const int c = lane & 15, part = lane >> 4;
     const int64_t col = c0 + c < F.hidden ? c0 + c : F.hidden - 1;
-    const int64_t nb = blocks_of(F.inner), nbh = blocks_of(F.hidden);
+    using Wp = Part<W>;
+    const int64_t nb = blocks_of(F.inner), row_w = Wp::row(F.inner);
     // whole blocks of all tasks in a pipeline; what is behind them (all, for rows that do not start on 16 bytes) one block at a time
     const int per = WIDE ? (int)(F.inner / kBlock) : 0;
     const int64_t total = (int64_t)n_tasks * per;
@@ -1294,14 +1333,15 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
         }
     };
     auto multiply = [&](const Act& a, const Part<W>& v, float scale) {
-        v4f y = {0.f, 0.f, 0.f, 0.f};
+        v4f y = Wp::INSIDE ? acc : v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-            const v8b bw = v.eight(h);
+            const v8b bw = v.eight(h, scale);
             y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.x[h], bw, y, 0, 0, 0);
             y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.z[h], bw, y, 0, 0, 0);
         }
-        acc += y * scale;
+        if (Wp::INSIDE) acc = y;
+        else acc += y * scale;
     };
     auto keep = [&](int task) {                                   // to the tokens' sums
         const int n = task_count[task], p0 = task_first[task];
@@ -1319,14 +1359,14 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
     if constexpr (WIDE) {
         struct Ahead { Part<W> v; float k; Act a; };
         struct Cursor { int task, block; };                       // a place in the sequence
-        const int64_t at_s = col / kBlock * nb;
-        const unsigned off_w = (unsigned)(col * F.inner * sizeof(W)) + part * 16;
+        const int64_t at_s = Wp::scales(0, F.hidden, col, F.inner, part), each = Wp::scales(1, F.hidden, 0, F.inner, 0);
+        const unsigned off_w = (unsigned)(col * row_w * sizeof(W)) + part * 16;
         auto step = [&](Cursor& q) { if (++q.block == per) { q.block = 0; ++q.task; } };
         Cursor now = {per ? lo / per : 0, per ? lo % per : 0}, far = now;
         auto fetch = [&](Ahead& t, int) {
             const int e = __builtin_amdgcn_readfirstlane(task_expert[far.task]);
-            t.v.whole((const W*)F.w2 + (int64_t)e * F.hidden * F.inner + far.block * kBlock, off_w);
-            t.k = scale_value<KIND>(F.s2, (int64_t)e * nbh * nb + far.block + at_s);
+            t.v.whole((const W*)F.w2 + (int64_t)e * F.hidden * row_w + far.block * Wp::kUnit, off_w);
+            t.k = scale_value<KIND>(F.s2, e * each + far.block * Wp::kScales + at_s);
             load_h(t.a, far.task, far.block * kBlock, Int<1>{});
             step(far);
         };
@@ -1342,10 +1382,10 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
             const int e = __builtin_amdgcn_readfirstlane(task_expert[task]);
             for (int64_t b = per; b < nb; ++b) {
                 Part<W> v;
-                v.template load<WIDE>((const W*)F.w2 + ((int64_t)e * F.hidden + col) * F.inner + b * kBlock, part, F.inner - b * kBlock);
+                v.template load<WIDE>((const W*)F.w2 + ((int64_t)e * F.hidden + col) * row_w + b * Wp::kUnit, part, F.inner - b * kBlock);
                 Act a;
                 load_h(a, task, b * kBlock, Int<0>{});
-                multiply(a, v, scale_value<KIND>(F.s2, ((int64_t)e * nbh + col / kBlock) * nb + b));
+                multiply(a, v, scale_value<KIND>(F.s2, Wp::last(Wp::scales(e, F.hidden, col, F.inner, part) + b * Wp::kScales, b, part, F.inner)));
             }
             keep(task);
         }

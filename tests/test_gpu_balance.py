@@ -1,0 +1,232 @@
+"""The balance loss of include/tuna_moe.h on the GPU against its definition in 64 bits (fp4_plain.py)."""
+import math
+
+import pytest
+import torch
+
+import fp4_plain as plain
+import paper_2411_02581_amd as tuna
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+CODE = {"f32": tuna.TUNA_F32, "bf16": tuna.TUNA_BF16}
+EPS = 2.0 ** -24
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def ok(rc):
+    assert rc == tuna.TUNA_OK, tuna.tuna_strerror(rc)
+
+
+def strided(x, ld):
+    mem = torch.zeros(x.shape[0], ld, dtype=x.dtype, device=DEV)
+    mem[:, :x.shape[1]] = x
+    return mem
+
+
+def choices(logits, k):
+    order = torch.sort(torch.where(logits.isnan(), -math.inf, logits.double()), dim=-1, descending=True, stable=True)
+    return torch.where(order.values[:, :k] > -math.inf, order.indices[:, :k], -1).to(torch.int32)
+
+
+def loss(logits, dtype, experts, bounds, ld=None):
+    t, e = logits.shape
+    k, groups = experts.shape[1], len(bounds) - 1
+    d = strided(logits, ld or e)
+    rc, size = tuna.tuna_moe_balance_workspace(t, e, groups)
+    ok(rc)
+    ws = torch.full((size + 32,), 0x5A, dtype=torch.uint8, device=DEV)
+    new = lambda *s, dtype=torch.int32: torch.full(s, 77, dtype=dtype, device=DEV)  # noqa: E731
+    out = new(groups + 1, e), new(groups + 1), new(groups + 1, e, dtype=torch.float32), new(groups + 1, dtype=torch.float32)
+    rows = None if groups == 1 and bounds == [0, t] else torch.tensor(bounds, dtype=torch.int32, device=DEV)
+    ok(tuna.tuna_moe_balance(d, CODE[dtype], ld or e, t, e, experts.to(DEV), k, rows, groups, *out, ws, max(size, 16)))
+    torch.cuda.synchronize()
+    assert bool((ws[max(size, 16):] == 0x5A).all()) and all(bool((v[groups:] == 77).all()) for v in out)
+    return d, rows, [v[:groups] for v in out]
+
+
+def check(logits, dtype, k, bounds, ld=None, experts=None):
+    logits = logits.to(TYPES[dtype])
+    t, e = logits.shape
+    groups = len(bounds) - 1
+    experts = choices(logits, k) if experts is None else experts
+    d, rows, (counts, tokens, shares, l) = loss(logits, dtype, experts, bounds, ld)
+    held = [0]
+    for b in bounds:
+        held.append(max(held[-1], min(max(b, 0), t)))
+    held = held[1:]
+    wc, wt, wsh, wl = plain.balance(logits, experts, held)
+    assert torch.equal(counts.cpu().long(), wc) and torch.equal(tokens.cpu().long(), wt)
+    # a share: an exponential of 2 units, a sum of up to 1024 of them in 16 sums and 6 steps, an inverse and a product: 48 half units; up to 16 of a wave's and
+    # 16 waves' are added in 32 bits, then in 64; one rounding at the end
+    room = (48 + 32 + 2) * EPS
+    assert torch.allclose(shares.cpu().double(), wsh, rtol=room, atol=1e-37)
+    assert torch.allclose(l.cpu().double(), wl, rtol=room, atol=1e-37)
+    dloss = torch.randn(groups, generator=gen(3))
+    exact = plain.balance_grad(logits, wc, wt, held, dloss)
+    base = torch.randn(t, e, generator=gen(4)).to(TYPES[dtype])
+    for add in (False, True):
+        dl = torch.full((t, e + 3), 5.0, dtype=TYPES[dtype], device=DEV)
+        dl[:, :e] = base if add else 7.0
+        ok(tuna.tuna_moe_balance_grad(d, CODE[dtype], ld or e, t, e, rows, groups, counts, tokens, dloss.to(DEV), tuna.TUNA_BALANCE_ADD if add else 0, dl, e + 3))
+        torch.cuda.synchronize()
+        want = exact + (base.double() if add else 0)
+        # slope p (f - <f, p>): f is at most 1 and <f, p> too; every factor within 64 half units of what is added
+        p, step = plain.softmax(logits), torch.zeros(t, 1, dtype=torch.float64)
+        for s in range(groups):
+            step[held[s]:held[s + 1]] = abs(float(dloss[s])) * e / max(int(wt[s]), 1)
+        f = torch.zeros(t, e, dtype=torch.float64)
+        for s in range(groups):
+            f[held[s]:held[s + 1]] = wc[s].double() / max(int(wc[s].sum()), 1)
+        size = step * p * (f + (p * f).sum(1, keepdim=True))
+        half = 2.0 ** -8 if dtype == "bf16" else 2 * EPS
+        assert bool(((dl[:, :e].cpu().double() - want).abs() <= 128 * EPS * size + half * want.abs() + 1e-37).all())
+        assert bool((dl[:, e:] == 5.0).all())
+        outside = torch.ones(t, dtype=torch.bool)
+        outside[held[0]:held[-1]] = False
+        assert torch.equal(dl[outside, :e].cpu(), base[outside] if add else torch.zeros_like(base[outside]))
+
+
+@pytest.mark.parametrize("t,e,k", [(1, 1, 1), (1, 8, 2), (3, 5, 5), (24, 64, 4), (65, 60, 6), (64, 65, 8), (130, 128, 8), (257, 200, 8), (1000, 256, 16), (40, 1000, 8),
+                                   (33, 1024, 16), (513, 64, 1)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_balance(t, e, k, dtype):
+    check(torch.randn(t, e, generator=gen(t * e)) * 3, dtype, k, [0, t])
+
+
+@pytest.mark.parametrize("bounds", [[0, 300], [0, 0, 0, 7, 300], [0, 100, 200, 300], [5, 290], [0, 256, 300], [17, 17, 40, 298], [0, 1, 2, 3, 4, 5, 6, 300],
+                                    [-4, 100, 50, 120, 9000], [300, 300], [sum(range(i)) % 301 for i in range(70)]])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_balance_of_sequences(bounds, dtype):
+    check(torch.randn(300, 70, generator=gen(1)) * 2, dtype, 4, bounds, ld=77)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_balance_masks(dtype):
+    x = torch.randn(90, 70, generator=gen(2))
+    x[::2, :60] = -math.inf
+    x[1::9, 3] = math.nan
+    x[2::9] = -math.inf                                          # nothing is left
+    x[3::9, :68] = -math.inf
+    x[4::9] = torch.finfo(torch.bfloat16).min
+    x[5::9] = math.nan
+    x[6::9, [5, 50]] = math.inf
+    x[7::9, 69] = 1e30
+    check(x, dtype, 4, [0, 90])
+    check(x, dtype, 4, [0, 30, 31, 90])
+    check(torch.full((20, 8), -math.inf), dtype, 2, [0, 5, 20])
+
+
+def test_balance_of_absent_experts():
+    """Numbers outside the experts count nowhere; the same expert twice in a token counts twice."""
+    x = torch.randn(50, 10, generator=gen(3))
+    ex = torch.randint(-3, 14, (50, 3), generator=gen(4), dtype=torch.int32)
+    ex[7] = 4
+    ex[8] = torch.tensor([1 << 30, -(1 << 31), 10])
+    check(x, "f32", 3, [0, 20, 50], experts=ex)
+    check(x, "f32", 3, [0, 50], experts=torch.full((50, 3), -1, dtype=torch.int32))
+
+
+def test_balance_of_no_token():
+    for bounds in ([0, 0], [0, 0, 0]):
+        _, _, (counts, tokens, shares, l) = loss(torch.zeros(0, 6), "f32", torch.zeros(0, 2, dtype=torch.int32), bounds)
+        assert all(int(v.abs().sum()) == 0 for v in (counts, tokens, shares, l))
+
+
+def test_even_and_uneven_use():
+    """One where all experts are used evenly, the number of experts where one has everything."""
+    t, e = 64, 16
+    x = torch.zeros(t, e)
+    even = (torch.arange(t)[:, None] % e).to(torch.int32)
+    assert float(loss(x, "f32", even, [0, t])[2][3]) == 1.0
+    x[:, 3] = 200.0
+    assert float(loss(x, "f32", torch.full((t, 1), 3, dtype=torch.int32), [0, t])[2][3]) == e
+
+
+def test_gradient_against_differences():
+    t, e, k, h, bounds = 9, 12, 3, 2.0 ** -6, [0, 4, 9]
+    x = torch.randn(t, e, generator=gen(4))
+    ex, dloss = choices(x, k), torch.tensor([0.7, -1.3])
+    d, rows, (counts, tokens, _, _) = loss(x, "f32", ex, bounds)
+    dl = torch.empty(t, e, device=DEV)
+    ok(tuna.tuna_moe_balance_grad(d, 0, e, t, e, rows, 2, counts, tokens, dloss.to(DEV), 0, dl, e))
+    for i in range(e):
+        side = []
+        for s in (h, -h):
+            for r in range(t):
+                y = x.clone()
+                y[r, i] += s
+                side.append(float((loss(y, "f32", ex, bounds)[2][3].cpu().double() * dloss).sum()))
+        for r in range(t):
+            # the loss is some 1 within 82 half units, twice, over 2 h; its third derivative is at most some 10 e / n, times h^2 / 6
+            assert abs((side[r] - side[t + r]) / (2 * h) - float(dl[r, i])) <= 4 * 82 * EPS * 4 / (2 * h) + 10 * h * h / 6
+
+
+def test_the_router_s_whole_gradient():
+    """tuna_moe_route, tuna_moe_balance, and both gradients in one array."""
+    t, e, k = 200, 32, 4
+    x = torch.randn(t, e, generator=gen(5))
+    d = x.to(DEV)
+    rc, size = tuna.tuna_moe_route_workspace(t, e, k, False)
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    i32 = lambda *s: torch.empty(*s, dtype=torch.int32, device=DEV)  # noqa: E731
+    ex, w, slots, rows = i32(t, k), torch.empty(t, k, device=DEV), i32(t, k), i32(e + 1)
+    ok(tuna.tuna_moe_route(d, 0, e, t, e, k, 1, ex, w, slots, rows, 1, None, None, None, None, ws, size))
+    rc, size = tuna.tuna_moe_balance_workspace(t, e, 1)
+    ws2, counts, tokens, shares, l = torch.empty(size, dtype=torch.uint8, device=DEV), i32(1, e), i32(1), torch.empty(1, e, device=DEV), torch.empty(1, device=DEV)
+    ok(tuna.tuna_moe_balance(d, 0, e, t, e, ex, k, None, 1, counts, tokens, shares, l, ws2, size))
+    assert torch.equal(counts[0].cpu(), (rows[1:] - rows[:-1]).cpu())
+    dw, dloss, dl = torch.randn(t, k, generator=gen(6)), torch.tensor([0.01]), torch.empty(t, e, device=DEV)
+    ok(tuna.tuna_moe_route_grad(d, 0, e, t, e, k, 1, ex, w, dw.to(DEV), dl, e))
+    ok(tuna.tuna_moe_balance_grad(d, 0, e, t, e, None, 1, counts, tokens, dloss.to(DEV), tuna.TUNA_BALANCE_ADD, dl, e))
+    y = x.double().requires_grad_()
+    p = torch.softmax(y, -1)
+    chosen = p.gather(1, ex.cpu().long())
+    f = counts[0].cpu().double() / (t * k)
+    ((chosen / chosen.sum(-1, keepdim=True) * dw).sum() + 0.01 * e * (f * p.mean(0)).sum()).backward()
+    assert torch.allclose(dl.cpu().double(), y.grad, rtol=0, atol=200 * EPS * float(dw.abs().sum(1).max() + 1))
+
+
+@pytest.mark.parametrize("groups", [1, 3])
+def test_in_a_graph_and_on_two_streams(groups):
+    t, e, k = 700, 48, 4
+    bounds = [t * i // groups for i in range(groups + 1)]
+    logits = torch.randn(t, e, generator=gen(1)).to(DEV)
+    ex = choices(logits.cpu(), k).to(DEV)
+    rows = torch.tensor(bounds, dtype=torch.int32, device=DEV)
+    dloss = torch.ones(groups, device=DEV)
+    rc, size = tuna.tuna_moe_balance_workspace(t, e, groups)
+
+    def new():
+        i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device=DEV)  # noqa: E731
+        return [i32(groups, e), i32(groups), torch.zeros(groups, e, device=DEV), torch.zeros(groups, device=DEV), torch.zeros(t, e, device=DEV),
+                torch.empty(size, dtype=torch.uint8, device=DEV)]
+
+    def step(o):
+        ok(tuna.tuna_moe_balance(logits, 0, e, t, e, ex, k, rows, groups, *o[:4], o[5], size))
+        ok(tuna.tuna_moe_balance_grad(logits, 0, e, t, e, rows, groups, o[0], o[1], dloss, 0, o[4], e))
+
+    eager, kept, sides = new(), new(), [(torch.cuda.Stream(), new()) for _ in range(2)]
+    step(eager)
+    for s, o in sides:
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            step(o)
+    torch.cuda.synchronize()
+    for _, o in sides:
+        assert all(torch.equal(a, b) for a, b in zip(o[:5], eager[:5]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=sides[0][0]):
+        step(kept)
+    for n in range(3):
+        logits.copy_(torch.randn(t, e, generator=gen(10 + n)))
+        step(eager)
+        for v in kept[:5]:
+            v.fill_(0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(kept[:5], eager[:5]))
