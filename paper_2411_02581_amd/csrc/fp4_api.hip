@@ -102,7 +102,27 @@ bool product_wide(const Product4& P) {
            P.ld_bs % 4 == 0 && P.bs_group % 4 == 0;
 }
 
+template <int BM, int BN, int WM, int WN, bool COLS, class OUT> void launch_tiles(const Product4& P, void* stream) {
+    const int64_t nt = ceil_div(P.n, BN), mt = COLS ? ceil_div(P.m, BM) : ceil_div(P.m, BM) + P.groups - 1;
+    const int64_t grid = COLS ? ceil_div(mt * nt, 8) * 8 * P.groups : ceil_div(mt * nt, 8) * 8;
+    LAUNCH((k_fp4_product<COLS, OUT, BM, BN, WM, WN>), dim3((unsigned)grid), 256, P, (int)mt, (int)nt);
+}
+
+// Tiles of the large form: rows of scales start on 16 bytes, offsets inside a tile are 32 bits.
+bool product_large(const Product4& P, bool cols) {
+    const int64_t nt = ceil_div(P.n, 128), mt = ceil_div(P.m, 128) + (cols ? 0 : P.groups - 1);
+    return product_wide(P) && on(P.as, 16) && on(P.bs, 16) && P.ld_as % 16 == 0 && P.ld_bs % 16 == 0 && P.bs_group % 16 == 0 && P.lda < (1 << 22) && P.ldb < (1 << 22) &&
+           grid_fits((mt * nt + 8) * (cols ? P.groups : 1), 256) && P.n > 64;
+}
+
 int launch_product(const Product4& P, bool cols, int out_type, void* stream) {
+    if (product_large(P, cols)) {
+        with_type(out_type, [&](auto* o) {
+            using O = Pointee<decltype(o)>;
+            with_bool(cols, [&](auto cl) { launch_tiles<256, 256, 2, 2, cl.value != 0, O>(P, stream); });
+        });
+        return launched();
+    }
     const int64_t nt = ceil_div(P.n, 64), mt = cols ? ceil_div(P.m, 64) : ceil_div(P.m, 64) + P.groups - 1;
     if (!grid_fits(mt, 256)) return TUNA_ERR_TOO_LARGE;
     const dim3 grid((unsigned)mt, (unsigned)nt, cols ? P.groups : 1);

@@ -247,4 +247,221 @@ __global__ __launch_bounds__(256) void k_fp4_product64(Product4 P) {
     }
 }
 
+// Sixteen bytes a lane from memory straight into the LDS, lane after lane behind `to`, which a wave has in common: from a base that it has in common and a
+// lane's offset, or from a lane's address.  Nothing but the counter of loads says when they are there: whoever reads the LDS waits for it (see loads_left).
+__device__ __forceinline__ void dma16(const uint8_t* base, unsigned off, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void dma16(const uint8_t* from, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+// An address that a wave has in common, as one of its scalars.
+__device__ __forceinline__ const uint8_t* scalar(const uint8_t* p) {
+    const uint64_t v = (uint64_t)p;
+    const unsigned low = __builtin_amdgcn_readfirstlane((unsigned)v), high = __builtin_amdgcn_readfirstlane((unsigned)(v >> 32));
+    return (const uint8_t*)((uint64_t)high << 32 | low);
+}
+// At most N of the wave's loads are still under way, none of its reads of the LDS is, and all waves of the workgroup are here.
+template <int N> __device__ __forceinline__ void loads_left_and_barrier() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// The large form: a tile of BM x BN, four waves, stages of 128 of the length through four parts of the LDS.  While a stage is multiplied, the next
+// one's rows go from the LDS to registers, the two behind it are on their way and the one after them is asked for: a load has three stages' time (some
+// 1.3 us in the largest tile) to arrive, and between stages there is one barrier.  A row of a stage is 64 bytes; its sixteen number c lies at place c xor
+// (row / 4 mod 4), so that the lanes that the LDS serves together meet every bank once.  The scales come in sixteens, for four stages (512 of the
+// length, from multiples of 512); a lane collects its block's byte of four stages in one register, of which a product takes byte STEP.
+// The waves' rows: WM x WN waves, 16 MT by 16 NT each.
+template <bool COLS, class OUT, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles, int n_tiles) {
+    constexpr int W = 4, MT = BM / (16 * WM), NT = BN / (16 * WN), LA = BM / 16 / W, LB = BN / 16 / W, LS = (BM + BN) / 64 / W, PART = (BM + BN) * 64;
+    static_assert(WM * WN == W && LA * 16 * W == BM && LB * 16 * W == BN && LS * 64 * W == BM + BN && LA + LB <= MT && BM % 64 == 0, "");
+    __shared__ __align__(1024) uint8_t tile[4][PART];
+    __shared__ __align__(1024) uint8_t scale[2][(BM + BN) * 16];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w / WN, wn = w % WN;
+    int group = 0, id;
+    if (COLS) {                                                   // every XCD has an eighth of each group, for groups are of any length
+        const unsigned share = (m_tiles * n_tiles + 7) / 8, at = blockIdx.x / 8;
+        group = at / share;
+        id = blockIdx.x % 8 * share + at % share;
+        if (id >= m_tiles * n_tiles) return;
+    } else {
+        m_tiles = __builtin_amdgcn_readfirstlane(count_tiles(P.group_rows, P.groups, P.m, BM));
+        id = xcd_run(blockIdx.x, (unsigned)m_tiles * n_tiles);
+        if (id < 0) return;
+    }
+    // runs of four rows of tiles, column after column
+    const int run = id / (4 * n_tiles), in_run = id - run * 4 * n_tiles, height = m_tiles - run * 4 < 4 ? m_tiles - run * 4 : 4;
+    const int ti = run * 4 + in_run % height, tj = in_run / height;
+    int64_t i0, i_end, first = 0, last;
+    const int64_t j0 = (int64_t)tj * BN;
+    if (COLS) {
+        i0 = (int64_t)ti * BM;
+        i_end = i0 + BM < P.m ? i0 + BM : P.m;
+        int64_t count;
+        group_blocks(P.group_rows, P.groups, group, P.k, first, count);
+        last = first + count;
+    } else {
+        const Place pl = find_tile(P.group_rows, P.groups, P.m, BM, ti);
+        if (pl.group < 0) return;
+        group = pl.group; i0 = pl.first; i_end = pl.end;
+        last = blocks_of(P.k);
+    }
+    i0 = (int64_t)__builtin_amdgcn_readfirstlane((int)i0);
+    i_end = (int64_t)__builtin_amdgcn_readfirstlane((int)i_end);
+    group = __builtin_amdgcn_readfirstlane(group);
+    const int s0 = __builtin_amdgcn_readfirstlane((int)first), s1 = __builtin_amdgcn_readfirstlane((int)last);
+    const int whole = COLS ? s1 : (int)(P.k / kBlock);            // stages before this one are whole
+    const int rows_a = (int)(i_end - i0), rows_b = (int)(P.n - j0 < BN ? P.n - j0 : BN);
+    const uint8_t* a = scalar(P.a + i0 * P.lda);
+    const uint8_t* b = scalar(P.b + (COLS ? 0 : group * P.b_group) + j0 * P.ldb);
+    const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&tile[0][0];
+    const unsigned lds_scale = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&scale[0][0];
+    // this lane's sixteens of a stage: LA of a's rows, then LB of b's
+    const int chunk = (lane & 3) ^ (lane >> 4);
+    unsigned at[LA + LB];
+#pragma unroll
+    for (int j = 0; j < LA + LB; ++j) {
+        const bool of_a = j < LA;
+        const int r = (of_a ? w * LA + j : w * LB + j - LA) * 16 + (lane >> 2), most = of_a ? rows_a : rows_b;
+        at[j] = (unsigned)((r < most ? r : most - 1) * (of_a ? P.lda : P.ldb)) + chunk * 16;
+    }
+    // and its rows of scales
+    const uint8_t* at_s[LS];
+#pragma unroll
+    for (int j = 0; j < LS; ++j) {
+        const int r = (w * LS + j) * 64 + lane;
+        if (r < BM) at_s[j] = P.as + (i0 + (r < rows_a ? r : rows_a - 1)) * P.ld_as;
+        else at_s[j] = P.bs + (COLS ? 0 : group * P.bs_group) + (j0 + (r - BM < rows_b ? r - BM : rows_b - 1)) * P.ld_bs;
+    }
+    auto place = [&](int j) { return j < LA ? (w * LA + j) * 1024 : BM * 64 + (w * LB + j - LA) * 1024; };
+    auto ask = [&](int s, int part, int j) { dma16((j < LA ? a : b) + (int64_t)s * 64, at[j], lds + part * PART + place(j)); };
+    // a stage that ends inside: zeros behind the end, through registers
+    auto fill = [&](int s, int part) {
+        const int64_t left = P.k - (int64_t)s * kBlock - chunk * 32;
+#pragma unroll
+        for (int j = 0; j < LA + LB; ++j) {
+            const uint8_t* p = (j < LA ? a : b) + (int64_t)s * 64 + at[j];
+            v4u v = {0u, 0u, 0u, 0u};
+            if (left >= 32) v = *(const v4u*)p;
+            else if (left > 0) {
+#pragma unroll 1
+                for (int i = 0; 2 * i < left; ++i) {
+                    const unsigned one = (2 * i + 1 < left ? (unsigned)p[i] : (unsigned)p[i] & 15u) << (8 * (i & 3));
+                    if (i < 4) v[0] |= one; else if (i < 8) v[1] |= one; else if (i < 12) v[2] |= one; else v[3] |= one;
+                }
+            }
+            *(v4u*)&tile[part][place(j) + lane * 16] = v;
+        }
+    };
+    auto ask_scales = [&](int t) {
+        if (t * 4 >= s1) return;
+        // sixteen scales that all exist, of four stages, or what there is
+        const int64_t there = (COLS ? (int64_t)s1 * 4 : (P.k + kBlock4 - 1) / kBlock4) - (int64_t)t * 16;
+        if (there >= 16) {
+#pragma unroll
+            for (int j = 0; j < LS; ++j) dma16(at_s[j] + (int64_t)t * 16, lds_scale + (t & 1) * (BM + BN) * 16 + (w * LS + j) * 1024);
+        } else {
+#pragma unroll
+            for (int j = 0; j < LS; ++j) {
+                v4u v = {0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
+#pragma unroll 1
+                for (int i = 0; i < there; ++i) {
+                    const unsigned one = ((unsigned)at_s[j][(int64_t)t * 16 + i] ^ 0x7fu) << (8 * (i & 3));
+                    if (i < 4) v[0] ^= one; else if (i < 8) v[1] ^= one; else if (i < 12) v[2] ^= one; else v[3] ^= one;
+                }
+                *(v4u*)&scale[t & 1][(w * LS + j) * 1024 + lane * 16] = v;
+            }
+        }
+    };
+    v4f acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    const int r = lane & 15, g = lane >> 4, mine = r * 64 + (g ^ (r >> 2)) * 16;
+    v4u fa[2], fb[2][NT];
+    unsigned sa[MT], sb[NT];
+    auto read_a = [&](int part, int i) { return *(const v4u*)&tile[part][(wm * MT + i) * 1024 + mine]; };
+    auto read_b = [&](int part, int j) { return *(const v4u*)&tile[part][BM * 64 + (wn * NT + j) * 1024 + mine]; };
+    // byte g of four words
+    const unsigned low = 0x0c0c0400u + g * 0x0101u, high = 0x04000c0cu + g * 0x01010000u;
+    auto read_scale = [&](int t, int row) {
+        const v4u v = *(const v4u*)&scale[t & 1][row * 16];
+        return __builtin_amdgcn_perm(v[1], v[0], low) | __builtin_amdgcn_perm(v[3], v[2], high);
+    };
+    const int row_a = wm * MT * 16 + r, row_b = BM + wn * NT * 16 + r;
+    if (s0 < s1) {
+        const int t0 = s0 / 4;
+        ask_scales(t0);
+        ask_scales(t0 + 1);
+#pragma unroll 1
+        for (int s = s0; s < s0 + 3; ++s) {
+            if (s < whole) {
+#pragma unroll
+                for (int j = 0; j < LA + LB; ++j) ask(s, s & 3, j);
+            } else if (s < s1) {
+                fill(s, s & 3);
+            }
+        }
+        if (s0 + 2 < whole) loads_left_and_barrier<2 * (LA + LB)>(); else loads_left_and_barrier<0>();
+        fa[0] = read_a(s0 & 3, 0);
+        auto begin = [&](auto odd) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) fb[odd.value][j] = read_b(s0 & 3, j);
+        };
+        if (COLS && (s0 & 1)) begin(Int<1>{}); else begin(Int<0>{});
+#pragma unroll
+        for (int i = 0; i < MT; ++i) sa[i] = read_scale(t0, row_a + i * 16);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sb[j] = read_scale(t0, row_b + j * 16);
+        // Stage s = 4 t + U.  False: there is no such stage.
+        auto stage = [&](int t, auto step) {
+            constexpr int U = step.value, now = U & 1, then = now ^ 1;
+            const int s = 4 * t + U;
+            if (COLS && s < s0) return true;
+            if (s >= s1) return false;
+            if (s + 2 < whole) loads_left_and_barrier<LA + LB>(); else loads_left_and_barrier<0>();
+            if (U == 0 && t > t0) ask_scales(t + 1);
+            const bool more = s + 3 < whole;
+            if (!more && s + 3 < s1) fill(s + 3, (U + 3) & 3);
+            unsigned na[MT], nb[NT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                if (more && i < LA + LB) ask(s + 3, (U + 3) & 3, i);
+                fa[(i + 1) & 1] = i + 1 < MT ? read_a(U, i + 1) : read_a((U + 1) & 3, 0);
+                if (i < NT) fb[then][i] = read_b((U + 1) & 3, i);
+                if (U == 3) {
+                    na[i] = read_scale(t + 1, row_a + i * 16);
+                    if (i < NT) nb[i] = read_scale(t + 1, row_b + i * 16);
+                }
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = mma4<U>(fb[now][j], fa[i & 1], acc[i][j], sb[j], sa[i]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (U == 3) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i) sa[i] = na[i];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) sb[j] = nb[j];
+            }
+            return true;
+        };
+        static_assert(NT <= MT && MT % 2 == 0, "");
+        for (int t = t0; stage(t, Int<0>{}) && stage(t, Int<1>{}) && stage(t, Int<2>{}) && stage(t, Int<3>{}); ++t) {}
+    }
+    OUT* out = (OUT*)P.out + (COLS ? group * P.out_group : 0);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t row = i0 + (wm * MT + i) * 16 + r;
+        if (row >= i_end) continue;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int64_t col = j0 + (wn * NT + j) * 16 + g * 4;
+            if (col >= P.n) continue;
+            store_four(out + row * P.ldo + col, acc[i][j], (int)(P.n - col < 4 ? P.n - col : 4));
+        }
+    }
+}
+
 }  // namespace moe
