@@ -108,11 +108,11 @@ template <int BM, int BN, int WM, int WN, bool COLS, class OUT> void launch_tile
     LAUNCH((k_fp4_product<COLS, OUT, BM, BN, WM, WN>), dim3((unsigned)grid), 256, P, (int)mt, (int)nt);
 }
 
-// Tiles of the large form: rows of scales start on 16 bytes, offsets inside a tile are 32 bits.
+// Tiles of the large form: rows of scales start on 16 bytes, offsets inside a tile are 32 bits, and there is a whole stage of 128.
 bool product_large(const Product4& P, bool cols) {
     const int64_t nt = ceil_div(P.n, 128), mt = ceil_div(P.m, 128) + (cols ? 0 : P.groups - 1);
     return product_wide(P) && on(P.as, 16) && on(P.bs, 16) && P.ld_as % 16 == 0 && P.ld_bs % 16 == 0 && P.bs_group % 16 == 0 && P.lda < (1 << 22) && P.ldb < (1 << 22) &&
-           grid_fits((mt * nt + 8) * (cols ? P.groups : 1), 256) && P.n > 64;
+           grid_fits((mt * nt + 8) * (cols ? P.groups : 1), 256) && P.n > 64 && (cols || P.k >= kBlock);
 }
 
 int launch_product(const Product4& P, bool cols, int out_type, void* stream) {

@@ -278,6 +278,7 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
     static_assert(WM * WN == W && LA * 16 * W == BM && LB * 16 * W == BN && LS * 64 * W == BM + BN && LA + LB <= MT && BM % 64 == 0, "");
     __shared__ __align__(1024) uint8_t tile[4][PART];
     __shared__ __align__(1024) uint8_t scale[2][(BM + BN) * 16];
+    __shared__ __align__(1024) uint8_t nowhere[W][1024];          // where loads go that ask for no stage
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w / WN, wn = w % WN;
     int group = 0, id;
     if (COLS) {                                                   // every XCD has an eighth of each group, for groups are of any length
@@ -335,23 +336,24 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
         else at_s[j] = P.bs + (COLS ? 0 : group * P.bs_group) + (j0 + (r - BM < rows_b ? r - BM : rows_b - 1)) * P.ld_bs;
     }
     auto place = [&](int j) { return j < LA ? (w * LA + j) * 1024 : BM * 64 + (w * LB + j - LA) * 1024; };
-    auto ask = [&](int s, int part, int j) { dma16((j < LA ? a : b) + (int64_t)s * 64, at[j], lds + part * PART + place(j)); };
-    // a stage that ends inside: zeros behind the end, through registers
+    // sixteens number j of whole stage s; behind the whole stages the last one's, to nowhere, so that every stage is as many loads
+    const unsigned away = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&nowhere[w][0];
+    auto ask = [&](int s, int part, int j) {
+        const bool there = s < whole;
+        dma16((j < LA ? a : b) + (int64_t)(there ? s : whole - 1) * 64, at[j], there ? lds + part * PART + place(j) : away);
+    };
+    // a stage that ends inside: zeros behind the end, through registers; a sixteen that ends inside is read up to the row's end, from as many bytes ahead
     auto fill = [&](int s, int part) {
-        const int64_t left = P.k - (int64_t)s * kBlock - chunk * 32;
+        const int left = (int)(P.k - (int64_t)s * kBlock) - chunk * 32, ahead = left >= 32 ? 0 : 16 - (left + 1) / 2;
 #pragma unroll
         for (int j = 0; j < LA + LB; ++j) {
-            const uint8_t* p = (j < LA ? a : b) + (int64_t)s * 64 + at[j];
-            v4u v = {0u, 0u, 0u, 0u};
-            if (left >= 32) v = *(const v4u*)p;
-            else if (left > 0) {
-#pragma unroll 1
-                for (int i = 0; 2 * i < left; ++i) {
-                    const unsigned one = (2 * i + 1 < left ? (unsigned)p[i] : (unsigned)p[i] & 15u) << (8 * (i & 3));
-                    if (i < 4) v[0] |= one; else if (i < 8) v[1] |= one; else if (i < 12) v[2] |= one; else v[3] |= one;
-                }
+            unsigned __int128 v = 0;
+            if (left > 0) {
+                __builtin_memcpy(&v, (j < LA ? P.a + i0 * P.lda : P.b + group * P.b_group + j0 * P.ldb) + (int64_t)s * 64 + at[j] - ahead, 16);
+                v >>= 8 * ahead;
+                if (left < 32) v &= ((unsigned __int128)1 << (4 * left)) - 1;
             }
-            *(v4u*)&tile[part][place(j) + lane * 16] = v;
+            __builtin_memcpy(&tile[part][place(j) + lane * 16], &v, 16);
         }
     };
     auto ask_scales = [&](int t) {
@@ -380,7 +382,7 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
     const int r = lane & 15, g = lane >> 4, mine = r * 64 + (g ^ (r >> 2)) * 16;
-    v4u fa[2], fb[2][NT];
+    v4u fa[4], fb[2][NT];
     unsigned sa[MT], sb[NT];
     auto read_a = [&](int part, int i) { return *(const v4u*)&tile[part][(wm * MT + i) * 1024 + mine]; };
     auto read_b = [&](int part, int j) { return *(const v4u*)&tile[part][BM * 64 + (wn * NT + j) * 1024 + mine]; };
@@ -397,15 +399,13 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
         ask_scales(t0 + 1);
 #pragma unroll 1
         for (int s = s0; s < s0 + 3; ++s) {
-            if (s < whole) {
+            if (s >= whole && s < s1) fill(s, s & 3);
 #pragma unroll
-                for (int j = 0; j < LA + LB; ++j) ask(s, s & 3, j);
-            } else if (s < s1) {
-                fill(s, s & 3);
-            }
+            for (int j = 0; j < LA + LB; ++j) ask(s, s & 3, j);
         }
-        if (s0 + 2 < whole) loads_left_and_barrier<2 * (LA + LB)>(); else loads_left_and_barrier<0>();
+        loads_left_and_barrier<2 * (LA + LB)>();
         fa[0] = read_a(s0 & 3, 0);
+        fa[1] = read_a(s0 & 3, 1);
         auto begin = [&](auto odd) {
 #pragma unroll
             for (int j = 0; j < NT; ++j) fb[odd.value][j] = read_b(s0 & 3, j);
@@ -421,22 +421,21 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
             const int s = 4 * t + U;
             if (COLS && s < s0) return true;
             if (s >= s1) return false;
-            if (s + 2 < whole) loads_left_and_barrier<LA + LB>(); else loads_left_and_barrier<0>();
+            loads_left_and_barrier<LA + LB>();
             if (U == 0 && t > t0) ask_scales(t + 1);
-            const bool more = s + 3 < whole;
-            if (!more && s + 3 < s1) fill(s + 3, (U + 3) & 3);
+            if (s + 3 >= whole && s + 3 < s1) fill(s + 3, (U + 3) & 3);
             unsigned na[MT], nb[NT];
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                if (more && i < LA + LB) ask(s + 3, (U + 3) & 3, i);
-                fa[(i + 1) & 1] = i + 1 < MT ? read_a(U, i + 1) : read_a((U + 1) & 3, 0);
+                if (i < LA + LB) ask(s + 3, (U + 3) & 3, i);
+                fa[(i + 2) & 3] = i + 2 < MT ? read_a(U, i + 2) : read_a((U + 1) & 3, i + 2 - MT);
                 if (i < NT) fb[then][i] = read_b((U + 1) & 3, i);
                 if (U == 3) {
                     na[i] = read_scale(t + 1, row_a + i * 16);
                     if (i < NT) nb[i] = read_scale(t + 1, row_b + i * 16);
                 }
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = mma4<U>(fb[now][j], fa[i & 1], acc[i][j], sb[j], sa[i]);
+                for (int j = 0; j < NT; ++j) acc[i][j] = mma4<U>(fb[now][j], fa[i & 3], acc[i][j], sb[j], sa[i]);
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (U == 3) {
@@ -447,7 +446,7 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
             }
             return true;
         };
-        static_assert(NT <= MT && MT % 2 == 0, "");
+        static_assert(NT <= MT && MT % 4 == 0, "");
         for (int t = t0; stage(t, Int<0>{}) && stage(t, Int<1>{}) && stage(t, Int<2>{}) && stage(t, Int<3>{}); ++t) {}
     }
     OUT* out = (OUT*)P.out + (COLS ? group * P.out_group : 0);
