@@ -6,6 +6,7 @@
 namespace moe {
 
 typedef float v2f __attribute__((ext_vector_type(2)));
+typedef float v16f __attribute__((ext_vector_type(16)));
 
 // ------------------------------------------------------------------------------------------------ quantisation
 
@@ -188,6 +189,12 @@ template <int STEP> __device__ __forceinline__ v4f mma4(const v4u& b, const v4u&
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wb, wa, c, 4, 4, STEP, (int)sb, STEP, (int)sa);
 }
 
+// 32 x 32 x 64, lane (r, g) with block number g of two of row r: a lane holds four times four neighbours of one row of `out`.
+template <int STEP> __device__ __forceinline__ v16f mma4_32(const v4u& b, const v4u& a, v16f c, unsigned sb, unsigned sa) {
+    const v8i wb = {(int)b[0], (int)b[1], (int)b[2], (int)b[3]}, wa = {(int)a[0], (int)a[1], (int)a[2], (int)a[3]};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wb, wa, c, 4, 4, STEP, (int)sb, STEP, (int)sa);
+}
+
 // The simple form: a tile of 64 x 64, four waves of 16 rows each, 128 of the length at a time through the LDS; any alignment.
 // COLS: the reduction is over the groups' rows (gradient of the weights).
 template <bool COLS, bool WIDE, class OUT>
@@ -270,12 +277,12 @@ template <int N> __device__ __forceinline__ void loads_left_and_barrier() {
 // one's rows go from the LDS to registers, the two behind it are on their way and the one after them is asked for: a load has three stages' time (some
 // 1.3 us in the largest tile) to arrive, and between stages there is one barrier.  A row of a stage is 64 bytes; its sixteen number c lies at place c xor
 // (row / 4 mod 4), so that the lanes that the LDS serves together meet every bank once.  The scales come in sixteens, for four stages (512 of the
-// length, from multiples of 512); a lane collects its block's byte of four stages in one register, of which a product takes byte STEP.
-// The waves' rows: WM x WN waves, 16 MT by 16 NT each.
+// length, from multiples of 512); a lane collects its blocks' bytes of two stages in one register, of which a product takes byte STEP.
+// The waves: WM x WN, 32 MT by 32 NT each; a stage is two steps of 64, in which lane (r, g) has block number 2 g + step of row r.
 template <bool COLS, class OUT, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles, int n_tiles) {
-    constexpr int W = 4, MT = BM / (16 * WM), NT = BN / (16 * WN), LA = BM / 16 / W, LB = BN / 16 / W, LS = (BM + BN) / 64 / W, PART = (BM + BN) * 64;
-    static_assert(WM * WN == W && LA * 16 * W == BM && LB * 16 * W == BN && LS * 64 * W == BM + BN && LA + LB <= MT && BM % 64 == 0, "");
+    constexpr int W = 4, MT = BM / (32 * WM), NT = BN / (32 * WN), LA = BM / 16 / W, LB = BN / 16 / W, LS = (BM + BN) / 64 / W, PART = (BM + BN) * 64;
+    static_assert(WM * WN == W && LA * 16 * W == BM && LB * 16 * W == BN && LS * 64 * W == BM + BN && BM % 64 == 0 && MT % 2 == 0 && NT == 4, "");
     __shared__ __align__(1024) uint8_t tile[4][PART];
     __shared__ __align__(1024) uint8_t scale[2][(BM + BN) * 16];
     __shared__ __align__(1024) uint8_t nowhere[W][1024];          // where loads go that ask for no stage
@@ -311,7 +318,9 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
     i0 = (int64_t)__builtin_amdgcn_readfirstlane((int)i0);
     i_end = (int64_t)__builtin_amdgcn_readfirstlane((int)i_end);
     group = __builtin_amdgcn_readfirstlane(group);
-    const int s0 = __builtin_amdgcn_readfirstlane((int)first), s1 = __builtin_amdgcn_readfirstlane((int)last);
+    int s0 = __builtin_amdgcn_readfirstlane((int)first);
+    asm("" : "+s"(s0));                                           // (a first stage that the compiler knows makes it peel the loop, and spill)
+    const int s1 = __builtin_amdgcn_readfirstlane((int)last);
     const int whole = COLS ? s1 : (int)(P.k / kBlock);            // stages before this one are whole
     const int rows_a = (int)(i_end - i0), rows_b = (int)(P.n - j0 < BN ? P.n - j0 : BN);
     const uint8_t* a = scalar(P.a + i0 * P.lda);
@@ -345,15 +354,17 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
     // a stage that ends inside: zeros behind the end, through registers; a sixteen that ends inside is read up to the row's end, from as many bytes ahead
     auto fill = [&](int s, int part) {
         const int left = (int)(P.k - (int64_t)s * kBlock) - chunk * 32, ahead = left >= 32 ? 0 : 16 - (left + 1) / 2;
-#pragma unroll
+#pragma unroll 1
         for (int j = 0; j < LA + LB; ++j) {
+            const int to = place(j), row = (j < LA ? to : to - BM * 64) / 64 + (lane >> 2), most = j < LA ? rows_a : rows_b;
             unsigned __int128 v = 0;
             if (left > 0) {
-                __builtin_memcpy(&v, (j < LA ? P.a + i0 * P.lda : P.b + group * P.b_group + j0 * P.ldb) + (int64_t)s * 64 + at[j] - ahead, 16);
+                __builtin_memcpy(&v, (j < LA ? P.a + i0 * P.lda : P.b + group * P.b_group + j0 * P.ldb) + (row < most ? row : most - 1) * (j < LA ? P.lda : P.ldb) +
+                                 (int64_t)s * 64 + chunk * 16 - ahead, 16);
                 v >>= 8 * ahead;
                 if (left < 32) v &= ((unsigned __int128)1 << (4 * left)) - 1;
             }
-            __builtin_memcpy(&tile[part][place(j) + lane * 16], &v, 16);
+            __builtin_memcpy(&tile[part][to + lane * 16], &v, 16);
         }
     };
     auto ask_scales = [&](int t) {
@@ -376,23 +387,26 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
             }
         }
     };
-    v4f acc[MT][NT];
+    v16f acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-    const int r = lane & 15, g = lane >> 4, mine = r * 64 + (g ^ (r >> 2)) * 16;
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+    const int r = lane & 31, g = lane >> 5, mine = r * 64 + (2 * g ^ ((r >> 2) & 3)) * 16;
+    constexpr int G = 2 * MT, L = LA + LB;                        // groups of NT products, and loads, of a stage
     v4u fa[4], fb[2][NT];
-    unsigned sa[MT], sb[NT];
-    auto read_a = [&](int part, int i) { return *(const v4u*)&tile[part][(wm * MT + i) * 1024 + mine]; };
-    auto read_b = [&](int part, int j) { return *(const v4u*)&tile[part][BM * 64 + (wn * NT + j) * 1024 + mine]; };
-    // byte g of four words
-    const unsigned low = 0x0c0c0400u + g * 0x0101u, high = 0x04000c0cu + g * 0x01010000u;
-    auto read_scale = [&](int t, int row) {
-        const v4u v = *(const v4u*)&scale[t & 1][row * 16];
-        return __builtin_amdgcn_perm(v[1], v[0], low) | __builtin_amdgcn_perm(v[3], v[2], high);
+    unsigned sa[MT][2], sb[NT][2];
+    auto read_a = [&](int part, int i, int h) { return *(const v4u*)&tile[part][(wm * MT + i) * 2048 + (mine ^ h * 16)]; };
+    auto read_b = [&](int part, int j, int h) { return *(const v4u*)&tile[part][BM * 64 + (wn * NT + j) * 2048 + (mine ^ h * 16)]; };
+    const unsigned two = 0x05040100u + g * 0x02020202u;           // bytes 2 g and 2 g + 1 of two words
+    auto read_scale = [&](int t, int row) { return *(const v4u*)&scale[t & 1][row * 16]; };
+    auto spread = [&](const v4u& v, unsigned (&to)[2]) {
+        to[0] = __builtin_amdgcn_perm(v[1], v[0], two);
+        to[1] = __builtin_amdgcn_perm(v[3], v[2], two);
     };
-    const int row_a = wm * MT * 16 + r, row_b = BM + wn * NT * 16 + r;
+    const int row_a = wm * MT * 32 + r, row_b = BM + wn * NT * 32 + r;
     if (s0 < s1) {
         const int t0 = s0 / 4;
         ask_scales(t0);
@@ -401,65 +415,93 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
         for (int s = s0; s < s0 + 3; ++s) {
             if (s >= whole && s < s1) fill(s, s & 3);
 #pragma unroll
-            for (int j = 0; j < LA + LB; ++j) ask(s, s & 3, j);
+            for (int j = 0; j < L; ++j) ask(s, s & 3, j);
         }
-        loads_left_and_barrier<2 * (LA + LB)>();
-        fa[0] = read_a(s0 & 3, 0);
-        fa[1] = read_a(s0 & 3, 1);
-        auto begin = [&](auto odd) {
+        loads_left_and_barrier<2 * L>();
+        fa[0] = read_a(s0 & 3, 0, 0);
+        fa[1] = read_a(s0 & 3, 1, 0);
 #pragma unroll
-            for (int j = 0; j < NT; ++j) fb[odd.value][j] = read_b(s0 & 3, j);
-        };
-        if (COLS && (s0 & 1)) begin(Int<1>{}); else begin(Int<0>{});
+        for (int j = 0; j < NT; ++j) fb[0][j] = read_b(s0 & 3, j, 0);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) sa[i] = read_scale(t0, row_a + i * 16);
+        for (int i = 0; i < MT; ++i) spread(read_scale(t0, row_a + i * 32), sa[i]);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) sb[j] = read_scale(t0, row_b + j * 16);
+        for (int j = 0; j < NT; ++j) spread(read_scale(t0, row_b + j * 32), sb[j]);
         // Stage s = 4 t + U.  False: there is no such stage.
-        auto stage = [&](int t, auto step) {
-            constexpr int U = step.value, now = U & 1, then = now ^ 1;
+        auto stage = [&](int t, auto number) {
+            constexpr int U = number.value;
             const int s = 4 * t + U;
-            if (COLS && s < s0) return true;
+            if (s < s0) return true;
             if (s >= s1) return false;
-            loads_left_and_barrier<LA + LB>();
+            loads_left_and_barrier<L>();
             if (U == 0 && t > t0) ask_scales(t + 1);
             if (s + 3 >= whole && s + 3 < s1) fill(s + 3, (U + 3) & 3);
-            unsigned na[MT], nb[NT];
+            v4u raw[MT + NT];
+            // Between two products one read of the LDS or one load: a product takes 32 cycles, in whose shadow the others are issued.
+            auto group = [&](auto which) {
+                constexpr int q = which.value, h = q / MT, i = q % MT, ahead = q + 2, J0 = i * NT / MT, J1 = (i + 1) * NT / MT;
+                auto between = [&](auto slot) {
+                    constexpr int n = slot.value;                 // 0: a's rows of two groups ahead; then b's of the next step, this group's loads, and scales
+                    if constexpr (n == 0) {
+                        fa[ahead & 3] = ahead < G ? read_a(U, ahead % MT, ahead / MT) : read_a((U + 1) & 3, ahead - G, 0);
+                    } else if constexpr (n <= J1 - J0) {
+                        fb[h ^ 1][J0 + n - 1] = h == 0 ? read_b(U, J0 + n - 1, 1) : read_b((U + 1) & 3, J0 + n - 1, 0);
+                    } else if constexpr (n == J1 - J0 + 1) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                if (i < LA + LB) ask(s + 3, (U + 3) & 3, i);
-                fa[(i + 2) & 3] = i + 2 < MT ? read_a(U, i + 2) : read_a((U + 1) & 3, i + 2 - MT);
-                if (i < NT) fb[then][i] = read_b((U + 1) & 3, i);
-                if (U == 3) {
-                    na[i] = read_scale(t + 1, row_a + i * 16);
-                    if (i < NT) nb[i] = read_scale(t + 1, row_b + i * 16);
-                }
+                        for (int j = q * L / G; j < (q + 1) * L / G; ++j) ask(s + 3, (U + 3) & 3, j);
+                    } else if constexpr (U == 3) {
+                        if constexpr (h == 0) raw[i] = read_scale(t + 1, row_a + i * 32);
+                        else
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = mma4<U>(fb[now][j], fa[i & 3], acc[i][j], sb[j], sa[i]);
-                __builtin_amdgcn_sched_barrier(0);
+                            for (int j = J0; j < J1; ++j) raw[MT + j] = read_scale(t + 1, row_b + j * 32);
+                    }
+                };
+                auto product = [&](auto jj) {
+                    constexpr int j = jj.value;
+                    acc[i][j] = mma4_32<(U & 1) * 2 + h>(fb[h][j], fa[q & 3], acc[i][j], sb[j][U / 2], sa[i][U / 2]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    between(Int<j>{});
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                product(Int<0>{});
+                product(Int<1>{});
+                product(Int<2>{});
+                product(Int<3>{});
+            };
+            group(Int<0>{});
+            group(Int<1>{});
+            group(Int<2>{});
+            group(Int<3>{});
+            if constexpr (G == 8) {
+                group(Int<4>{});
+                group(Int<5>{});
+                group(Int<6>{});
+                group(Int<7>{});
             }
             if (U == 3) {
 #pragma unroll
-                for (int i = 0; i < MT; ++i) sa[i] = na[i];
+                for (int i = 0; i < MT; ++i) spread(raw[i], sa[i]);
 #pragma unroll
-                for (int j = 0; j < NT; ++j) sb[j] = nb[j];
+                for (int j = 0; j < NT; ++j) spread(raw[MT + j], sb[j]);
             }
             return true;
         };
-        static_assert(NT <= MT && MT % 4 == 0, "");
+        static_assert(G == 4 || G == 8, "");
         for (int t = t0; stage(t, Int<0>{}) && stage(t, Int<1>{}) && stage(t, Int<2>{}) && stage(t, Int<3>{}); ++t) {}
     }
     OUT* out = (OUT*)P.out + (COLS ? group * P.out_group : 0);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        const int64_t row = i0 + (wm * MT + i) * 16 + r;
+        const int64_t row = i0 + (wm * MT + i) * 32 + r;
         if (row >= i_end) continue;
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            const int64_t col = j0 + (wn * NT + j) * 16 + g * 4;
-            if (col >= P.n) continue;
-            store_four(out + row * P.ldo + col, acc[i][j], (int)(P.n - col < 4 ? P.n - col : 4));
-        }
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t col = j0 + (wn * NT + j) * 32 + q * 8 + g * 4;
+                if (col >= P.n) continue;
+                const v4f v = {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+                store_four(out + row * P.ldo + col, v, (int)(P.n - col < 4 ? P.n - col : 4));
+            }
     }
 }
 
