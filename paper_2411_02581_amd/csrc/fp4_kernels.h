@@ -255,7 +255,7 @@ __global__ __launch_bounds__(256) void k_fp4_product64(Product4 P) {
 }
 
 // Sixteen bytes a lane from memory straight into the LDS, lane after lane behind `to`, which a wave has in common: from a base that it has in common and a
-// lane's offset, or from a lane's address.  Nothing but the counter of loads says when they are there: whoever reads the LDS waits for it (see loads_left).
+// lane's offset, or from a lane's address.  Nothing but the counter of loads says when they are there: whoever reads the LDS waits for it (left_and_barrier).
 __device__ __forceinline__ void dma16(const uint8_t* base, unsigned off, unsigned to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
 }
@@ -268,9 +268,9 @@ __device__ __forceinline__ const uint8_t* scalar(const uint8_t* p) {
     const unsigned low = __builtin_amdgcn_readfirstlane((unsigned)v), high = __builtin_amdgcn_readfirstlane((unsigned)(v >> 32));
     return (const uint8_t*)((uint64_t)high << 32 | low);
 }
-// At most N of the wave's loads are still under way, none of its reads of the LDS is, and all waves of the workgroup are here.
-template <int N> __device__ __forceinline__ void loads_left_and_barrier() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+// At most N of the wave's loads and M of its reads of the LDS are still under way, and all waves of the workgroup are here.
+template <int N, int M> __device__ __forceinline__ void left_and_barrier() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)\n\ts_barrier" ::"n"(N), "n"(M) : "memory");
 }
 
 // The large form: a tile of BM x BN, four waves, stages of 128 of the length through four parts of the LDS.  While a stage is multiplied, the next
@@ -396,6 +396,8 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
             for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
     const int r = lane & 31, g = lane >> 5, mine = r * 64 + (2 * g ^ ((r >> 2) & 3)) * 16;
     constexpr int G = 2 * MT, L = LA + LB;                        // groups of NT products, and loads, of a stage
+    // reads that a stage does behind its last one of its own rows (they come back in order): those of the next stage's rows
+    constexpr int LATE = G == 8 ? 5 : 6;
     v4u fa[4], fb[2][NT];
     unsigned sa[MT][2], sb[NT][2];
     auto read_a = [&](int part, int i, int h) { return *(const v4u*)&tile[part][(wm * MT + i) * 2048 + (mine ^ h * 16)]; };
@@ -417,7 +419,7 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
 #pragma unroll
             for (int j = 0; j < L; ++j) ask(s, s & 3, j);
         }
-        loads_left_and_barrier<2 * L>();
+        left_and_barrier<2 * L, 0>();
         fa[0] = read_a(s0 & 3, 0, 0);
         fa[1] = read_a(s0 & 3, 1, 0);
 #pragma unroll
@@ -432,7 +434,7 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
             const int s = 4 * t + U;
             if (s < s0) return true;
             if (s >= s1) return false;
-            loads_left_and_barrier<L>();
+            left_and_barrier<L, LATE>();
             if (U == 0 && t > t0) ask_scales(t + 1);
             if (s + 3 >= whole && s + 3 < s1) fill(s + 3, (U + 3) & 3);
             v4u raw[MT + NT];
@@ -488,20 +490,51 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
         static_assert(G == 4 || G == 8, "");
         for (int t = t0; stage(t, Int<0>{}) && stage(t, Int<1>{}) && stage(t, Int<2>{}) && stage(t, Int<3>{}); ++t) {}
     }
+    // The result goes through the LDS, a wave's own part of it, so that a store takes whole pieces of 256 or 512 bytes of a row: a lane's four neighbours
+    // alone are 8 or 16 bytes of 32 rows (16384 x 8192 columns in bf16 then took 125 us beside the products).  A row's sixteen number c lies at place c xor
+    // the row's number.
+    constexpr int SZ = (int)sizeof(OUT), CH = NT * 32 * SZ / 16, IP = SZ == 2 ? MT : MT / 2, REGION = IP * 32 * CH * 16;
+    static_assert(W * REGION <= 4 * PART, "");
+    left_and_barrier<0, 0>();
+    uint8_t* own = &tile[0][0] + w * REGION;
     OUT* out = (OUT*)P.out + (COLS ? group * P.out_group : 0);
+    const bool wide = (((uintptr_t)P.out | (uintptr_t)(P.ldo * SZ) | (uintptr_t)(COLS ? P.out_group * SZ : 0)) & 15) == 0;
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int64_t row = i0 + (wm * MT + i) * 32 + r;
-        if (row >= i_end) continue;
+    for (int i1 = 0; i1 < MT; i1 += IP) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int i = 0; i < IP; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int64_t col = j0 + (wn * NT + j) * 32 + q * 8 + g * 4;
-                if (col >= P.n) continue;
-                const v4f v = {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
-                store_four(out + row * P.ldo + col, v, (int)(P.n - col < 4 ? P.n - col : 4));
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const v16f& c = acc[i1 + i][j];
+                    uint8_t* row = own + (i * 32 + r) * CH * 16;
+                    if constexpr (SZ == 2)
+                        *(v2u*)(row + ((j * 4 + q) ^ (r & 15)) * 16 + g * 8) = v2u{(unsigned)to_bf16(c[q * 4]) | (unsigned)to_bf16(c[q * 4 + 1]) << 16,
+                                                                                  (unsigned)to_bf16(c[q * 4 + 2]) | (unsigned)to_bf16(c[q * 4 + 3]) << 16};
+                    else
+                        *(v4f*)(row + ((j * 8 + q * 2 + g) ^ r) * 16) = v4f{c[q * 4], c[q * 4 + 1], c[q * 4 + 2], c[q * 4 + 3]};
+                }
+        wave_lds_done();
+#pragma unroll 4
+        for (int k = 0; k < IP * 32 * CH / 64; ++k) {
+            const int at_row = k * (64 / CH) + lane / CH, c = lane % CH;
+            const v4u v = *(const v4u*)(own + at_row * CH * 16 + (c ^ (at_row & (CH - 1))) * 16);
+            const int64_t row = i0 + (wm * MT + i1) * 32 + at_row, col = j0 + wn * NT * 32 + c * (16 / SZ);
+            if (row >= i_end || col >= P.n) continue;
+            OUT* to = out + row * P.ldo + col;
+            if (wide && P.n - col >= 16 / SZ) {
+                *(v4u*)to = v;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16 / SZ; ++e)
+                    if (col + e < P.n) {
+                        if constexpr (SZ == 2) ((unsigned short*)to)[e] = (unsigned short)(v[e >> 1] >> (16 * (e & 1)));
+                        else ((unsigned*)to)[e] = v[e];
+                    }
             }
+        }
+        wave_lds_done();
     }
 }
 
