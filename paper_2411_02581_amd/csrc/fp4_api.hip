@@ -115,14 +115,49 @@ bool product_large(const Product4& P, bool cols) {
            grid_fits((mt * nt + 8) * (cols ? P.groups : 1), 256) && P.n > 64 && (cols || P.k >= kBlock);
 }
 
-int launch_product(const Product4& P, bool cols, int out_type, void* stream) {
-    if (product_large(P, cols)) {
-        with_type(out_type, [&](auto* o) {
-            using O = Pointee<decltype(o)>;
-            with_bool(cols, [&](auto cl) { launch_tiles<256, 256, 2, 2, cl.value != 0, O>(P, stream); });
-        });
-        return launched();
+// Whether tiles of 256 x 256 fill the device: with fewer than a tile for each compute unit, or groups that are mostly shorter than one, tiles of 128 x 256
+// are faster.  256 x 256 / 128 x 256, us a call, 4096 x 4096 weights: 512 rows 28 / 20, 1024 rows 30 / 22, 2048 rows 33 / 28, 4096 rows 43 / 51; 64 groups,
+// 3584 x 4096: 4096 rows 156 / 136, 8192 rows 172 / 149, 16384 rows 212 / 257; by columns, 2048 x 2048 of 2048 rows 21 / 15, 16 groups of it 63 / 73.
+bool product_fills(const Product4& P, bool cols) {
+    return ceil_div(P.m, 256) * ceil_div(P.n, 256) * (cols ? P.groups : 1) >= 256 && (cols || P.m >= 192 * (int64_t)P.groups);
+}
+
+// Few rows: tiles for which the waves of a workgroup share the length.  Which of them, and whether: the tiles of one group are one round of workgroups.
+// 4096 x 4096, us a call, this form / tiles of 256 x 256: 1 row 6.5 / 25, 16 rows 6.8 / 25, 64 rows 12 / 25, 128 rows 14.5 / 26, 256 rows 20 / 26, 512 rows 37 / 28;
+// 16 groups, 2816 x 2048: 32 rows 17 / 21, 96 rows 18 / 21, 256 rows 20 / 21, and 2048 x 1408: 96 rows 8 / 19.
+template <class F> bool product_thin(const Product4& P, F rows) {
+    if (!product_wide(P) || ceil_div(P.m, 16) + P.groups > kMaxGridY || ceil_div(P.n, 16) > kMaxRows / 512) return false;
+    if (P.groups > 1) {
+        if (P.m > 16 * (int64_t)P.groups) return false;
+        rows(Int<1>{}, Int<2>{}, Int<4>{});
+        return true;
     }
+    if (P.m <= 16) rows(Int<1>{}, Int<1>{}, Int<8>{});
+    else if (P.m <= 32) rows(Int<2>{}, Int<1>{}, Int<8>{});
+    else if (P.m <= 48) rows(Int<3>{}, Int<1>{}, Int<8>{});
+    else if (P.m <= 64) rows(Int<4>{}, Int<1>{}, Int<8>{});
+    else if (ceil_div(P.m, 64) * ceil_div(P.n, 32) <= 256) rows(Int<4>{}, Int<2>{}, Int<8>{});
+    else if (ceil_div(P.m, 64) * ceil_div(P.n, 64) <= 256) rows(Int<4>{}, Int<4>{}, Int<8>{});
+    else return false;
+    return true;
+}
+
+int launch_product(const Product4& P, bool cols, int out_type, void* stream) {
+    bool done = false;
+    with_type(out_type, [&](auto* o) {
+        using O = Pointee<decltype(o)>;
+        done = !cols && product_thin(P, [&](auto mt, auto nt, auto w) {
+            const dim3 grid((unsigned)ceil_div(P.n, 16 * nt.value), (unsigned)(ceil_div(P.m, 16 * mt.value) + P.groups - 1));
+            LAUNCH((k_fp4_product_thin<O, mt.value, nt.value, w.value>), grid, w.value * 64, P);
+        });
+        if (done || !product_large(P, cols)) return;
+        done = true;
+        with_bool(cols, [&](auto cl) {
+            if (product_fills(P, cols)) launch_tiles<256, 256, 2, 2, cl.value != 0, O>(P, stream);
+            else launch_tiles<128, 256, 2, 2, cl.value != 0, O>(P, stream);
+        });
+    });
+    if (done) return launched();
     const int64_t nt = ceil_div(P.n, 64), mt = cols ? ceil_div(P.m, 64) : ceil_div(P.m, 64) + P.groups - 1;
     if (!grid_fits(mt, 256)) return TUNA_ERR_TOO_LARGE;
     const dim3 grid((unsigned)mt, (unsigned)nt, cols ? P.groups : 1);

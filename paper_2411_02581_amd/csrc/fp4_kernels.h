@@ -281,8 +281,8 @@ template <int N, int M> __device__ __forceinline__ void left_and_barrier() {
 // The waves: WM x WN, 32 MT by 32 NT each; a stage is two steps of 64, in which lane (r, g) has block number 2 g + step of row r.
 template <bool COLS, class OUT, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles, int n_tiles) {
-    constexpr int W = 4, MT = BM / (32 * WM), NT = BN / (32 * WN), LA = BM / 16 / W, LB = BN / 16 / W, LS = (BM + BN) / 64 / W, PART = (BM + BN) * 64;
-    static_assert(WM * WN == W && LA * 16 * W == BM && LB * 16 * W == BN && LS * 64 * W == BM + BN && BM % 64 == 0 && MT % 2 == 0 && NT == 4, "");
+    constexpr int W = 4, MT = BM / (32 * WM), NT = BN / (32 * WN), LA = BM / 16 / W, LB = BN / 16 / W, LS = ((BM + BN) / 64 + W - 1) / W, PART = (BM + BN) * 64;
+    static_assert(WM * WN == W && LA * 16 * W == BM && LB * 16 * W == BN && BM % 64 == 0 && BN % 64 == 0 && MT % 2 == 0 && NT == 4, "");
     __shared__ __align__(1024) uint8_t tile[4][PART];
     __shared__ __align__(1024) uint8_t scale[2][(BM + BN) * 16];
     __shared__ __align__(1024) uint8_t nowhere[W][1024];          // where loads go that ask for no stage
@@ -341,7 +341,8 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
 #pragma unroll
     for (int j = 0; j < LS; ++j) {
         const int r = (w * LS + j) * 64 + lane;
-        if (r < BM) at_s[j] = P.as + (i0 + (r < rows_a ? r : rows_a - 1)) * P.ld_as;
+        if (r >= BM + BN) at_s[j] = P.as;                         // (no row: not asked for)
+        else if (r < BM) at_s[j] = P.as + (i0 + (r < rows_a ? r : rows_a - 1)) * P.ld_as;
         else at_s[j] = P.bs + (COLS ? 0 : group * P.bs_group) + (j0 + (r - BM < rows_b ? r - BM : rows_b - 1)) * P.ld_bs;
     }
     auto place = [&](int j) { return j < LA ? (w * LA + j) * 1024 : BM * 64 + (w * LB + j - LA) * 1024; };
@@ -373,10 +374,12 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
         const int64_t there = (COLS ? (int64_t)s1 * 4 : (P.k + kBlock4 - 1) / kBlock4) - (int64_t)t * 16;
         if (there >= 16) {
 #pragma unroll
-            for (int j = 0; j < LS; ++j) dma16(at_s[j] + (int64_t)t * 16, lds_scale + (t & 1) * (BM + BN) * 16 + (w * LS + j) * 1024);
+            for (int j = 0; j < LS; ++j)
+                if ((w * LS + j) * 64 < BM + BN) dma16(at_s[j] + (int64_t)t * 16, lds_scale + (t & 1) * (BM + BN) * 16 + (w * LS + j) * 1024);
         } else {
 #pragma unroll
             for (int j = 0; j < LS; ++j) {
+                if ((w * LS + j) * 64 >= BM + BN) break;
                 v4u v = {0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
 #pragma unroll 1
                 for (int i = 0; i < there; ++i) {
@@ -450,7 +453,8 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
                     } else if constexpr (n == J1 - J0 + 1) {
 #pragma unroll
                         for (int j = q * L / G; j < (q + 1) * L / G; ++j) ask(s + 3, (U + 3) & 3, j);
-                    } else if constexpr (U == 3) {
+                    }
+                    if constexpr (U == 3 && n == NT - 1) {
                         if constexpr (h == 0) raw[i] = read_scale(t + 1, row_a + i * 32);
                         else
 #pragma unroll
@@ -535,6 +539,73 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
             }
         }
         wave_lds_done();
+    }
+}
+
+// The form for few rows, which reads the weights once and little else: a workgroup has 16 NT rows of b and 16 MT rows of a, its W waves share the length
+// in units of 128, operands go from memory to registers, and the waves' sums are added up in their order.
+template <class OUT, int MT, int NT, int W>
+__global__ __launch_bounds__(W * 64) void k_fp4_product_thin(Product4 P) {
+    constexpr int T = MT * NT, AHEAD = T > 4 ? 2 : 3;
+    __shared__ v4f sums[W][T][64];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Place pl = find_tile(P.group_rows, P.groups, P.m, 16 * MT, blockIdx.y);
+    if (pl.group < 0) return;
+    const int group = __builtin_amdgcn_readfirstlane(pl.group);
+    const int64_t i0 = pl.first, i_end = pl.end, j0 = (int64_t)blockIdx.x * (16 * NT);
+    const int r = lane & 15, g = lane >> 4;
+    const uint8_t *a[MT], *as[MT], *b[NT], *bs[NT];
+#pragma unroll
+    for (int s = 0; s < MT; ++s) {
+        const int64_t row = i0 + s * 16 + r < i_end ? i0 + s * 16 + r : i_end - 1;
+        a[s] = P.a + row * P.lda;
+        as[s] = P.as + row * P.ld_as;
+    }
+#pragma unroll
+    for (int s = 0; s < NT; ++s) {
+        const int64_t row = j0 + s * 16 + r < P.n ? j0 + s * 16 + r : P.n - 1;
+        b[s] = P.b + group * P.b_group + row * P.ldb;
+        bs[s] = P.bs + group * P.bs_group + row * P.ld_bs;
+    }
+    v4f acc[MT][NT];
+#pragma unroll
+    for (int s = 0; s < MT; ++s)
+#pragma unroll
+        for (int q = 0; q < NT; ++q) acc[s][q] = v4f{0.f, 0.f, 0.f, 0.f};
+    struct Ahead { v4u a[MT], b[NT]; unsigned sa[MT], sb[NT]; };
+    auto fetch = [&](Ahead& t, int64_t kb, auto full) {
+        const int64_t blk = kb * 4 + g, left = P.k - blk * kBlock4;
+        auto row = [&](const uint8_t* p) { return full.value ? *(const v4u*)(p + blk * 16) : chunk32<true>(p + blk * 16, left); };
+        auto one = [&](const uint8_t* p) { return full.value || left > 0 ? (unsigned)p[blk] : 127u; };
+#pragma unroll
+        for (int s = 0; s < NT; ++s) { t.b[s] = row(b[s]); t.sb[s] = one(bs[s]); }
+#pragma unroll
+        for (int s = 0; s < MT; ++s) { t.a[s] = row(a[s]); t.sa[s] = one(as[s]); }
+    };
+    auto use = [&](const Ahead& t) {
+#pragma unroll
+        for (int s = 0; s < MT; ++s)
+#pragma unroll
+            for (int q = 0; q < NT; ++q) acc[s][q] = mma4<0>(t.b[q], t.a[s], acc[s][q], t.sb[q], t.sa[s]);
+    };
+    const int whole = (int)(P.k / kBlock), units = (whole - w + W - 1) / W;
+    Ahead st[AHEAD];
+    pipeline<AHEAD, false>(st, 0, units, [&](Ahead& t, int u) { fetch(t, (int64_t)u * W + w, Int<1>{}); }, [&](const Ahead& t, int) { use(t); });
+    if (whole * (int64_t)kBlock < P.k && whole % W == w) {
+        fetch(st[0], whole, Int<0>{});
+        use(st[0]);
+    }
+#pragma unroll
+    for (int s = 0; s < MT; ++s)
+#pragma unroll
+        for (int q = 0; q < NT; ++q) sums[w][s * NT + q][lane] = acc[s][q];
+    __syncthreads();
+    for (int t = w; t < T; t += W) {
+        v4f v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < W; ++q) v += sums[q][t][lane];
+        const int64_t row = i0 + t / NT * 16 + r, col = j0 + t % NT * 16 + g * 4;
+        if (row < i_end && col < P.n) store_four((OUT*)P.out + row * P.ldo + col, v, (int)(P.n - col < 4 ? P.n - col : 4));
     }
 }
 
