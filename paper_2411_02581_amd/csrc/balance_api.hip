@@ -9,18 +9,16 @@ namespace {
 constexpr int64_t kMostTokens = (int64_t)1 << 28;
 
 struct BalanceSizes {
-    int64_t tiles; int parts;
-    size_t counts, live, terms, bytes;                // offsets; the shares' sums come first
+    int64_t tiles;
+    size_t counts, live, bytes;                       // offsets; the shares' sums come first
 };
 
 BalanceSizes balance_sizes(int64_t n, int experts, int groups) {
     BalanceSizes b;
     b.tiles = ceil_div(n, kBalanceTile) + groups - 1;
-    b.parts = (int)ceil_div(experts, 64);
     size_t at = align16((size_t)b.tiles * experts * 4);
     b.counts = at; at += align16((size_t)b.tiles * experts * 4);
     b.live = at; at += align16((size_t)b.tiles * 4);
-    b.terms = at; at += (size_t)groups * b.parts * 16;
     b.bytes = at;
     return b;
 }
@@ -64,19 +62,22 @@ int tuna_moe_balance(const void* logits, int type, int64_t ld, int64_t n_tokens,
     if (rc != TUNA_OK) return rc;
     char* ws = (char*)workspace;
     const Balance B = {logits, ld, n_tokens, n_experts, experts, k, group_rows, groups, counts, tokens, shares, loss,
-                       (float*)ws, (int32_t*)(ws + s.counts), (int32_t*)(ws + s.live), (double*)(ws + s.terms)};
-    // every kernel reads what those before it have written: none is launched behind one that was not
-    int e;
+                       (float*)ws, (int32_t*)(ws + s.counts), (int32_t*)(ws + s.live)};
+    // Up to a tile of one sequence: one workgroup and one launch for everything.
+    const bool all = groups == 1 && !group_rows && n_tokens > 0 && n_tokens <= kBalanceTile;
     if (n_tokens > 0) {
         with_type(type, [&](auto* t) {
             using T = Pointee<decltype(t)>;
-            held(n_experts, [&](auto per) { LAUNCH((k_balance_part<T, per.value>), dim3((unsigned)s.tiles), 1024, B); });
+            held(n_experts, [&](auto per) {
+                if (all) LAUNCH((k_balance_part<T, per.value, true>), dim3(1), 1024, B);
+                else LAUNCH((k_balance_part<T, per.value, false>), dim3((unsigned)s.tiles), 1024, B);
+            });
         });
-        if ((e = launched()) != TUNA_OK) return e;
+        // the next kernel reads what this one has written: it is not launched behind one that was not
+        const int e = launched();
+        if (all || e != TUNA_OK) return e;
     }
-    LAUNCH(k_balance_join, dim3(groups, s.parts), 256, B);
-    if ((e = launched()) != TUNA_OK) return e;
-    LAUNCH(k_balance_loss, dim3((unsigned)ceil_div(groups, 256)), 256, B, s.parts);
+    held(n_experts, [&](auto per) { LAUNCH((k_balance_join<per.value>), dim3(groups), 1024, B); });
     return launched();
 }
 

@@ -12,42 +12,67 @@ struct Balance {
     const int32_t* chosen; int k;
     const int32_t* group_rows; int groups;
     int32_t* counts; int32_t* live; float* shares; float* loss;
-    // workspace: what each tile has of every expert, [tiles, experts] each, and its tokens with an eligible expert; C and the loss's sum of 64 experts
-    float* part; int32_t* part_count; int32_t* part_live; double* terms;
+    // workspace: what each tile has of every expert, [tiles, experts] each, and its tokens with an eligible expert
+    float* part; int32_t* part_count; int32_t* part_live;
 };
 
-// A token's softmax by a wave: lane i holds the experts i, i + 64, ...; false where no logit is eligible (all shares are 0 then).
-template <class T, int PER> __device__ __forceinline__ bool shares_of(const T* row, int n_experts, int lane, float (&p)[PER]) {
-    unsigned top = 0;
+// A token's logits in a wave: lane i holds the experts i, i + 64, ...; one that is NaN or does not exist is -inf.
+template <class T, int PER> __device__ __forceinline__ void load_logits(const T* row, int n_experts, int lane, float (&v)[PER]) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int e = i * 64 + lane;
-        p[i] = e < n_experts ? load1(row + e) : -__builtin_inff();
-        const unsigned key = logit_key(p[i]);
-        top = key > top ? key : top;
+        v[i] = e < n_experts ? load1(row + e) : -__builtin_inff();
     }
-    top = wave_max(top);
-    const float most = key_logit(top);
-    float sum = 0.f;
+}
+
+// Their softmax in their place; false where no logit is eligible (all shares are 0 then).
+template <int PER> __device__ __forceinline__ bool shares_of(float (&v)[PER]) {
+    float most = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        p[i] = top ? exp_share(p[i], most) : 0.f;
-        sum += p[i];
+        v[i] = v[i] == v[i] ? v[i] : -__builtin_inff();
+        most = fmaxf(most, v[i]);
+    }
+    const unsigned top = wave_max(logit_key(most));
+    most = key_logit(top);
+    float sum = 0.f;
+    if (most == __builtin_inff()) {                               // they share the whole equally
+#pragma unroll
+        for (int i = 0; i < PER; ++i) { v[i] = v[i] == most ? 1.f : 0.f; sum += v[i]; }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) { v[i] = top ? exp_32(v[i] - most) : 0.f; sum += v[i]; }
     }
     sum = wave_total(sum);
     const float inverse = top ? 1.f / sum : 0.f;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) p[i] *= inverse;
+    for (int i = 0; i < PER; ++i) v[i] *= inverse;
     return top != 0;
 }
 
-// One workgroup per tile of a sequence: sixteen waves add up their tokens' shares, then the waves' sums are added in their order.
-template <class T, int PER>
+// A workgroup's sums of every expert's 64 bits and counts: the loss.
+__device__ __forceinline__ void balance_loss(const Balance& B, int64_t g, double both, double all, double (&part)[2][16]) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    for (int d = 32; d; d >>= 1) { both += __shfl_xor(both, d); all += __shfl_xor(all, d); }
+    if (lane == 0) { part[0][w] = both; part[1][w] = all; }
+    __syncthreads();
+    if (threadIdx.x) return;
+    both = all = 0;
+    for (int q = 0; q < 16; ++q) { both += part[0][q]; all += part[1][q]; }
+    B.loss[g] = all > 0 ? (float)(B.experts * both / all) : 0.f;
+}
+
+// One workgroup per tile of a sequence: sixteen waves add up their tokens' shares, the logits of up to four under way together, then the waves' sums are
+// added in their order.  ALL: the tile is the whole batch, one sequence, and the sums are the results.  65536 x 256 in 32 bits, 37 sequences: 67 MB.
+template <class T, int PER, bool ALL>
 __global__ __launch_bounds__(1024) void k_balance_part(Balance B) {
+    constexpr int U = PER <= 4 ? 4 : PER == 8 ? 2 : 1;
     __shared__ float sums[16][PER * 64];
     __shared__ int count[PER * 64];
     __shared__ int live[16];
-    const Place pl = find_tile(B.group_rows, B.groups, B.tokens, kBalanceTile, blockIdx.x);
+    __shared__ double terms[2][16];
+    Place pl = {0, 0, B.tokens, 0};
+    if (!ALL) pl = find_tile(B.group_rows, B.groups, B.tokens, kBalanceTile, blockIdx.x);
     if (pl.group < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (tid < PER * 64) count[tid] = 0;
@@ -56,11 +81,20 @@ __global__ __launch_bounds__(1024) void k_balance_part(Balance B) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) sum[i] = 0.f;
     int mine = 0;
-    for (int64_t t = pl.first + w; t < pl.end; t += 16) {
-        float p[PER];
-        mine += shares_of<T, PER>((const T*)B.logits + t * B.ld, B.experts, lane, p);
+    for (int64_t t0 = pl.first + w; t0 < pl.end; t0 += 16 * U) {
+        float p[U][PER];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) sum[i] += p[i];
+        for (int u = 0; u < U; ++u) {
+            const int64_t t = t0 + u * 16 < pl.end ? t0 + u * 16 : pl.end - 1;
+            load_logits<T, PER>((const T*)B.logits + t * B.ld, B.experts, lane, p[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (t0 + u * 16 >= pl.end) break;
+            mine += shares_of<PER>(p[u]);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) sum[i] += p[u][i];
+        }
     }
     for (int64_t i = pl.first * B.k + tid; i < pl.end * B.k; i += 1024) {
         const int e = B.chosen[i];
@@ -70,67 +104,64 @@ __global__ __launch_bounds__(1024) void k_balance_part(Balance B) {
     for (int i = 0; i < PER; ++i) sums[w][i * 64 + lane] = sum[i];
     if (lane == 0) live[w] = mine;
     __syncthreads();
+    int n = 0;
+    for (int q = 0; q < 16; ++q) n += live[q];
+    float s = 0.f;                                                // a thread per expert there can be
+    if (tid < B.experts) for (int q = 0; q < 16; ++q) s += sums[q][tid];
+    if (ALL) {
+        const double share = n > 0 ? (double)s / n : 0.;
+        const int c = tid < B.experts ? count[tid] : 0;
+        if (tid < B.experts) {
+            B.counts[tid] = c;
+            B.shares[tid] = (float)share;
+        }
+        if (tid == 0) B.live[0] = n;
+        balance_loss(B, 0, c * share, c, terms);
+        return;
+    }
     const int64_t at = (int64_t)blockIdx.x * B.experts;
-    for (int e = tid; e < B.experts; e += 1024) {
-        float s = 0.f;
-        for (int q = 0; q < 16; ++q) s += sums[q][e];
-        B.part[at + e] = s;
-        B.part_count[at + e] = count[e];
+    if (tid < B.experts) {
+        B.part[at + tid] = s;
+        B.part_count[at + tid] = count[tid];
     }
-    if (tid == 0) {
-        int n = 0;
-        for (int q = 0; q < 16; ++q) n += live[q];
-        B.part_live[blockIdx.x] = n;
-    }
+    if (tid == 0) B.part_live[blockIdx.x] = n;
 }
 
-// A workgroup per sequence and 64 experts: four waves share its tiles, in 64 bits.
-__global__ __launch_bounds__(256) void k_balance_join(Balance B) {
-    __shared__ double sums[4][64];
-    __shared__ int counts[4][64], live[4];
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = blockIdx.x, e = blockIdx.y * 64 + lane;
+// A workgroup per sequence: its sixteen waves are C columns of 64 experts and 16 / C runs of its tiles; sums in 64 bits.
+template <int C>
+__global__ __launch_bounds__(1024) void k_balance_join(Balance B) {
+    constexpr int R = 16 / C;
+    __shared__ double sums[R][C * 64];
+    __shared__ int counts[R][C * 64], live[R];
+    __shared__ double terms[2][16];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), run = w / C, g = blockIdx.x, e = (w % C) * 64 + lane;
     int64_t first, tiles;
     group_blocks(B.group_rows, B.groups, g, B.tokens, first, tiles, kBalanceTile);
     double s = 0;
     int c = 0, n = 0;
-    for (int64_t i = first + w; i < first + tiles; i += 4) {
+#pragma unroll 4
+    for (int64_t i = first + run; i < first + tiles; i += R) {
         if (e < B.experts) {
             s += (double)B.part[i * B.experts + e];
             c += B.part_count[i * B.experts + e];
         }
         n += B.part_live[i];
     }
-    sums[w][lane] = s;
-    counts[w][lane] = c;
-    if (lane == 0) live[w] = n;
+    sums[run][e] = s;
+    counts[run][e] = c;
+    if (lane == 0) live[run] = n;                                 // (the columns' waves have the same)
     __syncthreads();
-    if (w) return;
-    for (int q = 1; q < 4; ++q) { s += sums[q][lane]; c += counts[q][lane]; n += live[q]; }
-    s = n > 0 ? s / n : 0.;
-    if (e < B.experts) {
-        B.counts[(int64_t)g * B.experts + e] = c;
-        B.shares[(int64_t)g * B.experts + e] = (float)s;
+    s = 0;
+    c = n = 0;
+    for (int q = 0; q < R; ++q) n += live[q];
+    if (tid < B.experts) {                                        // a thread per expert
+        for (int q = 0; q < R; ++q) { s += sums[q][tid]; c += counts[q][tid]; }
+        s = n > 0 ? s / n : 0.;
+        B.counts[(int64_t)g * B.experts + tid] = c;
+        B.shares[(int64_t)g * B.experts + tid] = (float)s;
     }
-    double both = c * s, all = c;
-    for (int d = 32; d; d >>= 1) { both += __shfl_xor(both, d); all += __shfl_xor(all, d); }
-    if (lane == 0) {
-        double* to = B.terms + ((int64_t)g * gridDim.y + blockIdx.y) * 2;
-        to[0] = both;
-        to[1] = all;
-        if (blockIdx.y == 0) B.live[g] = n;
-    }
-}
-
-// A thread per sequence.
-__global__ __launch_bounds__(256) void k_balance_loss(Balance B, int parts) {
-    const int g = blockIdx.x * 256 + threadIdx.x;
-    if (g >= B.groups) return;
-    double both = 0, all = 0;
-    for (int i = 0; i < parts; ++i) {
-        both += B.terms[((int64_t)g * parts + i) * 2];
-        all += B.terms[((int64_t)g * parts + i) * 2 + 1];
-    }
-    B.loss[g] = all > 0 ? (float)(B.experts * both / all) : 0.f;
+    if (tid == 0) B.live[g] = n;
+    balance_loss(B, g, c * s, c, terms);
 }
 
 // Every wave has the fractions f_e = counts_e / C of its tile's sequence in registers: dl_i = dloss E / N p_i (f_i - sum over e of f_e p_e).  The tiles behind the
@@ -167,19 +198,30 @@ __global__ __launch_bounds__(256) void k_balance_grad(Balance B, const float* dl
     const float slope = all > 0 && n > 0 ? dloss[pl.group] * ((float)B.experts / (float)n) : 0.f, inverse = all > 0 ? 1.f / (float)all : 0.f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) f[i] *= inverse;
-    for (int64_t t = pl.first + w; t < pl.end; t += 4) {
-        float p[PER];
-        shares_of<T, PER>((const T*)B.logits + t * B.ld, B.experts, lane, p);
-        float dot = 0.f;
+    constexpr int U = PER <= 4 ? 4 : PER == 8 ? 2 : 1;            // tokens whose logits are under way together
+    for (int64_t t0 = pl.first + w; t0 < pl.end; t0 += 4 * U) {
+        float p[U][PER], before[U][PER];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) dot += p[i] * f[i];
-        dot = wave_total(dot);
+        for (int u = 0; u < U; ++u) {
+            const int64_t t = t0 + u * 4 < pl.end ? t0 + u * 4 : pl.end - 1;
+            load_logits<T, PER>((const T*)B.logits + t * B.ld, B.experts, lane, p[u]);
+            if (ADD) load_logits<T, PER>(dlogits + t * ld_d, B.experts, lane, before[u]);
+        }
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = i * 64 + lane;
-            if (e >= B.experts) continue;
-            T* to = dlogits + t * ld_d + e;
-            store1(to, (ADD ? load1(to) : 0.f) + slope * p[i] * (f[i] - dot));
+        for (int u = 0; u < U; ++u) {
+            const int64_t t = t0 + u * 4;
+            if (t >= pl.end) break;
+            shares_of<PER>(p[u]);
+            float dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) dot += p[u][i] * f[i];
+            dot = wave_total(dot);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int e = i * 64 + lane;
+                const float d = slope * p[u][i] * (f[i] - dot);
+                if (e < B.experts) store1(dlogits + t * ld_d + e, ADD ? before[u][i] + d : d);
+            }
         }
     }
 }

@@ -928,18 +928,19 @@ struct Few {
 // every e4m3 exactly.  at(h, part): where the eight number h of lane `part` start.  Every load takes 64 bytes of a row in a piece.  whole(): all of it
 // is inside the row, so that the loads hang on no condition; the address is a wave's base and a lane's 32-bit offset in bytes.
 // row(n): the elements of a row of n values; kUnit: those of a block of 128.  A lane's scales of row r of `rows` of expert e: scales(...) says where the
-// first is, the next block's is kScales behind.  4-bit values take theirs where they are widened (INSIDE: bf16 holds the products), others in 32 bits.
+// first is, the next block's is kScales behind.  kAhead1, kAhead2: blocks that a wave
+// of the first kernel has in registers or on their way, weights and tokens, and of the second, weights and activations.  4-bit values take theirs where they are widened (INSIDE: bf16 holds the products), others in 32 bits.
 struct Four { uint8_t two; };           // two 4-bit values
 template <class W> struct Part;
 template <class W> struct PartBase {
-    static constexpr int kUnit = kBlock, kScales = 1;
+    static constexpr int kUnit = kBlock, kScales = 1, kAhead1 = 3, kAhead2 = 4;
     static constexpr bool INSIDE = false;
     static __device__ __forceinline__ int64_t row(int64_t n) { return n; }
     static __device__ __forceinline__ int64_t scales(int64_t e, int64_t rows, int64_t r, int64_t cols, int) { return (e * blocks_of(rows) + r / kBlock) * blocks_of(cols); }
     static __device__ __forceinline__ int64_t last(int64_t at, int64_t, int, int64_t) { return at; }
 };
 template <> struct Part<Four> {
-    static constexpr int kUnit = kBlock / 2, kScales = kBlock / kBlock4;
+    static constexpr int kUnit = kBlock / 2, kScales = kBlock / kBlock4, kAhead1 = 3, kAhead2 = 4;
     static constexpr bool INSIDE = true;
     v4u v;
     static __device__ __forceinline__ int at(int h, int part) { return part * 32 + h * 8; }
@@ -1001,8 +1002,6 @@ template <int KIND> __device__ __forceinline__ float scale_value(const void* s, 
 
 constexpr int kFewFirst = 4;           // waves of a workgroup of the first kernel: they share the length of the sums
 constexpr int kFewSecond = 8;         // and of the second: they share the experts
-constexpr int kFewAhead1 = 3;          // blocks of 128 that a wave of the first kernel has in registers or on their way: weights and tokens
-constexpr int kFewAhead2 = 4;          // and of the second: weights and activations
 
 // First kernel: a workgroup makes 16 activations, or 64, of one expert (as many rows of the gate half and of the up half) for all tokens that
 // chose it, 16 MT of them at a time.  Bound by reading the weights: 40 tokens, k = 8 of 128 experts, 1536 x 4096: 1.49 GB in 367 us (357), 4.1 TB/s; one
@@ -1176,7 +1175,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
         constexpr int stride = SPLIT ? kFewFirst : 1, skip = SPLIT;
         if constexpr (WIDE) {
             struct Ahead { Part<W> g, u; float kg, ku; v8b a[MT][4]; };
-            Ahead st[kFewAhead1];
+            Ahead st[Wp::kAhead1];
             const int units = (whole - skip * w + stride - 1) / stride;
             auto fetch = [&](Ahead& t, int unit) {
                 const int64_t b = unit * stride + skip * w;
@@ -1186,7 +1185,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
                 t.ku = scale_value<KIND>(F.s1, su + b * Wp::kScales);
                 load_x(t.a, b * kBlock, Int<1>{});
             };
-            pipeline<kFewAhead1, !SPLIT>(st, 0, units, fetch, [&](const Ahead& t, int) { multiply(t.a, t.g, t.u, t.kg, t.ku); });
+            pipeline<Wp::kAhead1, !SPLIT>(st, 0, units, fetch, [&](const Ahead& t, int) { multiply(t.a, t.g, t.u, t.kg, t.ku); });
         }
         for (int64_t b = whole + skip * w; b < nb; b += stride) {
             Part<W> g, u;
@@ -1370,8 +1369,8 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
             load_h(t.a, far.task, far.block * kBlock, Int<1>{});
             step(far);
         };
-        Ahead st[kFewAhead2];
-        pipeline<kFewAhead2, false>(st, lo, hi, fetch, [&](const Ahead& t, int u) {
+        Ahead st[Wp::kAhead2];
+        pipeline<Wp::kAhead2, false>(st, lo, hi, fetch, [&](const Ahead& t, int u) {
             multiply(t.a, t.v, t.k);
             if (u + 1 == hi || now.block + 1 == per) keep(now.task);      // the wave's last of this task
             step(now);
