@@ -4,13 +4,13 @@
 
 namespace moe {
 
-constexpr int kBalanceTile = 256;      // tokens of a sequence that a workgroup adds up
+constexpr int kBalanceTile = 128;      // the most tokens of a sequence that a workgroup adds up
 constexpr int kBalanceGradTile = 32;   // and of which it makes the gradient
 
 struct Balance {
     const void* logits; int64_t ld, tokens; int experts;
     const int32_t* chosen; int k;
-    const int32_t* group_rows; int groups;
+    const int32_t* group_rows; int groups, tile;                  // tile: tokens of a workgroup
     int32_t* counts; int32_t* live; float* shares; float* loss;
     // workspace: what each tile has of every expert, [tiles, experts] each, and its tokens with an eligible expert
     float* part; int32_t* part_count; int32_t* part_live;
@@ -44,7 +44,7 @@ template <int PER> __device__ __forceinline__ bool shares_of(float (&v)[PER]) {
         for (int i = 0; i < PER; ++i) { v[i] = top ? exp_32(v[i] - most) : 0.f; sum += v[i]; }
     }
     sum = wave_total(sum);
-    const float inverse = top ? 1.f / sum : 0.f;
+    const float r = __builtin_amdgcn_rcpf(sum), inverse = top ? __builtin_fmaf(__builtin_fmaf(-sum, r, 1.f), r, r) : 0.f;      // to a unit of the last place
 #pragma unroll
     for (int i = 0; i < PER; ++i) v[i] *= inverse;
     return top != 0;
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(1024) void k_balance_part(Balance B) {
     __shared__ int live[16];
     __shared__ double terms[2][16];
     Place pl = {0, 0, B.tokens, 0};
-    if (!ALL) pl = find_tile(B.group_rows, B.groups, B.tokens, kBalanceTile, blockIdx.x);
+    if (!ALL) pl = find_tile(B.group_rows, B.groups, B.tokens, B.tile, blockIdx.x);
     if (pl.group < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (tid < PER * 64) count[tid] = 0;
@@ -85,8 +85,7 @@ __global__ __launch_bounds__(1024) void k_balance_part(Balance B) {
         float p[U][PER];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t t = t0 + u * 16 < pl.end ? t0 + u * 16 : pl.end - 1;
-            load_logits<T, PER>((const T*)B.logits + t * B.ld, B.experts, lane, p[u]);
+            if (t0 + u * 16 < pl.end) load_logits<T, PER>((const T*)B.logits + (t0 + u * 16) * B.ld, B.experts, lane, p[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -127,19 +126,20 @@ __global__ __launch_bounds__(1024) void k_balance_part(Balance B) {
     if (tid == 0) B.part_live[blockIdx.x] = n;
 }
 
-// A workgroup per sequence: its sixteen waves are C columns of 64 experts and 16 / C runs of its tiles; sums in 64 bits.
-template <int C>
+// A workgroup per sequence: its sixteen waves are C columns of 64 experts and 16 / C runs of its tiles; sums in 64 bits.  WHOLE: that is all experts, and the
+// loss follows; else blockIdx.y counts the columns, and k_balance_loss makes it.
+template <int C, bool WHOLE>
 __global__ __launch_bounds__(1024) void k_balance_join(Balance B) {
     constexpr int R = 16 / C;
     __shared__ double sums[R][C * 64];
     __shared__ int counts[R][C * 64], live[R];
     __shared__ double terms[2][16];
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), run = w / C, g = blockIdx.x, e = (w % C) * 64 + lane;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), run = w / C, g = blockIdx.x, col = (w % C) * 64 + lane, e0 = blockIdx.y * (C * 64), e = e0 + col;
     int64_t first, tiles;
-    group_blocks(B.group_rows, B.groups, g, B.tokens, first, tiles, kBalanceTile);
+    group_blocks(B.group_rows, B.groups, g, B.tokens, first, tiles, B.tile);
     double s = 0;
     int c = 0, n = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t i = first + run; i < first + tiles; i += R) {
         if (e < B.experts) {
             s += (double)B.part[i * B.experts + e];
@@ -147,21 +147,30 @@ __global__ __launch_bounds__(1024) void k_balance_join(Balance B) {
         }
         n += B.part_live[i];
     }
-    sums[run][e] = s;
-    counts[run][e] = c;
+    sums[run][col] = s;
+    counts[run][col] = c;
     if (lane == 0) live[run] = n;                                 // (the columns' waves have the same)
     __syncthreads();
     s = 0;
     c = n = 0;
     for (int q = 0; q < R; ++q) n += live[q];
-    if (tid < B.experts) {                                        // a thread per expert
+    if (tid < C * 64 && e0 + tid < B.experts) {                   // a thread per expert
         for (int q = 0; q < R; ++q) { s += sums[q][tid]; c += counts[q][tid]; }
         s = n > 0 ? s / n : 0.;
-        B.counts[(int64_t)g * B.experts + tid] = c;
-        B.shares[(int64_t)g * B.experts + tid] = (float)s;
+        B.counts[(int64_t)g * B.experts + e0 + tid] = c;
+        B.shares[(int64_t)g * B.experts + e0 + tid] = (float)s;
     }
-    if (tid == 0) B.live[g] = n;
-    balance_loss(B, g, c * s, c, terms);
+    if (tid == 0 && blockIdx.y == 0) B.live[g] = n;
+    if (WHOLE) balance_loss(B, g, c * s, c, terms);
+}
+
+// A workgroup per sequence, from its counts and shares.
+__global__ __launch_bounds__(1024) void k_balance_loss(Balance B) {
+    __shared__ double terms[2][16];
+    const int64_t at = (int64_t)blockIdx.x * B.experts + threadIdx.x;
+    const bool there = (int)threadIdx.x < B.experts;
+    const double c = there ? B.counts[at] : 0, s = there ? B.shares[at] : 0.f;
+    balance_loss(B, blockIdx.x, c * s, c, terms);
 }
 
 // Every wave has the fractions f_e = counts_e / C of its tile's sequence in registers: dl_i = dloss E / N p_i (f_i - sum over e of f_e p_e).  The tiles behind the
@@ -203,7 +212,8 @@ __global__ __launch_bounds__(256) void k_balance_grad(Balance B, const float* dl
         float p[U][PER], before[U][PER];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t t = t0 + u * 4 < pl.end ? t0 + u * 4 : pl.end - 1;
+            const int64_t t = t0 + u * 4;
+            if (t >= pl.end) break;
             load_logits<T, PER>((const T*)B.logits + t * B.ld, B.experts, lane, p[u]);
             if (ADD) load_logits<T, PER>(dlogits + t * ld_d, B.experts, lane, before[u]);
         }

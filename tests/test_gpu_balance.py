@@ -105,6 +105,12 @@ def test_balance_of_sequences(bounds, dtype):
     check(torch.randn(300, 70, generator=gen(1)) * 2, dtype, 4, bounds, ld=77)
 
 
+@pytest.mark.parametrize("t,e,bounds", [(9000, 70, [0, 9000]), (20000, 8, [3, 40, 18000, 19990]), (5000, 130, [0, 5000]), (70000, 6, [0, 70000]), (3000, 600, [0, 3000])])
+def test_balance_of_many_tiles(t, e, bounds):
+    """Sequences that many workgroups add up, in tiles of 16 to 128 tokens."""
+    check(torch.randn(t, e, generator=gen(t)) * 2, "f32", 2, bounds)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_balance_masks(dtype):
     x = torch.randn(90, 70, generator=gen(2))
