@@ -254,20 +254,6 @@ __global__ __launch_bounds__(256) void k_fp4_product64(Product4 P) {
     }
 }
 
-// Sixteen bytes a lane from memory straight into the LDS, lane after lane behind `to`, which a wave has in common: from a base that it has in common and a
-// lane's offset, or from a lane's address.  Nothing but the counter of loads says when they are there: whoever reads the LDS waits for it (left_and_barrier).
-__device__ __forceinline__ void dma16(const uint8_t* base, unsigned off, unsigned to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
-}
-__device__ __forceinline__ void dma16(const uint8_t* from, unsigned to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
-}
-// An address that a wave has in common, as one of its scalars.
-__device__ __forceinline__ const uint8_t* scalar(const uint8_t* p) {
-    const uint64_t v = (uint64_t)p;
-    const unsigned low = __builtin_amdgcn_readfirstlane((unsigned)v), high = __builtin_amdgcn_readfirstlane((unsigned)(v >> 32));
-    return (const uint8_t*)((uint64_t)high << 32 | low);
-}
 // At most N of the wave's loads and M of its reads of the LDS are still under way, and all waves of the workgroup are here.
 template <int N, int M> __device__ __forceinline__ void left_and_barrier() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)\n\ts_barrier" ::"n"(N), "n"(M) : "memory");

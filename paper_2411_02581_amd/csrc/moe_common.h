@@ -336,6 +336,21 @@ template <int BYTES> __device__ __forceinline__ void to_lds(const void* from, vo
     else __builtin_amdgcn_global_load_lds(g, l, 1, 0, 0);
 }
 
+// Sixteen bytes a lane from memory straight into the LDS, lane after lane behind `to`, which a wave has in common: from a base that it has in common and a
+// lane's offset, or from a lane's address.  Nothing but the counter of loads says when they are there: whoever reads the LDS waits for it.
+__device__ __forceinline__ void dma16(const uint8_t* base, unsigned off, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void dma16(const uint8_t* from, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+// An address that a wave has in common, as one of its scalars.
+__device__ __forceinline__ const uint8_t* scalar(const uint8_t* p) {
+    const uint64_t v = (uint64_t)p;
+    const unsigned low = __builtin_amdgcn_readfirstlane((unsigned)v), high = __builtin_amdgcn_readfirstlane((unsigned)(v >> 32));
+    return (const uint8_t*)((uint64_t)high << 32 | low);
+}
+
 // Up to four neighbours of a row of the result, in one store where all exist and lie on their size.
 template <class OUT> __device__ __forceinline__ void store_four(OUT* o, const v4f& v, int n) {
     if (n == 4 && ((uintptr_t)o & (4 * sizeof(OUT) - 1)) == 0) {

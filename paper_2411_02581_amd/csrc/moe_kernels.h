@@ -940,7 +940,7 @@ template <class W> struct PartBase {
     static __device__ __forceinline__ int64_t last(int64_t at, int64_t, int, int64_t) { return at; }
 };
 template <> struct Part<Four> {
-    static constexpr int kUnit = kBlock / 2, kScales = kBlock / kBlock4, kAhead1 = 3, kAhead2 = 4;
+    static constexpr int kUnit = kBlock / 2, kScales = kBlock / kBlock4, kAhead1 = 4, kAhead2 = 6;
     static constexpr bool INSIDE = true;
     v4u v;
     static __device__ __forceinline__ int at(int h, int part) { return part * 32 + h * 8; }
@@ -995,6 +995,21 @@ __device__ __forceinline__ v8b as_bf16(const v4u& a) {
     return r;
 }
 
+// Lane (c, part) of sixteen c holds step c / (16 / P) of the place c mod (16 / P): the places' four steps, each in the lanes of its place.  What the lanes behind
+// them then hold makes rows of a product that nobody reads.
+template <int SHIFT> __device__ __forceinline__ v8b lanes_down(const v8b& a) {
+    v4u v;
+    __builtin_memcpy(&v, &a, 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v[i], 0x100 + SHIFT, 0xf, 0xf, true);
+    return as_bf16(v);
+}
+template <int P> __device__ __forceinline__ void later_steps(const v8b (&from)[4 / P], v8b (&to)[4]) {
+    if constexpr (P == 4) { to[0] = from[0]; to[1] = lanes_down<4>(from[0]); to[2] = lanes_down<8>(from[0]); to[3] = lanes_down<12>(from[0]); }
+    else if constexpr (P == 2) { to[0] = from[0]; to[1] = lanes_down<8>(from[0]); to[2] = from[1]; to[3] = lanes_down<8>(from[1]); }
+    else { to[0] = from[0]; to[1] = from[1]; to[2] = from[2]; to[3] = from[3]; }
+}
+
 template <int KIND> __device__ __forceinline__ float scale_value(const void* s, int64_t i) {
     if (KIND < 0) return 1.f;
     return scale_float<KIND>(scale_at<KIND>(s, i));
@@ -1014,6 +1029,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
     __shared__ int rank_of[TUNA_MOE_FEW_TOKENS];                  // how many come before this expert, or -1: not chosen
     __shared__ int list[TUNA_MOE_FEW_TOKENS];
     __shared__ float sums[SPLIT ? kFewFirst : 1][2][256];
+    __shared__ __align__(1024) uint8_t ring[kFewFirst][WIDE && Part<W>::INSIDE ? Part<W>::kAhead1 : 1][2][1024];
     const int tid = threadIdx.x, lane = tid & 63;
     const bool first = blockIdx.x == 0;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1173,7 +1189,64 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
             }
         };
         constexpr int stride = SPLIT ? kFewFirst : 1, skip = SPLIT;
-        if constexpr (WIDE) {
+        if constexpr (WIDE && Wp::INSIDE) {
+            // The weights go through the LDS, a wave's own part of it: its lanes load whole pieces of rows, where the product's lanes, sixteen rows side by side,
+            // would ask for every sixteen bytes by themselves.  The scales of gate rows and up rows are a word in the lanes 0 to 31.  A wait for the
+            // scales, which are asked for behind the weights, is a wait for these.  Up to 4 (8) tokens: the lanes of places without one load the
+            // tokens' later steps, P = 4 (2) steps in one load.  48 tokens, k = 8 of 128 experts, 1408 x 4096, first kernel: 316 us without all this,
+            // 250 with the weights through the LDS.
+            auto stream = [&](auto packed) {
+                constexpr int P = packed.value;
+                struct Ahead { unsigned k; v8b a[MT][4 / P]; };
+                Ahead st[Wp::kAhead1];
+                const int units = (whole - skip * w + stride - 1) / stride;
+                const unsigned slots = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&ring[w][0][0][0];
+                const int64_t mine = f0 + (lane >> 2) < F.inner ? f0 + (lane >> 2) : F.inner - 1;
+                const unsigned off = (unsigned)(mine * row_w) + ((lane & 3) ^ (lane >> 4)) * 16;
+                const uint8_t* scale_row = (const uint8_t*)F.s1 + (lane & 16 ? su : sg) - part;      // of this lane's column
+                const int place = c * 64 + (part ^ (c >> 2)) * 16;
+                unsigned x_at[MT];                                // this lane's token, and its first value of a block
+#pragma unroll
+                for (int s = 0; s < MT; ++s) {
+                    const int i = t0 + s * 16 + c % (16 / P);
+                    x_at[s] = i < n ? (unsigned)(list[i] * F.ldx) + part * 32 + c / (16 / P) * 8 : ~0u;
+                }
+                auto fetch = [&](Ahead& t, int unit) {
+                    const int64_t b = unit * stride + skip * w;
+                    const unsigned to = slots + (unsigned)unit % Wp::kAhead1 * 2048;
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // what is read of this part of the LDS has been read
+                    dma16(scalar((const uint8_t*)(wg + b * Wp::kUnit)), off, to);
+                    dma16(scalar((const uint8_t*)(wu + b * Wp::kUnit)), off, to + 1024);
+                    t.k = 0;
+                    if (lane < 32) __builtin_memcpy(&t.k, scale_row + b * Wp::kScales, 4);
+#pragma unroll
+                    for (int s = 0; s < MT; ++s) {
+#pragma unroll
+                        for (int q = 0; q < 4 / P; ++q) t.a[s][q] = v8b{};
+                        if (x_at[s] != ~0u) {
+#pragma unroll
+                            for (int q = 0; q < 4 / P; ++q) t.a[s][q] = as_bf16(*(const v4u*)((const uint8_t*)(F.x + b * kBlock + q * P * 8) + (size_t)(x_at[s] * 2)));
+                        }
+                    }
+                };
+                pipeline<Wp::kAhead1, !SPLIT>(st, 0, units, fetch, [&](const Ahead& t, int unit) {
+                    asm volatile("" ::"v"(t.k) : "memory");
+                    const uint8_t* from = ring[w][(unsigned)unit % Wp::kAhead1][0] + place;
+                    Part<W> g, u;
+                    g.v = *(const v4u*)from;
+                    u.v = *(const v4u*)(from + 1024);
+                    const unsigned kg = (unsigned)__shfl((int)t.k, c) >> (part * 8) & 255u, ku = (unsigned)__shfl((int)t.k, 16 + c) >> (part * 8) & 255u;
+                    v8b a[MT][4];
+#pragma unroll
+                    for (int s = 0; s < MT; ++s) later_steps<P>(t.a[s], a[s]);
+                    multiply(a, g, u, scale_float<TUNA_SCALE_E8>(kg), scale_float<TUNA_SCALE_E8>(ku));
+                });
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing is on its way to the LDS when it is used again, or given back
+            };
+            if (ONE || (MT == 1 && n - t0 <= 4)) stream(Int<4>{});
+            else if (MT == 1 && n - t0 <= 8) stream(Int<2>{});
+            else stream(Int<1>{});
+        } else if constexpr (WIDE) {
             struct Ahead { Part<W> g, u; float kg, ku; v8b a[MT][4]; };
             Ahead st[Wp::kAhead1];
             const int units = (whole - skip * w + stride - 1) / stride;
@@ -1236,6 +1309,9 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
 template <class W, int KIND, bool WIDE, class OUT, bool ONE>
 __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
     extern __shared__ float shared[];                             // [kFewSecond][tokens][16] sums
+    constexpr bool RING = WIDE && Part<W>::INSIDE;
+    constexpr int TASK = Part<W>::INSIDE ? 4 : 16;                // pairs of a task
+    __shared__ __align__(1024) uint8_t ring[kFewSecond][RING ? Part<W>::kAhead2 : 1][RING ? 1024 : 16];
     constexpr int PAIRS = TUNA_MOE_FEW_TOKENS * TUNA_MOE_MAX_K;
     __shared__ int pair_of[PAIRS];                                // pairs by expert
     __shared__ float weight[PAIRS];
@@ -1276,15 +1352,15 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
             int tasks = 0, pairs = 0;
             for (int e0 = 0; e0 < F.experts; e0 += 64) {
                 const int cnt = e0 + lane < F.experts ? count_of[e0 + lane] : 0;
-                const int inc = wave_scan(cnt, lane), parts = (cnt + 15) / 16, inc_parts = wave_scan(parts, lane);
+                const int inc = wave_scan(cnt, lane), parts = (cnt + TASK - 1) / TASK, inc_parts = wave_scan(parts, lane);
                 if (cnt > 0) {
                     first_of[e0 + lane] = pairs + inc - cnt;
                     count_of[e0 + lane] = 0;
                     for (int i = 0; i < parts; ++i) {
                         const int at = tasks + inc_parts - parts + i;
                         task_expert[at] = e0 + lane;
-                        task_first[at] = pairs + inc - cnt + i * 16;
-                        task_count[at] = cnt - i * 16 < 16 ? cnt - i * 16 : 16;
+                        task_first[at] = pairs + inc - cnt + i * TASK;
+                        task_count[at] = cnt - i * TASK < TASK ? cnt - i * TASK : TASK;
                     }
                 }
                 tasks += __shfl(inc_parts, 63);
@@ -1355,9 +1431,48 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
         acc = v4f{0.f, 0.f, 0.f, 0.f};
         wave_lds_done();
     };
-    if constexpr (WIDE) {
+    struct Cursor { int task, block; };                           // a place in the sequence
+    if constexpr (RING) {
+        // As in the first kernel: weights through the LDS, a wave's own part of it, scales as a word in the lanes 0 to 15.  A task is up to four pairs, so that one load
+        // of each part of the activations brings all their steps; more pairs of an expert are its next task, whose weights are then near.
+        struct Ahead { unsigned k; v8b x[1], z[1]; };
+        const unsigned slots = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&ring[w][0][0];
+        const int64_t mine = c0 + (lane >> 2) < F.hidden ? c0 + (lane >> 2) : F.hidden - 1, each = Wp::scales(1, F.hidden, 0, F.inner, 0);
+        const unsigned off = (unsigned)(mine * row_w) + ((lane & 3) ^ (lane >> 4)) * 16;
+        const uint8_t* scale_row = (const uint8_t*)F.s2 + Wp::scales(0, F.hidden, col, F.inner, 0);
+        const int place = c * 64 + (part ^ (c >> 2)) * 16;
+        auto step = [&](Cursor& q) { if (++q.block == per) { q.block = 0; ++q.task; } };
+        Cursor now = {per ? lo / per : 0, per ? lo % per : 0}, far = now;
+        auto fetch = [&](Ahead& t, int unit) {
+            const int e = __builtin_amdgcn_readfirstlane(task_expert[far.task]);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // what is read of this part of the LDS has been read
+            dma16(scalar((const uint8_t*)((const W*)F.w2 + (int64_t)e * F.hidden * row_w + far.block * Wp::kUnit)), off, slots + (unsigned)unit % Wp::kAhead2 * 1024);
+            t.k = 0;
+            if (lane < 16) __builtin_memcpy(&t.k, scale_row + e * each + far.block * Wp::kScales, 4);
+            t.x[0] = t.z[0] = v8b{};
+            if ((c & 3) < task_count[far.task]) {
+                const unsigned at = ((unsigned)(pair_of[task_first[far.task] + (c & 3)] * F.ld_h) + part * 32 + (c >> 2) * 8) * 2;
+                t.x[0] = as_bf16(*(const v4u*)((const uint8_t*)(F.hi + far.block * kBlock) + (size_t)at));
+                t.z[0] = as_bf16(*(const v4u*)((const uint8_t*)(F.lo + far.block * kBlock) + (size_t)at));
+            }
+            step(far);
+        };
+        Ahead st[Wp::kAhead2];
+        pipeline<Wp::kAhead2, false>(st, lo, hi, fetch, [&](const Ahead& t, int unit) {
+            asm volatile("" ::"v"(t.k) : "memory");
+            Part<W> v;
+            v.v = *(const v4u*)(ring[w][(unsigned)unit % Wp::kAhead2] + place);
+            const unsigned k = (unsigned)__shfl((int)t.k, c) >> (part * 8) & 255u;
+            Act a;
+            later_steps<4>(t.x, a.x);
+            later_steps<4>(t.z, a.z);
+            multiply(a, v, scale_float<TUNA_SCALE_E8>(k));
+            if (unit + 1 == hi || now.block + 1 == per) keep(now.task);
+            step(now);
+        });
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // nothing is on its way to the LDS when it is given back
+    } else if constexpr (WIDE) {
         struct Ahead { Part<W> v; float k; Act a; };
-        struct Cursor { int task, block; };                       // a place in the sequence
         const int64_t at_s = Wp::scales(0, F.hidden, col, F.inner, part), each = Wp::scales(1, F.hidden, 0, F.inner, 0);
         const unsigned off_w = (unsigned)(col * row_w * sizeof(W)) + part * 16;
         auto step = [&](Cursor& q) { if (++q.block == per) { q.block = 0; ++q.task; } };
