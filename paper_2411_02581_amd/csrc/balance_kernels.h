@@ -139,12 +139,11 @@ __global__ __launch_bounds__(1024) void k_balance_join(Balance B) {
     group_blocks(B.group_rows, B.groups, g, B.tokens, first, tiles, B.tile);
     double s = 0;
     int c = 0, n = 0;
+    const int there = e < B.experts ? e : B.experts - 1;          // (the others' sums are nobody's)
 #pragma unroll 8
     for (int64_t i = first + run; i < first + tiles; i += R) {
-        if (e < B.experts) {
-            s += (double)B.part[i * B.experts + e];
-            c += B.part_count[i * B.experts + e];
-        }
+        s += (double)B.part[i * B.experts + there];
+        c += B.part_count[i * B.experts + there];
         n += B.part_live[i];
     }
     sums[run][col] = s;

@@ -940,7 +940,7 @@ template <class W> struct PartBase {
     static __device__ __forceinline__ int64_t last(int64_t at, int64_t, int, int64_t) { return at; }
 };
 template <> struct Part<Four> {
-    static constexpr int kUnit = kBlock / 2, kScales = kBlock / kBlock4, kAhead1 = 4, kAhead2 = 6;
+    static constexpr int kUnit = kBlock / 2, kScales = kBlock / kBlock4, kAhead1 = 2, kAhead2 = 4;
     static constexpr bool INSIDE = true;
     v4u v;
     static __device__ __forceinline__ int at(int h, int part) { return part * 32 + h * 8; }
@@ -1029,7 +1029,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
     __shared__ int rank_of[TUNA_MOE_FEW_TOKENS];                  // how many come before this expert, or -1: not chosen
     __shared__ int list[TUNA_MOE_FEW_TOKENS];
     __shared__ float sums[SPLIT ? kFewFirst : 1][2][256];
-    __shared__ __align__(1024) uint8_t ring[kFewFirst][WIDE && Part<W>::INSIDE ? Part<W>::kAhead1 : 1][2][1024];
+    __shared__ __align__(1024) uint8_t ring[kFewFirst][WIDE && Part<W>::INSIDE ? Part<W>::kAhead1 : 1][2][2048];
     const int tid = threadIdx.x, lane = tid & 63;
     const bool first = blockIdx.x == 0;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1139,7 +1139,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
     const int64_t sg = Wp::scales(e, 2 * F.inner, col, F.hidden, part), su = Wp::scales(e, 2 * F.inner, F.inner + col, F.hidden, part);
     const unsigned off_w = (unsigned)(at_w * sizeof(W)) + part * 16;
     // whole blocks in a pipeline; what is behind them (all, for rows that do not start on 16 bytes) one block at a time
-    const int whole = WIDE ? (int)(F.hidden / kBlock) : 0;
+    const int pairs = WIDE ? (int)(F.hidden / (2 * kBlock)) : 0, whole = WIDE && Wp::INSIDE ? 2 * pairs : WIDE ? (int)(F.hidden / kBlock) : 0;
     for (int t0 = 0; t0 < n; t0 += MT * 16) {                     // more than 16 MT tokens of one expert read its weights again
         v4f gate[MT], up[MT];
         unsigned at_x[MT];
@@ -1191,20 +1191,24 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
         constexpr int stride = SPLIT ? kFewFirst : 1, skip = SPLIT;
         if constexpr (WIDE && Wp::INSIDE) {
             // The weights go through the LDS, a wave's own part of it: its lanes load whole pieces of rows, where the product's lanes, sixteen rows side by side,
-            // would ask for every sixteen bytes by themselves.  The scales of gate rows and up rows are a word in the lanes 0 to 31.  A wait for the
+            // would ask for every sixteen bytes by themselves; two blocks at a time, so that a piece is 128 bytes.  The scales of gate rows and up rows are two words in the lanes 0 to 31.  A wait for the
             // scales, which are asked for behind the weights, is a wait for these.  Up to 4 (8) tokens: the lanes of places without one load the
             // tokens' later steps, P = 4 (2) steps in one load.  48 tokens, k = 8 of 128 experts, 1408 x 4096, first kernel: 316 us without all this,
             // 250 with the weights through the LDS.
             auto stream = [&](auto packed) {
                 constexpr int P = packed.value;
-                struct Ahead { unsigned k; v8b a[MT][4 / P]; };
+                struct Ahead { v2u k; v8b a[MT][2][4 / P]; };
                 Ahead st[Wp::kAhead1];
-                const int units = (whole - skip * w + stride - 1) / stride;
+                const int units = (pairs - skip * w + stride - 1) / stride;
                 const unsigned slots = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&ring[w][0][0][0];
-                const int64_t mine = f0 + (lane >> 2) < F.inner ? f0 + (lane >> 2) : F.inner - 1;
-                const unsigned off = (unsigned)(mine * row_w) + ((lane & 3) ^ (lane >> 4)) * 16;
+                unsigned off[2];                                  // eight rows of 128 bytes a load; sixteen number i of a row lies at place i xor (row / 2 mod 8)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int64_t mine = f0 + j * 8 + (lane >> 3) < F.inner ? f0 + j * 8 + (lane >> 3) : F.inner - 1;
+                    off[j] = (unsigned)(mine * row_w) + ((lane & 7) ^ (lane >> 4) ^ j * 4) * 16;
+                }
                 const uint8_t* scale_row = (const uint8_t*)F.s1 + (lane & 16 ? su : sg) - part;      // of this lane's column
-                const int place = c * 64 + (part ^ (c >> 2)) * 16;
+                const int place = c * 128 + (part ^ (c >> 1)) * 16;
                 unsigned x_at[MT];                                // this lane's token, and its first value of a block
 #pragma unroll
                 for (int s = 0; s < MT; ++s) {
@@ -1212,34 +1216,42 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
                     x_at[s] = i < n ? (unsigned)(list[i] * F.ldx) + part * 32 + c / (16 / P) * 8 : ~0u;
                 }
                 auto fetch = [&](Ahead& t, int unit) {
-                    const int64_t b = unit * stride + skip * w;
-                    const unsigned to = slots + (unsigned)unit % Wp::kAhead1 * 2048;
+                    const int64_t b = 2 * (unit * stride + skip * w);
+                    const unsigned to = slots + (unsigned)unit % Wp::kAhead1 * 4096;
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // what is read of this part of the LDS has been read
-                    dma16(scalar((const uint8_t*)(wg + b * Wp::kUnit)), off, to);
-                    dma16(scalar((const uint8_t*)(wu + b * Wp::kUnit)), off, to + 1024);
-                    t.k = 0;
-                    if (lane < 32) __builtin_memcpy(&t.k, scale_row + b * Wp::kScales, 4);
+                    const uint8_t *from_g = scalar((const uint8_t*)(wg + b * Wp::kUnit)), *from_u = scalar((const uint8_t*)(wu + b * Wp::kUnit));
+                    dma16(from_g, off[0], to);
+                    dma16(from_g, off[1], to + 1024);
+                    dma16(from_u, off[0], to + 2048);
+                    dma16(from_u, off[1], to + 3072);
+                    t.k = v2u{0u, 0u};
+                    if (lane < 32) __builtin_memcpy(&t.k, scale_row + b * Wp::kScales, 8);
 #pragma unroll
                     for (int s = 0; s < MT; ++s) {
 #pragma unroll
-                        for (int q = 0; q < 4 / P; ++q) t.a[s][q] = v8b{};
+                        for (int q = 0; q < 8 / P; ++q) t.a[s][q / (4 / P)][q % (4 / P)] = v8b{};
                         if (x_at[s] != ~0u) {
 #pragma unroll
-                            for (int q = 0; q < 4 / P; ++q) t.a[s][q] = as_bf16(*(const v4u*)((const uint8_t*)(F.x + b * kBlock + q * P * 8) + (size_t)(x_at[s] * 2)));
+                            for (int q = 0; q < 8 / P; ++q)
+                                t.a[s][q / (4 / P)][q % (4 / P)] =
+                                    as_bf16(*(const v4u*)((const uint8_t*)(F.x + b * kBlock + q / (4 / P) * kBlock + q % (4 / P) * P * 8) + (size_t)(x_at[s] * 2)));
                         }
                     }
                 };
                 pipeline<Wp::kAhead1, !SPLIT>(st, 0, units, fetch, [&](const Ahead& t, int unit) {
                     asm volatile("" ::"v"(t.k) : "memory");
-                    const uint8_t* from = ring[w][(unsigned)unit % Wp::kAhead1][0] + place;
-                    Part<W> g, u;
-                    g.v = *(const v4u*)from;
-                    u.v = *(const v4u*)(from + 1024);
-                    const unsigned kg = (unsigned)__shfl((int)t.k, c) >> (part * 8) & 255u, ku = (unsigned)__shfl((int)t.k, 16 + c) >> (part * 8) & 255u;
-                    v8b a[MT][4];
 #pragma unroll
-                    for (int s = 0; s < MT; ++s) later_steps<P>(t.a[s], a[s]);
-                    multiply(a, g, u, scale_float<TUNA_SCALE_E8>(kg), scale_float<TUNA_SCALE_E8>(ku));
+                    for (int half = 0; half < 2; ++half) {
+                        const uint8_t* from = ring[w][(unsigned)unit % Wp::kAhead1][0] + (place ^ half * 64);
+                        Part<W> g, u;
+                        g.v = *(const v4u*)from;
+                        u.v = *(const v4u*)(from + 2048);
+                        const unsigned kg = (unsigned)__shfl((int)t.k[half], c) >> (part * 8) & 255u, ku = (unsigned)__shfl((int)t.k[half], 16 + c) >> (part * 8) & 255u;
+                        v8b a[MT][4];
+#pragma unroll
+                        for (int s = 0; s < MT; ++s) later_steps<P>(t.a[s][half], a[s]);
+                        multiply(a, g, u, scale_float<TUNA_SCALE_E8>(kg), scale_float<TUNA_SCALE_E8>(ku));
+                    }
                 });
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing is on its way to the LDS when it is used again, or given back
             };
@@ -1311,7 +1323,7 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
     extern __shared__ float shared[];                             // [kFewSecond][tokens][16] sums
     constexpr bool RING = WIDE && Part<W>::INSIDE;
     constexpr int TASK = Part<W>::INSIDE ? 4 : 16;                // pairs of a task
-    __shared__ __align__(1024) uint8_t ring[kFewSecond][RING ? Part<W>::kAhead2 : 1][RING ? 1024 : 16];
+    __shared__ __align__(1024) uint8_t ring[kFewSecond][RING ? Part<W>::kAhead2 : 1][RING ? 2048 : 16];
     constexpr int PAIRS = TUNA_MOE_FEW_TOKENS * TUNA_MOE_MAX_K;
     __shared__ int pair_of[PAIRS];                                // pairs by expert
     __shared__ float weight[PAIRS];
@@ -1383,7 +1395,8 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
     const int64_t nb = blocks_of(F.inner), row_w = Wp::row(F.inner);
     // whole blocks of all tasks in a pipeline; what is behind them (all, for rows that do not start on 16 bytes) one block at a time
     const int per = WIDE ? (int)(F.inner / kBlock) : 0;
-    const int64_t total = (int64_t)n_tasks * per;
+    const int units = RING ? (per + 1) / 2 : per;                // of a task
+    const int64_t total = (int64_t)n_tasks * units;
     const int lo = (int)(total * w / kFewSecond), hi = (int)(total * (w + 1) / kFewSecond);
     v4f acc = {0.f, 0.f, 0.f, 0.f};
     // one block of a task's activations, in two parts
@@ -1433,41 +1446,58 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
     };
     struct Cursor { int task, block; };                           // a place in the sequence
     if constexpr (RING) {
-        // As in the first kernel: weights through the LDS, a wave's own part of it, scales as a word in the lanes 0 to 15.  A task is up to four pairs, so that one load
-        // of each part of the activations brings all their steps; more pairs of an expert are its next task, whose weights are then near.
-        struct Ahead { unsigned k; v8b x[1], z[1]; };
+        // As in the first kernel: weights through the LDS, two blocks at a time (one where a task's last has none beside it: the other half is then that one again,
+        // and not used), scales as a word in the lanes 0 to 15 and one in 16 to 31.  A task is up to four pairs, so that one load of each part of
+        // the activations brings all steps of a block; more pairs of an expert are its next task, whose weights are then near.
+        struct Ahead { unsigned k; v8b x[2][1], z[2][1]; };
         const unsigned slots = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&ring[w][0][0];
-        const int64_t mine = c0 + (lane >> 2) < F.hidden ? c0 + (lane >> 2) : F.hidden - 1, each = Wp::scales(1, F.hidden, 0, F.inner, 0);
-        const unsigned off = (unsigned)(mine * row_w) + ((lane & 3) ^ (lane >> 4)) * 16;
+        const int64_t each = Wp::scales(1, F.hidden, 0, F.inner, 0);
+        unsigned off[2];
+        const int chunk = (lane & 7) ^ (lane >> 4);               // of the first eight rows; of the second it is 4 further or nearer
+#pragma unroll
+        for (int j = 0; j < 2; ++j) off[j] = (unsigned)((c0 + j * 8 + (lane >> 3) < F.hidden ? c0 + j * 8 + (lane >> 3) : F.hidden - 1) * row_w);
         const uint8_t* scale_row = (const uint8_t*)F.s2 + Wp::scales(0, F.hidden, col, F.inner, 0);
-        const int place = c * 64 + (part ^ (c >> 2)) * 16;
-        auto step = [&](Cursor& q) { if (++q.block == per) { q.block = 0; ++q.task; } };
-        Cursor now = {per ? lo / per : 0, per ? lo % per : 0}, far = now;
+        const int place = c * 128 + (part ^ (c >> 1)) * 16;
+        auto step = [&](Cursor& q) { if (++q.block == units) { q.block = 0; ++q.task; } };
+        Cursor now = {units ? lo / units : 0, units ? lo % units : 0}, far = now;
         auto fetch = [&](Ahead& t, int unit) {
             const int e = __builtin_amdgcn_readfirstlane(task_expert[far.task]);
+            const int two = far.block * 2 + 1 < per ? 1 : 0;      // there is a second block
+            const unsigned to = slots + (unsigned)unit % Wp::kAhead2 * 2048, in = (chunk & (two ? 7 : 3)) * 16;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // what is read of this part of the LDS has been read
-            dma16(scalar((const uint8_t*)((const W*)F.w2 + (int64_t)e * F.hidden * row_w + far.block * Wp::kUnit)), off, slots + (unsigned)unit % Wp::kAhead2 * 1024);
+            const uint8_t* from = scalar((const uint8_t*)((const W*)F.w2 + (int64_t)e * F.hidden * row_w + far.block * (2 * Wp::kUnit)));
+            dma16(from, off[0] + in, to);
+            dma16(from, off[1] + (two ? in ^ 64u : in), to + 1024);
             t.k = 0;
-            if (lane < 16) __builtin_memcpy(&t.k, scale_row + e * each + far.block * Wp::kScales, 4);
-            t.x[0] = t.z[0] = v8b{};
+            if (lane < 32) __builtin_memcpy(&t.k, scale_row + e * each + (far.block * 2 + (lane >> 4) * two) * Wp::kScales, 4);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) t.x[half][0] = t.z[half][0] = v8b{};
             if ((c & 3) < task_count[far.task]) {
                 const unsigned at = ((unsigned)(pair_of[task_first[far.task] + (c & 3)] * F.ld_h) + part * 32 + (c >> 2) * 8) * 2;
-                t.x[0] = as_bf16(*(const v4u*)((const uint8_t*)(F.hi + far.block * kBlock) + (size_t)at));
-                t.z[0] = as_bf16(*(const v4u*)((const uint8_t*)(F.lo + far.block * kBlock) + (size_t)at));
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int64_t b = (far.block * 2 + half * two) * kBlock;
+                    t.x[half][0] = as_bf16(*(const v4u*)((const uint8_t*)(F.hi + b) + (size_t)at));
+                    t.z[half][0] = as_bf16(*(const v4u*)((const uint8_t*)(F.lo + b) + (size_t)at));
+                }
             }
             step(far);
         };
         Ahead st[Wp::kAhead2];
         pipeline<Wp::kAhead2, false>(st, lo, hi, fetch, [&](const Ahead& t, int unit) {
             asm volatile("" ::"v"(t.k) : "memory");
-            Part<W> v;
-            v.v = *(const v4u*)(ring[w][(unsigned)unit % Wp::kAhead2] + place);
-            const unsigned k = (unsigned)__shfl((int)t.k, c) >> (part * 8) & 255u;
-            Act a;
-            later_steps<4>(t.x, a.x);
-            later_steps<4>(t.z, a.z);
-            multiply(a, v, scale_float<TUNA_SCALE_E8>(k));
-            if (unit + 1 == hi || now.block + 1 == per) keep(now.task);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                if (half && now.block * 2 + 1 >= per) break;
+                Part<W> v;
+                v.v = *(const v4u*)(ring[w][(unsigned)unit % Wp::kAhead2] + (place ^ half * 64));
+                const unsigned k = (unsigned)__shfl((int)t.k, half * 16 + c) >> (part * 8) & 255u;
+                Act a;
+                later_steps<4>(t.x[half], a.x);
+                later_steps<4>(t.z[half], a.z);
+                multiply(a, v, scale_float<TUNA_SCALE_E8>(k));
+            }
+            if (unit + 1 == hi || now.block + 1 == units) keep(now.task);
             step(now);
         });
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // nothing is on its way to the LDS when it is given back

@@ -412,7 +412,8 @@ def few(t, h, f, e, k, renorm=True, dtype="bf16", logits=None, lt="f32", shift=0
 
 @pytest.mark.parametrize("t,h,f,e,k", [(1, 128, 64, 8, 2), (1, 256, 100, 60, 4), (2, 300, 48, 5, 5), (7, 384, 144, 16, 1), (17, 520, 72, 12, 4), (64, 256, 128, 8, 3),
                                        (33, 136, 40, 100, 8), (64, 128, 32, 3, 2), (5, 1040, 1040, 4, 2), (3, 160, 224, 6, 2), (9, 2880, 352, 4, 1), (1, 1, 1, 1, 1),
-                                       (1, 2048, 1024, 16, 4), (40, 1024, 512, 32, 4)])
+                                       (1, 2048, 1024, 16, 4), (40, 1024, 512, 32, 4), (6, 640, 416, 8, 3), (50, 768, 384, 16, 4), (30, 896, 640, 20, 4),
+                                       (1, 1152, 928, 7, 3)])
 def test_few(t, h, f, e, k):
     few(t, h, f, e, k, renorm=t % 2 == 0)
 
