@@ -9,10 +9,11 @@ namespace {
 // Blocks of 32 that all rows have are counted in 31 bits.
 bool blocks_fit(int64_t rows, int64_t cols) { return rows <= kMaxRows && cols <= kMaxRows && rows * ceil_div(cols, kBlock4) <= kMaxRows; }
 
-// Four blocks in turn for every four lanes, or one where there would be too few workgroups for the device.
-template <class F> void in_turn(int64_t blocks, F f) {
-    if (blocks > 64 * 4 * 1024) f(Int<4>{}, dim3((unsigned)ceil_div(blocks, 256)));
-    else f(Int<1>{}, dim3((unsigned)ceil_div(blocks, 64)));
+// For every two (or four) lanes two (or four) blocks in turn, or one where there would be too few workgroups for the device.
+template <int LANES, class F> void in_turn(int64_t blocks, F f) {
+    constexpr int EACH = 256 / LANES;
+    if (blocks > 256 * 1024) f(Int<LANES>{}, dim3((unsigned)ceil_div(blocks, 256)));
+    else f(Int<1>{}, dim3((unsigned)ceil_div(blocks, EACH)));
 }
 
 }  // namespace
@@ -32,12 +33,12 @@ int tuna_fp4_quantize(const void* x, int type, int64_t ldx, int64_t rows, int64_
     if (out_rows == 0) return TUNA_OK;
     const int rc = tuna_host::ensure_device();
     if (rc != TUNA_OK) return rc;
-    const bool wide = rows_wide(x, size_of(type), ldx) && on(q, 4) && ldq % 4 == 0 && (act == TUNA_ACT_NONE || (cols * size_of(type)) % 16 == 0);
+    const bool wide = rows_wide(x, size_of(type), ldx) && on(q, 8) && ldq % 8 == 0 && (act == TUNA_ACT_NONE || (cols * size_of(type)) % 16 == 0);
     with_type(type, [&](auto* t) {
         using T = Pointee<decltype(t)>;
         with_bool(act == TUNA_ACT_SWIGLU, [&](auto a) {
             with_bool(wide, [&](auto wd) {
-                in_turn(rows * nb, [&](auto u, dim3 grid) {
+                in_turn<2>(rows * nb, [&](auto u, dim3 grid) {
                     LAUNCH((k_fp4_quantise<T, a.value, wd.value != 0, u.value>), grid, 256, (const T*)x, ldx, (unsigned)(rows * nb), cols, slots, copies, out_rows,
                            (uint8_t*)q, ldq, (uint8_t*)scales, ld_scales);
                 });
@@ -83,7 +84,7 @@ int tuna_fp4_dequantize(const void* q, int64_t ldq, const void* scales, int64_t 
     with_type(type, [&](auto* t) {
         using T = Pointee<decltype(t)>;
         with_bool(wide, [&](auto wd) {
-            in_turn(rows * nb, [&](auto u, dim3 grid) {
+            in_turn<4>(rows * nb, [&](auto u, dim3 grid) {
                 LAUNCH((k_fp4_dequantise<T, wd.value != 0, u.value>), grid, 256, (const uint8_t*)q, ldq, (const uint8_t*)scales, ld_scales, (unsigned)(rows * nb), cols,
                        (T*)x, ldx);
             });

@@ -43,45 +43,65 @@ template <bool WIDE> __device__ __forceinline__ void store_packed(uint8_t* d, un
     for (int i = 0; i < 4; ++i) if (2 * i < left) d[i] = (uint8_t)(q >> (8 * i));
 }
 
-// Four lanes per block of 32 values, eight each; U blocks in turn, whose loads are under way together.
+// Two lanes per block of 32 values, sixteen each; U blocks in turn, whose loads are under way together, and the first slots with them.
 template <class T, int ACT, bool WIDE, int U>
 __global__ __launch_bounds__(256) void k_fp4_quantise(const T* x, int64_t ldx, unsigned total, int64_t cols, const int32_t* slots, int copies, int64_t out_rows,
                                                       uint8_t* q, int64_t ldq, uint8_t* scales, int64_t ld_scales) {
-    const unsigned nb = (unsigned)((cols + kBlock4 - 1) / kBlock4), at0 = blockIdx.x * (64 * U) + (threadIdx.x >> 2);
-    float v[U][8], up[U][8];
+    constexpr int FIRST = 2;
+    const unsigned nb = (unsigned)((cols + kBlock4 - 1) / kBlock4), at0 = blockIdx.x * (128 * U) + (threadIdx.x >> 1);
+    const int mine = (threadIdx.x & 1) * 16;
+    float v[U][2][8], up[U][2][8];
     unsigned row[U], block[U];
+    int to_first[U][FIRST];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const unsigned at = at0 + u * 64 < total ? at0 + u * 64 : total - 1;
+        const unsigned at = at0 + u * 128 < total ? at0 + u * 128 : total - 1;
         row[u] = at / nb;
         block[u] = at - row[u] * nb;
-        const int64_t c = (int64_t)block[u] * kBlock4 + (threadIdx.x & 3) * 8;
-        const T* p = x + row[u] * ldx + c;
-        load8<WIDE>(p, cols - c, v[u]);
-        if (ACT == TUNA_ACT_SWIGLU) load8<WIDE>(p + cols, cols - c, up[u]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t c = (int64_t)block[u] * kBlock4 + mine + h * 8;
+            const T* p = x + row[u] * ldx + c;
+            load8<WIDE>(p, cols - c, v[u][h]);
+            if (ACT == TUNA_ACT_SWIGLU) load8<WIDE>(p + cols, cols - c, up[u][h]);
+        }
+        if (slots) {
+#pragma unroll
+            for (int j = 0; j < FIRST; ++j) to_first[u][j] = slots[(int64_t)row[u] * copies + (j < copies ? j : 0)];
+        }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        if (at0 + u * 64 >= total) break;                         // (four lanes together)
-        const int64_t r = row[u], b = block[u], c = b * kBlock4 + (threadIdx.x & 3) * 8, left = cols - c;
-        if (ACT == TUNA_ACT_SWIGLU) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[u][i] = i < left ? gate_of(v[u][i]).silu * up[u][i] : 0.f;
-        }
+        if (at0 + u * 128 >= total) break;                        // (two lanes together)
+        const int64_t r = row[u], b = block[u], c = b * kBlock4 + mine, left = cols - c;
         unsigned peak = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) peak = larger(peak, magnitude(v[u][i]));
-        peak = larger(peak, (unsigned)__shfl_xor((int)peak, 1));
-        peak = larger(peak, (unsigned)__shfl_xor((int)peak, 2));
-        const unsigned s = scale4_of(peak), o = pack8(v[u], s);
-        for (int j = 0; j < copies; ++j) {
-            int64_t to = r;
-            if (slots) {
-                to = slots[r * copies + j];
-                if (to < 0 || to >= out_rows) continue;
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (ACT == TUNA_ACT_SWIGLU) v[u][h][i] = h * 8 + i < left ? gate_of(v[u][h][i]).silu * up[u][h][i] : 0.f;
+                peak = larger(peak, magnitude(v[u][h][i]));
             }
-            store_packed<WIDE>(q + to * ldq + c / 2, o, left);
-            if ((threadIdx.x & 3) == 0) scales[to * ld_scales + b] = (uint8_t)s;
+        peak = larger(peak, dpp<0xb1>(peak, peak));               // the other lane of the two
+        const unsigned s = scale4_of(peak);
+        const v2u o = {pack8(v[u][0], s), pack8(v[u][1], s)};
+        auto put = [&](int64_t to) {
+            uint8_t* d = q + to * ldq + c / 2;
+            if (WIDE && left >= 16) {
+                *(v2u*)d = o;
+            } else {
+                store_packed<WIDE>(d, o[0], left);
+                store_packed<WIDE>(d + 4, o[1], left - 8);
+            }
+            if (mine == 0) scales[to * ld_scales + b] = (uint8_t)s;
+        };
+        if (!slots) {
+            put(r);
+            continue;
+        }
+        for (int j = 0; j < copies; ++j) {
+            const int64_t to = j == 0 ? to_first[u][0] : j < FIRST ? to_first[u][1] : slots[r * copies + j];
+            if (to >= 0 && to < out_rows) put(to);
         }
     }
 }
@@ -90,7 +110,7 @@ __global__ __launch_bounds__(256) void k_fp4_quantise(const T* x, int64_t ldx, u
 template <class T, bool WIDE>
 __global__ __launch_bounds__(256) void k_fp4_quantise_columns(const T* x, int64_t ldx, int64_t rows, int64_t cols, const int32_t* group_rows, int groups,
                                                               uint8_t* q, int64_t ldq, uint8_t* scales, int64_t ld_scales) {
-    __shared__ __align__(16) unsigned tile[kBlock][20];           // a column's 64 bytes, and its four scales behind them
+    __shared__ __align__(16) unsigned tile[kBlock][20];           // a column's 64 bytes, its sixteens moved on by column / 16 places; its four scales behind them
     const Place pl = find_tile(group_rows, groups, rows, kBlock, blockIdx.x);
     if (pl.group < 0) return;
     const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
@@ -114,7 +134,7 @@ __global__ __launch_bounds__(256) void k_fp4_quantise_columns(const T* x, int64_
         peak = larger(peak, (unsigned)__shfl_xor((int)peak, 16));
         peak = larger(peak, (unsigned)__shfl_xor((int)peak, 32));
         const unsigned s = scale4_of(peak);
-        tile[cx * 8 + j][ry] = pack8(col, s);
+        tile[cx * 8 + j][(ry + (cx >> 1) * 4) & 15] = pack8(col, s);
         if ((ry & 3) == 0) ((uint8_t*)&tile[cx * 8 + j][16])[ry >> 2] = (uint8_t)s;
     }
     __syncthreads();
@@ -124,7 +144,7 @@ __global__ __launch_bounds__(256) void k_fp4_quantise_columns(const T* x, int64_
         const int64_t to = (int64_t)blockIdx.y * kBlock + row;
         if (to >= cols) continue;
         uint8_t* d = q + to * ldq + pl.block * 64 + ch * 16;
-        const v4u val = *(const v4u*)&tile[row][ch * 4];
+        const v4u val = *(const v4u*)&tile[row][((ch + (row >> 4)) & 3) * 4];
         if (wide) *(v4u*)d = val;
         else for (int b = 0; b < 16; ++b) d[b] = (uint8_t)(val[b >> 2] >> (8 * (b & 3)));
         scales[to * ld_scales + pl.block * 4 + ch] = ((const uint8_t*)&tile[row][16])[ch];
