@@ -1327,7 +1327,8 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
     constexpr int PAIRS = TUNA_MOE_FEW_TOKENS * TUNA_MOE_MAX_K;
     __shared__ int pair_of[PAIRS];                                // pairs by expert
     __shared__ float weight[PAIRS];
-    __shared__ int first_of[TUNA_MOE_MAX_EXPERTS], count_of[TUNA_MOE_MAX_EXPERTS];
+    __shared__ int first_of[TUNA_MOE_MAX_EXPERTS];
+    __shared__ unsigned long long tokens_of[TUNA_MOE_MAX_EXPERTS];        // a bit per token: the order of the atomics does not matter
     __shared__ int task_expert[PAIRS], task_first[PAIRS], task_count[PAIRS];
     __shared__ int n_tasks;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1345,11 +1346,11 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
         }
         __syncthreads();
     } else {
-        for (int i = tid; i < F.experts; i += kFewSecond * 64) count_of[i] = 0;
+        for (int i = tid; i < F.experts; i += kFewSecond * 64) tokens_of[i] = 0;
         __syncthreads();
         for (int i = tid; i < np; i += kFewSecond * 64) {
             const int e = F.chosen[i];
-            if (e >= 0) atomicAdd(&count_of[e], 1);
+            if (e >= 0) atomicOr(&tokens_of[e], 1ull << (i / F.k));
             float s = e < 0 ? 0.f : F.share[i];
             if (F.renorm && e >= 0) {
                 const int t0 = i / F.k * F.k;
@@ -1363,11 +1364,10 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
         if (w == 0) {                                                 // the tasks in order of their experts
             int tasks = 0, pairs = 0;
             for (int e0 = 0; e0 < F.experts; e0 += 64) {
-                const int cnt = e0 + lane < F.experts ? count_of[e0 + lane] : 0;
+                const int cnt = e0 + lane < F.experts ? __popcll(tokens_of[e0 + lane]) : 0;
                 const int inc = wave_scan(cnt, lane), parts = (cnt + TASK - 1) / TASK, inc_parts = wave_scan(parts, lane);
                 if (cnt > 0) {
                     first_of[e0 + lane] = pairs + inc - cnt;
-                    count_of[e0 + lane] = 0;
                     for (int i = 0; i < parts; ++i) {
                         const int at = tasks + inc_parts - parts + i;
                         task_expert[at] = e0 + lane;
@@ -1381,10 +1381,10 @@ __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
             if (lane == 0) n_tasks = tasks;
         }
         __syncthreads();
-        // the order of an expert's pairs changes no sum: each has its own row
+        // an expert's pairs in order of their tokens: where a task begins and a wave's run of steps ends may change a sum's last place
         for (int i = tid; i < np; i += kFewSecond * 64) {
             const int e = F.chosen[i];
-            if (e >= 0) pair_of[first_of[e] + atomicAdd(&count_of[e], 1)] = i;
+            if (e >= 0) pair_of[first_of[e] + __popcll(tokens_of[e] & ((1ull << (i / F.k)) - 1))] = i;
         }
         __syncthreads();
     }
