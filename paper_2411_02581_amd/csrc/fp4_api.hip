@@ -127,7 +127,7 @@ bool product_fills(const Product4& P, bool cols) {
 // 4096 x 4096, us a call, this form / tiles of 256 x 256: 1 row 6.5 / 25, 16 rows 6.8 / 25, 64 rows 12 / 25, 128 rows 14.5 / 26, 256 rows 20 / 26, 512 rows 37 / 28;
 // 16 groups, 2816 x 2048: 32 rows 17 / 21, 96 rows 18 / 21, 256 rows 20 / 21, and 2048 x 1408: 96 rows 8 / 19.
 template <class F> bool product_thin(const Product4& P, F rows) {
-    if (!product_wide(P) || ceil_div(P.m, 16) + P.groups > kMaxGridY || ceil_div(P.n, 16) > kMaxRows / 512) return false;
+    if (!product_wide(P) || P.ldb >= (1 << 24) || ceil_div(P.m, 16) + P.groups > kMaxGridY || ceil_div(P.n, 16) > kMaxRows / 512) return false;
     if (P.groups > 1) {
         if (P.m > 16 * (int64_t)P.groups) return false;
         rows(Int<1>{}, Int<2>{}, Int<4>{});

@@ -549,58 +549,106 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
 }
 
 // The form for few rows, which reads the weights once and little else: a workgroup has 16 NT rows of b and 16 MT rows of a, its W waves share the length
-// in units of 128, operands go from memory to registers, and the waves' sums are added up in their order.
+// in units of 256, and the waves' sums are added up in their order.  Rows of b go through the LDS, a wave's own part of it, in whole pieces of 128 bytes
+// (sixteen number i of a row at place i xor (row / 2 mod 8)): the product's lanes, sixteen rows side by side, would ask for every sixteen bytes by
+// themselves.  A row's scales of a unit are two words in the lane of its number, read by those that need them.
 template <class OUT, int MT, int NT, int W>
 __global__ __launch_bounds__(W * 64) void k_fp4_product_thin(Product4 P) {
-    constexpr int T = MT * NT, AHEAD = T > 4 ? 2 : 3;
-    __shared__ v4f sums[W][T][64];
+    constexpr int T = MT * NT, AHEAD = T > 4 ? 2 : 3, RING = AHEAD * NT * 2048;
+    __shared__ __align__(1024) uint8_t shared[W * (RING > T * 1024 ? RING : T * 1024)];      // the waves' rings, and then their sums
+    v4f(*sums)[T][64] = (v4f(*)[T][64])shared;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Place pl = find_tile(P.group_rows, P.groups, P.m, 16 * MT, blockIdx.y);
     if (pl.group < 0) return;
     const int group = __builtin_amdgcn_readfirstlane(pl.group);
     const int64_t i0 = pl.first, i_end = pl.end, j0 = (int64_t)blockIdx.x * (16 * NT);
     const int r = lane & 15, g = lane >> 4;
-    const uint8_t *a[MT], *as[MT], *b[NT], *bs[NT];
-#pragma unroll
-    for (int s = 0; s < MT; ++s) {
-        const int64_t row = i0 + s * 16 + r < i_end ? i0 + s * 16 + r : i_end - 1;
-        a[s] = P.a + row * P.lda;
-        as[s] = P.as + row * P.ld_as;
-    }
-#pragma unroll
-    for (int s = 0; s < NT; ++s) {
-        const int64_t row = j0 + s * 16 + r < P.n ? j0 + s * 16 + r : P.n - 1;
-        b[s] = P.b + group * P.b_group + row * P.ldb;
-        bs[s] = P.bs + group * P.bs_group + row * P.ld_bs;
-    }
+    auto row_a = [&](int n) { return i0 + n < i_end ? i0 + n : i_end - 1; };
+    auto row_b = [&](int n) { return j0 + n < P.n ? j0 + n : P.n - 1; };
+    const uint8_t *first_b = P.b + group * P.b_group, *first_bs = P.bs + group * P.bs_group;
     v4f acc[MT][NT];
 #pragma unroll
     for (int s = 0; s < MT; ++s)
 #pragma unroll
         for (int q = 0; q < NT; ++q) acc[s][q] = v4f{0.f, 0.f, 0.f, 0.f};
-    struct Ahead { v4u a[MT], b[NT]; unsigned sa[MT], sb[NT]; };
-    auto fetch = [&](Ahead& t, int64_t kb, auto full) {
-        const int64_t blk = kb * 4 + g, left = P.k - blk * kBlock4;
-        auto row = [&](const uint8_t* p) { return full.value ? *(const v4u*)(p + blk * 16) : chunk32<true>(p + blk * 16, left); };
-        auto one = [&](const uint8_t* p) { return full.value || left > 0 ? (unsigned)p[blk] : 127u; };
+    // units of two whole blocks; the last may have one (the other half is then that one again, and not used); the rest of the length is less than a block
+    const int whole = (int)(P.k / kBlock), units = ((whole + 1) / 2 - w + W - 1) / W;
+    {
+        struct Ahead { v2u kb, ka; v4u a[MT][2]; };
+        const uint8_t* base = scalar(first_b + j0 * P.ldb);
+        unsigned off[2 * NT];                                     // eight rows of 128 bytes a load
 #pragma unroll
-        for (int s = 0; s < NT; ++s) { t.b[s] = row(b[s]); t.sb[s] = one(bs[s]); }
+        for (int j = 0; j < 2 * NT; ++j)
+            off[j] = (unsigned)((row_b(j * 8 + (lane >> 3)) - j0) * P.ldb);
+        const int chunk = (lane & 7) ^ (lane >> 4);               // of the first eight rows; of the next it is 4 further or nearer
+        const uint8_t *at_sb = first_bs + row_b(lane % (16 * NT)) * P.ld_bs, *at_sa = P.as + row_a(lane % (16 * MT)) * P.ld_as;
+        const uint8_t* at_a[MT];
 #pragma unroll
-        for (int s = 0; s < MT; ++s) { t.a[s] = row(a[s]); t.sa[s] = one(as[s]); }
-    };
-    auto use = [&](const Ahead& t) {
+        for (int s = 0; s < MT; ++s) at_a[s] = P.a + row_a(s * 16 + r) * P.lda + g * 16;
+        uint8_t* ring = shared + w * RING;
+        const unsigned slots = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)ring;
+        const int place = r * 128 + (g ^ (r >> 1)) * 16;
+        auto fetch = [&](Ahead& t, int u) {
+            const int64_t at = (int64_t)(u * W + w) * kBlock;     // in bytes
+            const int two = 2 * (u * W + w) + 1 < whole ? 1 : 0;
+            const unsigned in = (chunk & (two ? 7 : 3)) * 16;
+            const unsigned to = slots + (unsigned)u % AHEAD * (NT * 2048);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // what is read of this part of the LDS has been read
 #pragma unroll
-        for (int s = 0; s < MT; ++s)
+            for (int j = 0; j < 2 * NT; ++j) dma16(base + at, off[j] + (two && (j & 1) ? in ^ 64u : in), to + j * 1024);
+            t.kb = t.ka = v2u{0u, 0u};
+            auto words = [&](v2u& k, const uint8_t* p) {
+                if (two) __builtin_memcpy(&k, p, 8);
+                else __builtin_memcpy(&k, p, 4);
+            };
+            if (NT == 4 || lane < 16 * NT) words(t.kb, at_sb + at / 16);      // behind the rows of b: a wait for it is a wait for them
+            if (MT == 4 || lane < 16 * MT) words(t.ka, at_sa + at / 16);
 #pragma unroll
-            for (int q = 0; q < NT; ++q) acc[s][q] = mma4<0>(t.b[q], t.a[s], acc[s][q], t.sb[q], t.sa[s]);
-    };
-    const int whole = (int)(P.k / kBlock), units = (whole - w + W - 1) / W;
-    Ahead st[AHEAD];
-    pipeline<AHEAD, false>(st, 0, units, [&](Ahead& t, int u) { fetch(t, (int64_t)u * W + w, Int<1>{}); }, [&](const Ahead& t, int) { use(t); });
-    if (whole * (int64_t)kBlock < P.k && whole % W == w) {
-        fetch(st[0], whole, Int<0>{});
-        use(st[0]);
+            for (int s = 0; s < MT; ++s)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) t.a[s][h] = *(const v4u*)(at_a[s] + at + h * two * 64);
+        };
+        Ahead st[AHEAD];
+        pipeline<AHEAD, false>(st, 0, units, fetch, [&](const Ahead& t, int u) {
+            asm volatile("" ::"v"(t.kb) : "memory");
+            const uint8_t* from = ring + (unsigned)u % AHEAD * (NT * 2048);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (h && 2 * (u * W + w) + 1 >= whole) break;
+                v4u b[NT];
+                unsigned sb[NT], sa[MT];
+#pragma unroll
+                for (int q = 0; q < NT; ++q) {
+                    b[q] = *(const v4u*)(from + q * 2048 + (place ^ h * 64));
+                    sb[q] = (unsigned)__shfl((int)t.kb[h], q * 16 + r) >> (8 * g);
+                }
+#pragma unroll
+                for (int s = 0; s < MT; ++s) sa[s] = (unsigned)__shfl((int)t.ka[h], s * 16 + r) >> (8 * g);
+#pragma unroll
+                for (int s = 0; s < MT; ++s)
+#pragma unroll
+                    for (int q = 0; q < NT; ++q) acc[s][q] = mma4<0>(b[q], t.a[s][h], acc[s][q], sb[q], sa[s]);
+            }
+        });
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // nothing is on its way to the LDS when it is used again
     }
+    if (whole * (int64_t)kBlock < P.k && (whole + 1) / 2 % W == w) {
+        const int64_t blk = (int64_t)whole * 4 + g, left = P.k - blk * kBlock4;
+        auto row = [&](const uint8_t* p) { return chunk32<true>(p + blk * 16, left); };
+        auto one = [&](const uint8_t* p) { return left > 0 ? (unsigned)p[blk] : 127u; };
+        v4u b[NT];
+        unsigned sb[NT];
+#pragma unroll
+        for (int q = 0; q < NT; ++q) { b[q] = row(first_b + row_b(q * 16 + r) * P.ldb); sb[q] = one(first_bs + row_b(q * 16 + r) * P.ld_bs); }
+#pragma unroll
+        for (int s = 0; s < MT; ++s) {
+            const v4u a = row(P.a + row_a(s * 16 + r) * P.lda);
+            const unsigned sa = one(P.as + row_a(s * 16 + r) * P.ld_as);
+#pragma unroll
+            for (int q = 0; q < NT; ++q) acc[s][q] = mma4<0>(b[q], a, acc[s][q], sb[q], sa);
+        }
+    }
+    __syncthreads();
 #pragma unroll
     for (int s = 0; s < MT; ++s)
 #pragma unroll
