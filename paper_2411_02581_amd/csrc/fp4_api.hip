@@ -123,14 +123,16 @@ bool product_fills(const Product4& P, bool cols) {
     return ceil_div(P.m, 256) * ceil_div(P.n, 256) * (cols ? P.groups : 1) >= 256 && (cols || P.m >= 192 * (int64_t)P.groups);
 }
 
-// Few rows: tiles for which the waves of a workgroup share the length.  Which of them, and whether: the tiles of one group are one round of workgroups.
-// 4096 x 4096, us a call, this form / tiles of 256 x 256: 1 row 6.5 / 25, 16 rows 6.8 / 25, 64 rows 12 / 25, 128 rows 14.5 / 26, 256 rows 20 / 26, 512 rows 37 / 28;
-// 16 groups, 2816 x 2048: 32 rows 17 / 21, 96 rows 18 / 21, 256 rows 20 / 21, and 2048 x 1408: 96 rows 8 / 19.
+// Few rows: tiles for which the waves of a workgroup share the length.  Which of them, and whether: the tiles of one group are at most a round of workgroups.
+// 4096 x 4096, us a call, this form / tiles of 128 x 256: 1 row 6.4 / 19, 64 rows 8.4 / 19, 128 rows 9.5 / 19, 256 rows 11.4 / 19, 512 rows 22 / 19.
+// Groups, rows by 16 and columns by 32 / by 32 and 64 / tiles of 128 x 256: 16 of 2816 x 2048, 96 rows 12.5 / 14.4 / 15.9, 256 rows 13.8 / 14.7 / 16.1, 512 rows
+// 19 / 14.9 / 16.7, 1024 rows 32 / 25 / 17; 64 of 3584 x 4096, 512 rows 89 / 94 / 121, 1024 rows 107 / 102 / 127, 2048 rows 157 / 114 / 127.
 template <class F> bool product_thin(const Product4& P, F rows) {
     if (!product_wide(P) || P.ldb >= (1 << 24) || ceil_div(P.m, 16) + P.groups > kMaxGridY || ceil_div(P.n, 16) > kMaxRows / 512) return false;
     if (P.groups > 1) {
-        if (P.m > 16 * (int64_t)P.groups) return false;
-        rows(Int<1>{}, Int<2>{}, Int<4>{});
+        if (P.m <= 16 * (int64_t)P.groups) rows(Int<1>{}, Int<2>{}, Int<4>{});
+        else if (P.m <= 32 * (int64_t)P.groups) rows(Int<2>{}, Int<4>{}, Int<4>{});
+        else return false;
         return true;
     }
     if (P.m <= 16) rows(Int<1>{}, Int<1>{}, Int<8>{});

@@ -20,6 +20,12 @@ def gen(seed):
     return torch.Generator(device=DEV).manual_seed(seed)
 
 
+@pytest.fixture(scope="module", autouse=True)
+def memory_is_given_back():
+    yield
+    torch.cuda.empty_cache()
+
+
 def ok(rc):
     assert rc == tuna.TUNA_OK, tuna.tuna_strerror(rc)
 

@@ -13,6 +13,12 @@ EPS = 2.0 ** -24
 U8 = torch.uint8
 
 
+@pytest.fixture(scope="module", autouse=True)
+def memory_is_given_back():
+    yield
+    torch.cuda.empty_cache()
+
+
 def ok(rc):
     assert rc == tuna.TUNA_OK, tuna.tuna_strerror(rc)
 
