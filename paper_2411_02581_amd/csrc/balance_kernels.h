@@ -63,7 +63,8 @@ __device__ __forceinline__ void balance_loss(const Balance& B, int64_t g, double
 }
 
 // One workgroup per tile of a sequence: sixteen waves add up their tokens' shares, the logits of up to four under way together, then the waves' sums are
-// added in their order.  ALL: the tile is the whole batch, one sequence, and the sums are the results.  65536 x 256 in 32 bits, 37 sequences: 67 MB.
+// added in their order.  ALL: the tile is the whole batch, one sequence, and the sums are the results.  65536 x 256 in 32 bits, 37 sequences: 67 MB, 24 us (2.8 TB/s:
+// a wave's sums and largest logits take as long as its loads); 24 x 64 in one launch 4.8 us.
 template <class T, int PER, bool ALL>
 __global__ __launch_bounds__(1024) void k_balance_part(Balance B) {
     constexpr int U = PER <= 4 ? 4 : PER == 8 ? 2 : 1;
@@ -173,7 +174,8 @@ __global__ __launch_bounds__(1024) void k_balance_loss(Balance B) {
 }
 
 // Every wave has the fractions f_e = counts_e / C of its tile's sequence in registers: dl_i = dloss E / N p_i (f_i - sum over e of f_e p_e).  The tiles behind the
-// sequences' are the tokens outside every sequence: those before the first bound, then those behind the last.
+// sequences' are the tokens outside every sequence: those before the first bound, then those behind the last.  Bound by memory: 65536 x 256 in 32 bits, 134 MB, 27 us
+// (5.1 TB/s).
 template <class T, int PER, bool ADD>
 __global__ __launch_bounds__(256) void k_balance_grad(Balance B, const float* dloss, T* dlogits, int64_t ld_d) {
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
