@@ -287,8 +287,9 @@ template <int N, int M> __device__ __forceinline__ void left_and_barrier() {
 // (row / 4 mod 4), so that the lanes that the LDS serves together meet every bank once.  The scales come in sixteens, for four stages (512 of the
 // length, from multiples of 512); a lane collects its blocks' bytes of two stages in one register, of which a product takes byte STEP.
 // The waves: WM x WN, 32 MT by 32 NT each; a stage is two steps of 64, in which lane (r, g) has block number 2 g + step of row r.
-// 16384 x 8192 x 8192 0.56 to 0.61 ms (3.6 to 3.9 PFLOP/s): eight rounds of 64 stages, 1.1 us each, of which the matrix instructions take 0.43 at the highest
-// clock.  Short lengths pay the first loads and the stores of every tile: 20011 rows of 32 groups, 3584 x 2048, 154 us, where a third is not stages.  Tiles of 128 rows at
+// 16384 x 8192 x 8192 0.56 to 0.61 ms (3.6 to 3.9 PFLOP/s): eight rounds of 64 stages of 1.8 thousand cycles, 1.0 of them matrix instructions, while the clock
+// falls to some 1.6 GHz.  Short lengths pay the first loads and the stores of every tile: 20011 rows of 32 groups, 3584 x 2048, 154 us, six rounds of 52 thousand
+// cycles, of which 16 stages would be 29.  Tiles of 128 rows at
 // the ends of groups, and tiles dealt to the XCDs in runs of 32, changed the groups' times by less than one machine differs from itself, and cost the dense ones 2 to 4 %.
 template <bool COLS, class OUT, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles, int n_tiles) {
