@@ -123,6 +123,15 @@ bool product_fills(const Product4& P, bool cols) {
     return ceil_div(P.m, 256) * ceil_div(P.n, 256) * (cols ? P.groups : 1) >= 256 && (cols || P.m >= 192 * (int64_t)P.groups);
 }
 
+// Whether tiles of 128 x 128, of which a compute unit has two, are faster: one's first loads and stores are hidden behind the other's stages, which pays for lengths of
+// up to eight stages, and where there is at most one of them for each compute unit.  This form / the larger ones, us a call, bf16: 16384 x 4096 x 1024 70 / 87, x 2048
+// 109 / 103; 32 groups, 20011 x 2048 x 768 54 / 61, x 1792 88 / 78; 1024 x 4096 x 4096 16.8 / 20.7, 2048 rows 30 / 27; by columns, 2048 x 2048 of 2048 rows 12 / 16,
+// 16 groups of 1024 96 / 114, 8 groups of 1250, 2816 x 2048, 79 / 75.
+bool product_short(const Product4& P, bool cols) {
+    const int64_t length = cols ? P.k / P.groups : P.k;
+    return length <= 1024 || ceil_div(P.m, 128) * ceil_div(P.n, 128) * (cols ? P.groups : 1) <= 256;
+}
+
 // Few rows: tiles for which the waves of a workgroup share the length.  Which of them, and whether: the tiles of one group are at most a round of workgroups.
 // 4096 x 4096, us a call, this form / tiles of 128 x 256: 1 row 6.4 / 19, 64 rows 8.4 / 19, 128 rows 9.5 / 19, 256 rows 11.4 / 19, 512 rows 22 / 19.
 // Groups, rows by 16 and columns by 32 / by 32 and 64 / tiles of 128 x 256: 16 of 2816 x 2048, 96 rows 12.5 / 14.4 / 15.9, 256 rows 13.8 / 14.7 / 16.1, 512 rows
@@ -156,7 +165,8 @@ int launch_product(const Product4& P, bool cols, int out_type, void* stream) {
         if (done || !product_large(P, cols)) return;
         done = true;
         with_bool(cols, [&](auto cl) {
-            if (product_fills(P, cols)) launch_tiles<256, 256, 2, 2, cl.value != 0, O>(P, stream);
+            if (product_short(P, cols)) launch_tiles<128, 128, 2, 2, cl.value != 0, O>(P, stream);
+            else if (product_fills(P, cols)) launch_tiles<256, 256, 2, 2, cl.value != 0, O>(P, stream);
             else launch_tiles<128, 256, 2, 2, cl.value != 0, O>(P, stream);
         });
     });

@@ -289,12 +289,13 @@ template <int N, int M> __device__ __forceinline__ void left_and_barrier() {
 // The waves: WM x WN, 32 MT by 32 NT each; a stage is two steps of 64, in which lane (r, g) has block number 2 g + step of row r.
 // 16384 x 8192 x 8192 0.56 to 0.61 ms (3.6 to 3.9 PFLOP/s): eight rounds of 64 stages of 1.8 thousand cycles, 1.0 of them matrix instructions, while the clock
 // falls to some 1.6 GHz.  Short lengths pay the first loads and the stores of every tile: 20011 rows of 32 groups, 3584 x 2048, 154 us, six rounds of 52 thousand
-// cycles, of which 16 stages would be 29.  Tiles of 128 rows at
+// cycles, of which 16 stages would be 29.  128 x 128, two workgroups a compute unit: one's stages run beside the other's first loads and stores, at twice the reads of
+// the LDS for a product (16384 x 4096 x 1024 70 us against 87, x 2048 109 against 103).  Tiles of 128 rows at
 // the ends of groups, and tiles dealt to the XCDs in runs of 32, changed the groups' times by less than one machine differs from itself, and cost the dense ones 2 to 4 %.
 template <bool COLS, class OUT, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles, int n_tiles) {
+__global__ __launch_bounds__(256, BM + BN <= 256 ? 2 : 1) void k_fp4_product(Product4 P, int m_tiles, int n_tiles) {
     constexpr int W = 4, MT = BM / (32 * WM), NT = BN / (32 * WN), LA = BM / 16 / W, LB = BN / 16 / W, LS = ((BM + BN) / 64 + W - 1) / W, PART = (BM + BN) * 64;
-    static_assert(WM * WN == W && LA * 16 * W == BM && LB * 16 * W == BN && BM % 64 == 0 && BN % 64 == 0 && MT % 2 == 0 && NT == 4, "");
+    static_assert(WM * WN == W && LA * 16 * W == BM && LB * 16 * W == BN && BM % 64 == 0 && BN % 64 == 0 && MT % 2 == 0 && (NT == 4 || (NT == 2 && MT == 2)), "");
     __shared__ __align__(1024) uint8_t tile[4][PART];
     __shared__ __align__(1024) uint8_t scale[2][(BM + BN) * 16];
     __shared__ __align__(1024) uint8_t nowhere[W][1024];          // where loads go that ask for no stage
@@ -412,7 +413,7 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
     const int r = lane & 31, g = lane >> 5, mine = r * 64 + (2 * g ^ ((r >> 2) & 3)) * 16;
     constexpr int G = 2 * MT, L = LA + LB;                        // groups of NT products, and loads, of a stage
     // reads that a stage does behind its last one of its own rows (they come back in order): those of the next stage's rows
-    constexpr int LATE = G == 8 ? 5 : 6;
+    constexpr int LATE = G == 8 ? 5 : NT == 4 ? 6 : 4;
     v4u fa[4], fb[2][NT];
     unsigned sa[MT][2], sb[NT][2];
     auto read_a = [&](int part, int i, int h) { return *(const v4u*)&tile[part][(wm * MT + i) * 2048 + (mine ^ h * 16)]; };
@@ -462,7 +463,8 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
                         fa[ahead & 3] = ahead < G ? read_a(U, ahead % MT, ahead / MT) : read_a((U + 1) & 3, ahead - G, 0);
                     } else if constexpr (n <= J1 - J0) {
                         fb[h ^ 1][J0 + n - 1] = h == 0 ? read_b(U, J0 + n - 1, 1) : read_b((U + 1) & 3, J0 + n - 1, 0);
-                    } else if constexpr (n == J1 - J0 + 1) {
+                    }
+                    if constexpr (n == (J1 - J0 + 1 < NT ? J1 - J0 + 1 : NT - 1)) {
 #pragma unroll
                         for (int j = q * L / G; j < (q + 1) * L / G; ++j) ask(s + 3, (U + 3) & 3, j);
                     }
@@ -482,8 +484,10 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
                 };
                 product(Int<0>{});
                 product(Int<1>{});
-                product(Int<2>{});
-                product(Int<3>{});
+                if constexpr (NT == 4) {
+                    product(Int<2>{});
+                    product(Int<3>{});
+                }
             };
             group(Int<0>{});
             group(Int<1>{});
@@ -526,10 +530,10 @@ __global__ __launch_bounds__(256, 1) void k_fp4_product(Product4 P, int m_tiles,
                     const v16f& c = acc[i1 + i][j];
                     uint8_t* row = own + (i * 32 + r) * CH * 16;
                     if constexpr (SZ == 2)
-                        *(v2u*)(row + ((j * 4 + q) ^ (r & 15)) * 16 + g * 8) = v2u{(unsigned)to_bf16(c[q * 4]) | (unsigned)to_bf16(c[q * 4 + 1]) << 16,
+                        *(v2u*)(row + ((j * 4 + q) ^ (r & (CH - 1))) * 16 + g * 8) = v2u{(unsigned)to_bf16(c[q * 4]) | (unsigned)to_bf16(c[q * 4 + 1]) << 16,
                                                                                   (unsigned)to_bf16(c[q * 4 + 2]) | (unsigned)to_bf16(c[q * 4 + 3]) << 16};
                     else
-                        *(v4f*)(row + ((j * 8 + q * 2 + g) ^ r) * 16) = v4f{c[q * 4], c[q * 4 + 1], c[q * 4 + 2], c[q * 4 + 3]};
+                        *(v4f*)(row + ((j * 8 + q * 2 + g) ^ (r & (CH - 1))) * 16) = v4f{c[q * 4], c[q * 4 + 1], c[q * 4 + 2], c[q * 4 + 3]};
                 }
         wave_lds_done();
 #pragma unroll 4
