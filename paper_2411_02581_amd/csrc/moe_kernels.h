@@ -1223,7 +1223,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
                     dma16(from_g, off[0], to);
                     dma16(from_g, off[1], to + 1024);
                     dma16(from_u, off[0], to + 2048);
-                    dma16(from_u, off[1], to + 3072);
+                    dma16(from_u, off[1], to + 3 * 1024);
                     t.k = v2u{0u, 0u};
                     if (lane < 32) __builtin_memcpy(&t.k, scale_row + b * Wp::kScales, 8);
 #pragma unroll
