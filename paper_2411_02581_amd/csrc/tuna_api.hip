@@ -2200,7 +2200,12 @@ int plan_build_metadata(Plan* plan, void* meta, size_t mbytes, hipStream_t s, bo
     }
     // exact unit counts, bytes and staged chunks per phase: one read-back of the status block
     const Status* h_status = pr.sb.h_status;
-    HIPCHK(hipMemcpyAsync(pr.sb.h_status, pr.sb.d_status, sizeof(Status), hipMemcpyDeviceToHost, s));
+    if (pr.sb.h_status_dev) {
+        hipLaunchKernelGGL(k_mirror_counts, dim3(1), dim3(256), 0, s, pr.sb.d_status, pr.sb.h_status_dev);
+        HIPCHK(hipGetLastError());
+    } else {
+        HIPCHK(hipMemcpyAsync(pr.sb.h_status, pr.sb.d_status, sizeof(Status), hipMemcpyDeviceToHost, s));
+    }
     HIPCHK(hipStreamSynchronize(s));
     unsigned long long max_chunks = 0;
     if (pr.self_engine && !longs) pr.self_units = h_status->self_units;     // exact from now on

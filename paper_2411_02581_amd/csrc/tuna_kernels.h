@@ -611,6 +611,21 @@ __global__ void __launch_bounds__(256) k_validate_finish(const unsigned long lon
     }
 }
 
+// k_mirror_counts: what the metadata kernels have counted, from a status block to pinned host memory, for the host to read once the stream has ended (one
+// workgroup).  A copy command of these bytes goes through a copy engine, which on some machines and in some processes serves the queue in turns: whole
+// series of calls in two passes then ended on multiples of 7.5 ms (P = 1024, 16 ranks a node, staged, 2.5 ms of work: 7.5 ms a call, 5.0 of them the copy on
+// an idle stream); by this kernel 2.5 ms always.
+__global__ void __launch_bounds__(256) k_mirror_counts(const Status* __restrict__ st, Status* __restrict__ mirror) {
+    if (threadIdx.x < 64) {
+        const int i = threadIdx.x;
+        mirror->phase_bytes[i] = st->phase_bytes[i];
+        mirror->phase_chunks[i] = st->phase_chunks[i];
+        mirror->phase_units[i][0] = st->phase_units[i][0];
+        mirror->phase_units[i][1] = st->phase_units[i][1];
+    }
+    if (threadIdx.x == 64) mirror->self_units = st->self_units;
+}
+
 // ------------------------------------------------------------------------------------------
 // k_rotate_init: the index-only initial rotation (Algorithm "TuNA", lines 4-5; Algorithm
 // "Coalesced TuNA_l^g", line 5).  No payload moves: cur[p][j*Q + l] becomes the size of the
