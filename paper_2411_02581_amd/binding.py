@@ -462,8 +462,10 @@ def _misfit(a: Any, code: int, types: dict) -> None:
         import torch
         # 8-bit values and exponents travel as bytes too: the rows of a record are a tensor of bytes
         _scale_types.update({TUNA_SCALE_F32: (torch.float32,), TUNA_SCALE_E8: (torch.uint8, torch.float8_e8m0fnu)})
+        # (not every torch has a type of two 4-bit values)
+        pairs = getattr(torch, "float4_e2m1fn_x2", None)
         _value_types.update({TUNA_F32: (torch.float32,), TUNA_BF16: (torch.bfloat16,), TUNA_F8: (torch.float8_e4m3fn, torch.uint8),
-                             TUNA_F4: (torch.uint8, torch.float4_e2m1fn_x2)})
+                             TUNA_F4: (torch.uint8,) if pairs is None else (torch.uint8, pairs)})
     if a.dtype not in types.get(code, (a.dtype,)):
         raise TypeError("tensor dtype %s, expected %s" % (a.dtype, " or ".join(str(t) for t in types[code])))
 
