@@ -46,6 +46,13 @@ def quantise_weights_4(w):
     return q, s
 
 
+def rows_on_16(s):
+    """A copy of rows of scales in 4 bits that start on 16 bytes, as the products of many rows want them (tuna_moe_few takes them back to back)."""
+    p = torch.zeros(*s.shape[:2], -(-s.shape[2] // 16) * 16, dtype=s.dtype, device=s.device)
+    p[..., :s.shape[2]] = s
+    return p
+
+
 class ExpertParallel:
     """w1 [experts, 2 inner, hidden] (gate rows, then up rows), w2 [experts, hidden, inner]; buffers for up to max_tokens tokens; rows and weights in
     `bits` bits, 8 or 4."""
@@ -57,9 +64,11 @@ class ExpertParallel:
         self.k, self.per_node, self.max_tokens, self.bits, dev = k, experts_per_node, max_tokens, bits, w1.device
         held = quantise_weights if bits == 8 else quantise_weights_4
         (self.w1, self.s1), (self.w2, self.s2) = held(w1), held(w2)
+        self.p1, self.p2 = (self.s1, self.s2) if bits == 8 else (rows_on_16(self.s1), rows_on_16(self.s2))
         e, h, f, pairs = self.experts, self.hidden, self.inner, max_tokens * k
         size = (lambda n: (n, _blocks(n))) if bits == 8 else (lambda n: (-(-n // 2), -(-n // 32)))
-        (self.h_bytes, h_scales), (self.f_bytes, self.f_scales) = size(h), size(f)       # of a row's values, and its scales
+        (self.h_bytes, h_scales), (self.f_bytes, f_scales) = size(h), size(f)       # of a row's values, and its scales
+        self.f_scales = f_scales if bits == 8 else -(-f_scales // 16) * 16          # the distance of two rows'
         self.record = -(-(self.h_bytes + h_scales) // 16) * 16   # values, then scales; rows on 16 bytes
         new = lambda *s, dtype=torch.uint8: torch.empty(*s, dtype=dtype, device=dev)  # noqa: E731
         self.rows = new(e + 1, dtype=torch.int32)
@@ -121,9 +130,9 @@ class ExpertParallel:
         # the plan counts rows (records of one byte): times a record's size it is the call's
         sc, sd, rc, rd = (m * self.record for m in self.plan)
         _ok(tuna.tuna_alltoallv(send, sc, sd, recv, rc, rd, e, tuna.TUNA_RADIX_AUTO, self.per_node))
-        self._multiply(recv, self.record, recv[:, self.h_bytes:], self.record, self.w1, self.s1, self.mid, pairs, 2 * f, h)
+        self._multiply(recv, self.record, recv[:, self.h_bytes:], self.record, self.w1, self.p1, self.mid, pairs, 2 * f, h)
         self._pack(self.mid, 2 * f, pairs, f, tuna.TUNA_ACT_SWIGLU, None, 1, pairs, self.q, self.f_bytes, self.qs, self.f_scales)
-        self._multiply(self.q, self.f_bytes, self.qs, self.f_scales, self.w2, self.s2, self.y, pairs, h, f)
+        self._multiply(self.q, self.f_bytes, self.qs, self.f_scales, self.w2, self.p2, self.y, pairs, h, f)
         sc, sd, rc, rd = (m * (2 * h) for m in self.plan)
         _ok(tuna.tuna_alltoallv(self.y, rc, rd, self.back, sc, sd, e, tuna.TUNA_RADIX_AUTO, self.per_node))
         _ok(tuna.tuna_moe_combine(self.back, tuna.TUNA_BF16, h, pairs, slots, weights, t, k, h, out, tuna.TUNA_BF16, h))
