@@ -1323,7 +1323,7 @@ template <class W, int KIND, bool WIDE, class OUT, bool ONE>
 __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
     extern __shared__ float shared[];                             // [kFewSecond][tokens][16] sums
     constexpr bool RING = WIDE && Part<W>::INSIDE;
-    constexpr int TASK = Part<W>::INSIDE ? 4 : 16;                // pairs of a task
+    constexpr int TASK = RING ? 4 : 16;                           // pairs of a task
     __shared__ __align__(1024) uint8_t ring[kFewSecond][RING ? Part<W>::kAhead2 : 1][RING ? 2048 : 16];
     constexpr int PAIRS = TUNA_MOE_FEW_TOKENS * TUNA_MOE_MAX_K;
     __shared__ int pair_of[PAIRS];                                // pairs by expert

@@ -1,4 +1,5 @@
-"""tuna_moe_few with 4-bit weights whose scales lie at the ends of their range: NaN (255), and powers of two from 2^-127 on, where weights are subnormal in bf16."""
+"""tuna_moe_few with 4-bit weights whose scales lie at the ends of their range, NaN (255) and powers of two from 2^-127 on, where weights are subnormal in bf16; and with
+many pairs of an expert."""
 import pytest
 import torch
 
@@ -81,3 +82,13 @@ def test_large_scales(t, h, f, e, k):
     layer.s[0] = (layer.s[0].int() + 127).clamp_max(252).to(U8)
     layer.x = (layer.x.float() * 2.0 ** -125).bfloat16()
     layer.check()
+
+
+@pytest.mark.parametrize("t,h,f,e,k", [(64, 200, 88, 2, 2), (64, 200, 88, 3, 2), (40, 1000, 232, 4, 4), (64, 200, 88, 20, 1), (64, 256, 512, 2, 2), (33, 512, 640, 3, 3)])
+def test_more_pairs_of_an_expert_than_a_task_has(t, h, f, e, k):
+    """Sixteen pairs, or four where rows start on 16 bytes: the same every time."""
+    layer = Layer(t, h, f, e, k)
+    layer.check()
+    first = layer.run()
+    for _ in range(5):
+        assert torch.equal(layer.run(), first)
