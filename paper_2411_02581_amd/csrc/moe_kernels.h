@@ -951,7 +951,6 @@ template <> struct Part<Four> {
         const int64_t over = b * kScales + part - ((cols + kBlock4 - 1) / kBlock4 - 1);
         return over > 0 ? at - over : at;
     }
-    __device__ __forceinline__ void whole(const Four* base, unsigned off) { v = *(const v4u*)((const uint8_t*)base + (size_t)off); }
     template <bool WIDE> __device__ __forceinline__ void load(const Four* p, int part, int64_t left) { v = chunk32<WIDE>((const uint8_t*)p + part * 16, left - part * 32); }
     __device__ __forceinline__ v8b eight(int h, float k) const {
         const v2b a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[h], k, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[h], k, 1);
