@@ -25,7 +25,8 @@
  *     back before anything is enqueued.  Indices that live on the device (slots, expert numbers, group_rows) are held
  *     inside their arrays by the kernels: a slot or an expert outside its range counts as -1 (absent), a group bound
  *     counts as the largest of all bounds up to it, inside [0, m], so that groups never overlap.
- *   - Rows, columns and (token, expert) pairs number at most 2^31 - 1 each.  With b = 2^24 - 1, what a launch has threads for:
+ *   - Rows, columns and (token, expert) pairs number at most 2^31 - 1 each, groups of rows (experts, packed sequences) 1 to
+ *     TUNA_MOE_MAX_EXPERTS in every call that has them.  With b = 2^24 - 1, what a launch has threads for:
  *     the router and its gradient take 4 b tokens, the sum's gradient b tokens, tuna_fp8_quantize 32 b blocks of 128 values,
  *     its form by columns b blocks of rows and 128 * 65535 columns; products of rows off 16 bytes 64 b rows; y has up to
  *     64 * 65535 columns (dw: its k); the sum and the gate's gradient take 2^31 - 2^15 rows.  In 4 bits the blocks of 32 of all rows
@@ -33,7 +34,11 @@
  *   - Values: TUNA_F32, TUNA_BF16, TUNA_F8 (e4m3, largest 448, no infinity), TUNA_F4 (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
  *     negatives, two to a byte, the first in the low half; a row starts on a byte, and the high half behind an odd row's last value is
  *     written as 0 and not read).  Pointers are aligned to their elements; operands whose rows start on 16 bytes (and have such a
- *     distance) run wider loads, in 4 bits where the rows of scales start on 4 bytes too.
+ *     distance) run wider loads.
+ *   - The products in 4 bits go by their scales too.  Their tiles want rows and groups of values AND of scales on 16 bytes (the distances as
+ *     well): a row of ceil(k / 32) scales is then held in the next multiple of 16.  The form for few rows wants values on 16 and scales on 4 bytes.
+ *     All else runs a simple form: right, and slow.  20011 rows of 32 groups: 2048 x 1792 77 us, with rows of 56 scales 195; 5632 x 2880 0.37 ms,
+ *     with rows of 92 scales 1.2, of 90 scales 6.8; 60 rows of 4096 x 2880 6 us, with rows of 90 scales 75.
  *   - Sums, softmax statistics and products are accumulated in 32 bits and rounded once, to the type of the output, but for two
  *     places.  (1) The products of tuna_fp8_matmul(_grad_w) with an output of TUNA_BF16 run on the 8-bit matrix cores, which
  *     add eight neighbouring products at a time, each cut at 2^-13 of the largest one's power of two: off by at most 2^-10 of
@@ -109,6 +114,8 @@ int tuna_moe_route_grad(const void* logits, int type, int64_t ld, int64_t n_toke
  *   group_rows [groups + 1]: the sequences' bounds in the tokens, or NULL for one sequence of all tokens.  Tokens outside every
  *             sequence count nowhere.
  *   counts    [groups, n_experts]: how many of the sequence's (token, expert) pairs the expert has.
+ *             More than TUNA_MOE_MAX_EXPERTS sequences: a call for each so many of them (group_rows, counts, tokens, shares and loss from
+ *             there on), and the gradient with TUNA_BALANCE_ADD to zeros.
  *   tokens    [groups]: how many of its tokens have an eligible expert.
  *   shares    [groups, n_experts]: the mean over those tokens of the softmax over all eligible logits.
  *   loss      [groups].  All four are written whole.
@@ -204,7 +211,9 @@ int tuna_fp4_dequantize(const void* q, int64_t ldq, const void* scales, int64_t 
  *   group_rows [groups + 1]: the groups' bounds in the rows of x and y, or NULL for one group of all rows.  Rows outside
  *   every group are not written.
  * The gradient of x is the same product of dy in 4 bits with w in 4 bits along its other axis: tuna_fp4_quantize_columns of w as
- * [groups * n, k] with the bounds 0, n, 2 n, ... leaves it so, with w_group = 64 ceil(n / 128) and ws_group = 4 ceil(n / 128).
+ * [groups * n, k] with the bounds 0, n, 2 n, ... leaves it so, with w_group = 64 ceil(n / 128) and ws_group = 4 ceil(n / 128), which is
+ * a multiple of 16 where ceil(n / 128) is one of 4.  A call for each group leaves any distance, and so scales on 16 bytes for every n (10007
+ * rows of 8 groups, 2816 x 2048: the product 64 us in place of 154, the calls 70 in place of 35 once for each new w).
  */
 int tuna_fp4_matmul(const void* x, int64_t ldx, const void* xs, int64_t ld_xs,
                     const void* w, int64_t ldw, int64_t w_group, const void* ws, int64_t ld_ws, int64_t ws_group,
@@ -236,7 +245,7 @@ int tuna_moe_combine_grad(const void* dout, int out_type, int64_t ld_dout, const
  * The whole layer for at most TUNA_MOE_FEW_TOKENS tokens, in two kernels, for serving:
  *     out[t] = sum over the chosen experts e: weight(t, e) * w2[e] (silu(gate) * up),   [gate | up] = w1[e] x[t]
  * with the choice and the weights of tuna_moe_route.  A chosen expert's weights are read once for up to 16 of its tokens, w1 for up
- * to 32 where the experts have more than 8 pairs on average, and again for as many more.
+ * to 32 where the experts have more than 8 pairs on average, w2 in 4 bits whose rows start on 16 bytes for up to 4, and again for as many more.
  *   x  [n_tokens, hidden] TUNA_BF16;  logits [n_tokens, n_experts] TUNA_F32 or TUNA_BF16
  *   w1 [n_experts, 2 inner, hidden], w2 [n_experts, hidden, inner], dense: TUNA_F8 with s1 [n_experts, ceil(2 inner / 128),
  *      ceil(hidden / 128)], s2 [n_experts, ceil(hidden / 128), ceil(inner / 128)], or TUNA_BF16 (s1 = s2 = NULL), or TUNA_F4 (rows of
