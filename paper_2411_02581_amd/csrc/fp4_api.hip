@@ -109,7 +109,8 @@ template <int BM, int BN, int WM, int WN, bool COLS, class OUT> void launch_tile
     LAUNCH((k_fp4_product<COLS, OUT, BM, BN, WM, WN>), dim3((unsigned)grid), 256, P, (int)mt, (int)nt);
 }
 
-// Tiles of the large form: rows of scales start on 16 bytes, offsets inside a tile are 32 bits, and there is a whole stage of 128.
+// Tiles of the large form: rows of scales start on 16 bytes, as wide as their loads (where they do not, the simple form: 20011 rows of 32 groups, 2048 x 1792,
+// 195 us for 77; dx by columns, 10007 rows of 8, 2816 x 2048, 154 for 64), offsets inside a tile are 32 bits, and there is a whole stage of 128.
 bool product_large(const Product4& P, bool cols) {
     const int64_t nt = ceil_div(P.n, 128), mt = ceil_div(P.m, 128) + (cols ? 0 : P.groups - 1);
     return product_wide(P) && on(P.as, 16) && on(P.bs, 16) && P.ld_as % 16 == 0 && P.ld_bs % 16 == 0 && P.bs_group % 16 == 0 && P.lda < (1 << 22) && P.ldb < (1 << 22) &&
@@ -124,9 +125,9 @@ bool product_fills(const Product4& P, bool cols) {
 }
 
 // Whether tiles of 128 x 128, of which a compute unit has two, are faster: one's first loads and stores are hidden behind the other's stages, which pays for lengths of
-// up to eight stages, and where there is at most one of them for each compute unit.  This form / the larger ones, us a call, bf16: 16384 x 4096 x 1024 70 / 87, x 2048
+// up to eight stages, and where there is at most one of them for each compute unit.  This form / the larger ones, us a call, bf16, on two machines: 16384 x 4096 x 1024 64 to 70 / 87, x 2048
 // 109 / 103; 32 groups, 20011 x 2048 x 768 54 / 61, x 1792 88 / 78; 1024 x 4096 x 4096 16.8 / 20.7, 2048 rows 30 / 27; by columns, 2048 x 2048 of 2048 rows 12 / 16,
-// 16 groups of 1024 96 / 114, 8 groups of 1250, 2816 x 2048, 79 / 75.
+// 16 groups of 1024 96 to 99 / 114, 8 groups of 1250, 2816 x 2048, 79 / 75.
 bool product_short(const Product4& P, bool cols) {
     const int64_t length = cols ? P.k / P.groups : P.k;
     return length <= 1024 || ceil_div(P.m, 128) * ceil_div(P.n, 128) * (cols ? P.groups : 1) <= 256;
@@ -135,7 +136,9 @@ bool product_short(const Product4& P, bool cols) {
 // Few rows: tiles for which the waves of a workgroup share the length.  Which of them, and whether: the tiles of one group are at most a round of workgroups.
 // 4096 x 4096, us a call, this form / tiles of 128 x 256: 1 row 6.4 / 19, 64 rows 8.4 / 19, 128 rows 9.5 / 19, 256 rows 11.4 / 19, 512 rows 22 / 19.
 // Groups, rows by 16 and columns by 32 / by 32 and 64 / tiles of 128 x 256: 16 of 2816 x 2048, 96 rows 12.5 / 14.4 / 15.9, 256 rows 13.8 / 14.7 / 16.1, 512 rows
-// 19 / 14.9 / 16.7, 1024 rows 32 / 25 / 17; 64 of 3584 x 4096, 512 rows 89 / 94 / 121, 1024 rows 107 / 102 / 127, 2048 rows 157 / 114 / 127.
+// 19 / 14.9 / 16.7, 1024 rows 32 / 25 / 17; 64 of 3584 x 4096, 512 rows 89 / 94 / 121, 1024 rows 107 / 102 / 127, 2048 rows 157 / 114 / 127.  The host has the mean alone, for the
+// bounds are the device's: one group with half of the rows, 64 of 3584 x 4096, 768 rows 106 / 102 / 118, 1024 117 / 108 / 119, 2048 171 / 134 / 128; 128 of 2816 x 4096,
+// 768 rows 147 / 145 / 177, 2048 189 / 168 / 185, 4096 270 / 210 / 209; 16 of 2816 x 2048, 256 rows 15.6 / 15.3 / 17.0: at worst 15 % beside the best.
 template <class F> bool product_thin(const Product4& P, F rows) {
     if (!product_wide(P) || P.ldb >= (1 << 24) || ceil_div(P.m, 16) + P.groups > kMaxGridY || ceil_div(P.n, 16) > kMaxRows / 512) return false;
     if (P.groups > 1) {

@@ -282,15 +282,16 @@ template <int N, int M> __device__ __forceinline__ void left_and_barrier() {
 }
 
 // The large form: a tile of BM x BN, four waves, stages of 128 of the length through four parts of the LDS.  While a stage is multiplied, the next
-// one's rows go from the LDS to registers, the two behind it are on their way and the one after them is asked for: a load has three stages' time (some
-// 1.3 us in the largest tile) to arrive, and between stages there is one barrier.  A row of a stage is 64 bytes; its sixteen number c lies at place c xor
+// one's rows go from the LDS to registers, the one behind it is on its way and the one after that is asked for: a load has from one to two stages' time to arrive
+// (in the largest tile 1.1 to 2.2 us, a stage being 1.8 thousand cycles at 1.6 GHz), and between stages there is one barrier.  A row of a stage is 64 bytes; its sixteen number c lies at place c xor
 // (row / 4 mod 4), so that the lanes that the LDS serves together meet every bank once.  The scales come in sixteens, for four stages (512 of the
 // length, from multiples of 512); a lane collects its blocks' bytes of two stages in one register, of which a product takes byte STEP.
 // The waves: WM x WN, 32 MT by 32 NT each; a stage is two steps of 64, in which lane (r, g) has block number 2 g + step of row r.
 // 16384 x 8192 x 8192 0.56 to 0.61 ms (3.6 to 3.9 PFLOP/s): eight rounds of 64 stages of 1.8 thousand cycles, 1.0 of them matrix instructions, while the clock
 // falls to some 1.6 GHz.  Short lengths pay the first loads and the stores of every tile: 20011 rows of 32 groups, 3584 x 2048, 154 us, six rounds of 52 thousand
 // cycles, of which 16 stages would be 29.  128 x 128, two workgroups a compute unit: one's stages run beside the other's first loads and stores, at twice the reads of
-// the LDS for a product (16384 x 4096 x 1024 70 us against 87, x 2048 109 against 103).  Tiles of 128 rows at
+// the LDS for a product (16384 x 4096 x 1024 64 to 70 us against 87, x 2048 109 against 103).  Rows of scales start on 16 bytes, for their loads are as wide; others
+// go to the simple form.  The instances of 128 x 256 by columns keep 32 bytes a lane in scratch, none other does.  Tiles of 128 rows at
 // the ends of groups, and tiles dealt to the XCDs in runs of 32, changed the groups' times by less than one machine differs from itself, and cost the dense ones 2 to 4 %.
 template <bool COLS, class OUT, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(256, BM + BN <= 256 ? 2 : 1) void k_fp4_product(Product4 P, int m_tiles, int n_tiles) {
@@ -561,7 +562,8 @@ __global__ __launch_bounds__(256, BM + BN <= 256 ? 2 : 1) void k_fp4_product(Pro
 // The form for few rows, which reads the weights once and little else: a workgroup has 16 NT rows of b and 16 MT rows of a, its W waves share the length
 // in units of 256, and the waves' sums are added up in their order.  Rows of b go through the LDS, a wave's own part of it, in whole pieces of 128 bytes
 // (sixteen number i of a row at place i xor (row / 2 mod 8)): the product's lanes, sixteen rows side by side, would ask for every sixteen bytes by
-// themselves.  A row's scales of a unit are two words in the lane of its number, read by those that need them.
+// themselves.  A row's scales of a unit are two words in the lane of its number, read by those that need them.  These loads hang on the lane, and the compiler does
+// not count the rows' loads into the LDS: it waits for more than it has to, and of the AHEAD units the one just asked for is often the only one under way.
 // 40 x 4096 x 2880 5.1 us, most of it the way there and back; 96 rows of 16 groups, 2816 x 2048, 49 MB, 13 us (3.7 TB/s).  Loads of scales by all lanes, so that none
 // hangs on a condition: 6.0 and 14.4 us.
 template <class OUT, int MT, int NT, int W>

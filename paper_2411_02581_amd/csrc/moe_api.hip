@@ -440,11 +440,15 @@ int tuna_moe_few(const void* x, int64_t ldx, int64_t n_tokens, int64_t hidden, c
     // 16 columns, so that there are workgroups enough for the device; many: each wave has 16, and fewer workgroups look for their tokens.
     // Calls, shared / each 16: 8-bit weights, k = 4 of 64 experts, 1024 x 2048: 3 tokens 45 / 52 us, 4 54 / 56, 8 97 / 80, 12 120 / 95, 16 135 / 100;
     // bf16: 4 tokens 76 / 88, 8 123 / 126, 16 169 / 155.  k = 8 of 128, 1536 x 4096: 2 tokens 130 / 114, 5 245 / 216, 24 640 / 530, 40 755 / 580.
-    // k = 2 of 8, 1536 x 4096: 16 tokens 59 / 72.  What counts is how many experts have a token times their columns: the limit here is the pairs'.
+    // k = 2 of 8, 1536 x 4096: 16 tokens 59 / 72.  4-bit weights: k = 4 of 64, 1024 x 2048: 2 tokens 23.5 / 23.2, 8 43 / 41, 12 55 / 48, 16 61 / 53, 64 131 / 114; k = 8
+    // of 128, 1408 x 4096: 2 tokens 59 / 51, 5 105 / 98, 24 259 / 229, 48 364 / 321; k = 2 of 8, 1536 x 4096: 16 tokens 34 / 46; k = 8 of 8, 1024 x 2048: 4 tokens
+    // 21 / 26, 16 41 / 46, 64 125 / 149.  What counts is how many experts have a token times their columns: the limit here is the pairs'.
     const bool one = n_tokens == 1, split = one || (int64_t)pairs * ceil_div(inner, 64) < 1024;
     // Up to 8 pairs an expert 16 tokens at a time, else 32 (fewer waves have room).  16 / 32, 8-bit weights, 64 tokens, 1024 x 2048: k = 2 of 8 experts
     // 82 / 69 us, k = 2 of 16 65 / 65, k = 4 of 16 104 / 91, k = 4 of 32 109 / 109, k = 4 of 64 184 / 177; 16 tokens, k = 4 of 64, 101 / 126;
-    // k = 8 of 128, 1536 x 4096: 24 tokens 530 / 597, 40 tokens 584 / 667, 64 tokens 644 / 718.
+    // k = 8 of 128, 1536 x 4096: 24 tokens 530 / 597, 40 tokens 584 / 667, 64 tokens 644 / 718.  4-bit weights, 64 tokens, 1024 x 2048: k = 2 of 8 62 / 61, k = 2 of
+    // 16 56 / 58, k = 4 of 16 85 / 84, k = 4 of 32 84 / 84, k = 4 of 64 114 / 114, k = 8 of 8 149 / 145 (8 bits 166); k = 8 of 128, 1408 x 4096: 24 tokens 229 / 263,
+    // 48 321 / 356, 64 361 / 400.
     const dim3 g1((unsigned)ceil_div(inner, split ? 16 : 16 * kFewFirst), (unsigned)(one ? k : n_experts)), g2((unsigned)ceil_div(hidden, 16));
     const size_t sums = (size_t)kFewSecond * n_tokens * 16 * 4;
     int e = TUNA_OK;

@@ -300,7 +300,8 @@ __device__ __forceinline__ int count_tiles(const int32_t* group_rows, int groups
 // ------------------------------------------------------------------------------------------------ loads and stores
 
 // Units lo .. hi - 1: each is fetched AHEAD - 1 units before it is used.  In the loop no load hangs on a condition, so that a wait for one unit's
-// leaves the later ones' under way.  MANY: the loop runs to the end, where it fetches the last unit again; else the end is a loop of its own,
+// leaves the later ones' under way, as long as none does in `fetch`.  (Those of the 4-bit forms do, and load into the LDS besides, which the compiler does not
+// count: it then waits for all loads once a unit, or once in AHEAD units, the last asked for included.)  MANY: the loop runs to the end, where it fetches the last unit again; else the end is a loop of its own,
 // which costs registers and spares short runs those loads (one token: both kernels 23.1 us with them, 18.2 without).
 template <int AHEAD, bool MANY, class S, class FETCH, class USE> __device__ __forceinline__ void pipeline(S (&st)[AHEAD], int lo, int hi, FETCH fetch, USE use) {
     if (MANY && lo >= hi) return;

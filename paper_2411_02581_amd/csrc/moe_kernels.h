@@ -1193,7 +1193,8 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
             // would ask for every sixteen bytes by themselves; two blocks at a time, so that a piece is 128 bytes.  The scales of gate rows and up rows are two words in the lanes 0 to 31.  A wait for the
             // scales, which are asked for behind the weights, is a wait for these.  Up to 4 (8) tokens: the lanes of places without one load the
             // tokens' later steps, P = 4 (2) steps in one load.  48 tokens, k = 8 of 128 experts, 1408 x 4096, first kernel: 316 us without all this,
-            // 250 with the weights through the LDS, 194 so (0.78 GB, 4.0 TB/s; a stage more ahead, without a condition on any load, gives the same).
+            // 250 with the weights through the LDS, 194 so (0.78 GB, 4.0 TB/s; a stage more ahead, without a condition on any load, gives the same while the
+            // compiler sets the waits: it waits for all loads, those of the next unit too).
             auto stream = [&](auto packed) {
                 constexpr int P = packed.value;
                 struct Ahead { v2u k; v8b a[MT][2][4 / P]; };
@@ -1315,8 +1316,8 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void k_few_first(Few F) {
 }
 
 // Second kernel: a workgroup per 16 columns of the result, for all tokens and chosen experts.  A task is a chosen expert with up to 16 of its
-// pairs (more of them read its weights again); 0.74 GB in 210 us, 3.5 TB/s, and 8.4 MB in 7 us for the sizes above; 4-bit weights, 48 tokens, 1408 x 4096:
-// 0.39 GB in 146 us.  The tasks' steps are one sequence, of which every wave has a run; a wave's sums are its own,
+// pairs (more of them read its weights again), with up to four where 4-bit weights go through the LDS; 0.74 GB in 210 us, 3.5 TB/s, and 8.4 MB in 7 us for the sizes above; 4-bit weights, 48 tokens, 1408 x 4096:
+// 0.39 GB in 146 us (2.7 TB/s: once in four units all loads are waited for).  The tasks' steps are one sequence, of which every wave has a run; a wave's sums are its own,
 // and at the end they are added up in the waves' order.
 template <class W, int KIND, bool WIDE, class OUT, bool ONE>
 __global__ __launch_bounds__(kFewSecond * 64) void k_few_second(Few F) {
