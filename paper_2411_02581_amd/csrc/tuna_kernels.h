@@ -613,8 +613,8 @@ __global__ void __launch_bounds__(256) k_validate_finish(const unsigned long lon
 
 // k_mirror_counts: what the metadata kernels have counted, from a status block to pinned host memory, for the host to read once the stream has ended (one
 // workgroup).  A copy command of these bytes goes through a copy engine, which on some machines and in some processes serves the queue in turns: whole
-// series of calls in two passes then ended on multiples of 7.5 ms (P = 1024, 16 ranks a node, staged, 2.5 ms of work: 7.5 ms a call, 5.0 of them the copy on
-// an idle stream); by this kernel 2.5 ms always.
+// series of calls in two passes then ended on multiples of 7.5 ms (P = 2048, 32 ranks a node, radices 32 and 64, staged, 2.5 ms of work: 7.5 ms a call, 5.0 of them
+// the copy on an idle stream); by this kernel 2.5 ms always.
 __global__ void __launch_bounds__(256) k_mirror_counts(const Status* __restrict__ st, Status* __restrict__ mirror) {
     if (threadIdx.x < 64) {
         const int i = threadIdx.x;
